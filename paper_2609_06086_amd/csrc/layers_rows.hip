@@ -1,0 +1,431 @@
+// Row operators of poseidon_layers.h: the 8-bit form of activations, the gated
+// activation, the experts' gather and combination, the embedding lookup.  Each
+// reads its inputs once and writes its outputs once; memory bounds all of them.
+#include "layers_device.h"
+
+namespace pl {
+
+// ---- activations kept in 8 bits ----
+
+// Codes and scale bytes have no gaps, so a lane's slice is slice i of both.
+template <class T>
+__global__ __launch_bounds__(kBlock) void stash_kernel(const typename T::raw *x, uint64_t pitch, uint32_t total,
+                                                       Div per_row, uint32_t width, int8_t *codes, uint8_t *scales) {
+    const uint32_t i = blockIdx.x * kBlock + threadIdx.x;
+    if (i >= total) return;    // whole groups of 8 lanes: total is a multiple of 8
+    const uint32_t row = quotient(i, per_row), s = i - row * per_row.d;
+    float v[8];
+    load_slice<T>(x + (uint64_t)row * pitch, s * kSlice, width, v);
+    const uint32_t byte = scale_byte<T>(v);
+    uint32_t w[2];
+    codes_of(v, byte, w);
+    reinterpret_cast<uint2 *>(codes)[i] = make_uint2(w[0], w[1]);
+    if (!(i & 7)) scales[i >> 3] = (uint8_t)byte;
+}
+
+template <class T>
+__global__ __launch_bounds__(kBlock) void restore_kernel(const int8_t *codes, const uint8_t *scales, uint32_t total,
+                                                         Div per_row, uint32_t width, typename T::raw *out,
+                                                         uint64_t pitch) {
+    const uint32_t i = blockIdx.x * kBlock + threadIdx.x;
+    if (i >= total) return;
+    const uint32_t row = quotient(i, per_row), s = i - row * per_row.d;
+    uint32_t w[2];
+    load_codes(codes, i, w);
+    float v[8];
+    values_of(w, scale_of(scales[i >> 3]), v);
+    store_slice<T>(out + (uint64_t)row * pitch, s * kSlice, width, v);
+}
+
+// ---- gated activation ----
+
+// 1 / (1 + exp(-z)).  16-bit outputs take the hardware's exponential and
+// reciprocal (about 1e-7 off); 32-bit ones the exact-to-the-last-bits functions.
+template <class T>
+__device__ __forceinline__ float sigmoid(float z) {
+    if constexpr (T::kShort)
+        return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * z));
+    else
+        return 1.0f / (1.0f + expf(-z));
+}
+
+template <class T, bool KEEP>
+__global__ __launch_bounds__(kBlock) void gated_forward_kernel(
+    const typename T::raw *gate, uint64_t gate_pitch, const typename T::raw *up, uint64_t up_pitch, uint32_t total,
+    Div per_row, uint32_t width, typename T::raw *out, uint64_t out_pitch, int8_t *gate_codes, uint8_t *gate_scales,
+    int8_t *up_codes, uint8_t *up_scales) {
+    const uint32_t i = blockIdx.x * kBlock + threadIdx.x;
+    if (i >= total) return;
+    const uint32_t row = quotient(i, per_row), s = i - row * per_row.d;
+    float g[8], u[8], h[8];
+    load_slice<T>(gate + (uint64_t)row * gate_pitch, s * kSlice, width, g);
+    load_slice<T>(up + (uint64_t)row * up_pitch, s * kSlice, width, u);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) h[j] = g[j] * sigmoid<T>(g[j]) * u[j];
+    store_slice<T>(out + (uint64_t)row * out_pitch, s * kSlice, width, h);
+    if constexpr (KEEP) {
+        uint32_t w[2];
+        const uint32_t bg = scale_byte<T>(g), bu = scale_byte<T>(u);
+        codes_of(g, bg, w);
+        reinterpret_cast<uint2 *>(gate_codes)[i] = make_uint2(w[0], w[1]);
+        codes_of(u, bu, w);
+        reinterpret_cast<uint2 *>(up_codes)[i] = make_uint2(w[0], w[1]);
+        if (!(i & 7)) {
+            gate_scales[i >> 3] = (uint8_t)bg;
+            up_scales[i >> 3] = (uint8_t)bu;
+        }
+    }
+}
+
+template <class T>
+__global__ __launch_bounds__(kBlock) void gated_backward_kernel(
+    const typename T::raw *dout, uint64_t dout_pitch, uint32_t total, Div per_row, uint32_t width,
+    const int8_t *gate_codes, const uint8_t *gate_scales, const int8_t *up_codes, const uint8_t *up_scales,
+    typename T::raw *dgate, uint64_t dgate_pitch, typename T::raw *dup, uint64_t dup_pitch) {
+    const uint32_t i = blockIdx.x * kBlock + threadIdx.x;
+    if (i >= total) return;
+    const uint32_t row = quotient(i, per_row), s = i - row * per_row.d;
+    uint32_t wg[2], wu[2];
+    load_codes(gate_codes, i, wg);
+    load_codes(up_codes, i, wu);
+    const float sg = scale_of(gate_scales[i >> 3]), su = scale_of(up_scales[i >> 3]);
+    float d[8], g[8], u[8];
+    load_slice<T>(dout + (uint64_t)row * dout_pitch, s * kSlice, width, d);
+    values_of(wg, sg, g);
+    values_of(wu, su, u);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float sig = sigmoid<T>(g[j]), ds = d[j] * sig, slope = 1.0f + g[j] * (1.0f - sig);
+        const float for_up = ds * g[j];
+        g[j] = ds * u[j] * slope;
+        u[j] = for_up;
+    }
+    store_slice<T>(dgate + (uint64_t)row * dgate_pitch, s * kSlice, width, g);
+    store_slice<T>(dup + (uint64_t)row * dup_pitch, s * kSlice, width, u);
+}
+
+// ---- experts ----
+
+// Rows [*n_kept, rows) of `out` (and their 8-bit form) become zeros: a wave a row.
+template <class T, bool WRITE, bool KEEP>
+__device__ __forceinline__ void clear_rows(uint32_t wave, uint32_t waves, const int32_t *n_kept, uint64_t rows,
+                                           uint32_t width, uint32_t groups, typename T::raw *out, int8_t *codes,
+                                           uint8_t *scales) {
+    const float zero[8] = {};
+    const uint32_t lane = threadIdx.x & 63;
+    for (uint64_t r = (uint64_t)max(*n_kept, 0) + wave; r < rows; r += waves)
+        for (uint32_t s = lane; s < groups * 8; s += 64) {
+            if constexpr (WRITE) store_slice<T>(out + r * width, s * kSlice, width, zero);
+            if constexpr (KEEP) {
+                reinterpret_cast<uint2 *>(codes)[r * (groups * 8) + s] = make_uint2(0, 0);
+                if (!(s & 7)) scales[r * groups + (s >> 3)] = (uint8_t)T::kLow;
+            }
+        }
+}
+
+// A lane reads its slice of a token once and writes it to each of the token's
+// places; the rounding to 8 bits is done once too.  Blocks from `main` on clear the places past the last choice.
+template <class T, bool WRITE, bool KEEP>
+__global__ __launch_bounds__(kBlock) void gather_kernel(const typename T::raw *x, uint64_t pitch, uint32_t total,
+                                                        Div per_row, uint32_t width, const int32_t *position,
+                                                        uint32_t k, uint32_t main, const int32_t *n_kept,
+                                                        uint32_t places, typename T::raw *xs, int8_t *codes,
+                                                        uint8_t *scales) {
+    if (blockIdx.x >= main) {
+        const uint32_t waves = kBlock / 64;
+        clear_rows<T, WRITE, KEEP>((blockIdx.x - main) * waves + threadIdx.x / 64, (gridDim.x - main) * waves, n_kept,
+                                   places, width, per_row.d / 8, xs, codes, scales);
+        return;
+    }
+    const uint32_t i = blockIdx.x * kBlock + threadIdx.x;
+    if (i >= total) return;
+    const uint32_t row = quotient(i, per_row), s = i - row * per_row.d;
+    float v[8];
+    load_slice<T>(x + (uint64_t)row * pitch, s * kSlice, width, v);
+    uint32_t w[2] = {0, 0}, byte = 0;
+    if constexpr (KEEP) {
+        byte = scale_byte<T>(v);
+        codes_of(v, byte, w);
+    }
+    const int32_t *at = position + (uint64_t)row * k;
+    for (uint32_t j = 0; j < k; ++j) {
+        const uint32_t p = (uint32_t)at[j];
+        if (p >= places) continue;
+        if constexpr (WRITE) store_slice<T>(xs + (uint64_t)p * width, s * kSlice, width, v);
+        if constexpr (KEEP) {
+            reinterpret_cast<uint2 *>(codes)[(uint64_t)p * per_row.d + s] = make_uint2(w[0], w[1]);
+            if (!(s & 7)) scales[((uint64_t)p * per_row.d + s) >> 3] = (uint8_t)byte;
+        }
+    }
+}
+
+// A lane sums its slice over the token's places, in the order of the choices.
+template <class T>
+__global__ __launch_bounds__(kBlock) void combine_kernel(const typename T::raw *ys, uint32_t total, Div per_row,
+                                                         uint32_t width, const int32_t *position, uint32_t k,
+                                                         uint32_t places, const float *weights, typename T::raw *out,
+                                                         uint64_t pitch) {
+    const uint32_t i = blockIdx.x * kBlock + threadIdx.x;
+    if (i >= total) return;
+    const uint32_t row = quotient(i, per_row), s = i - row * per_row.d;
+    const int32_t *at = position + (uint64_t)row * k;
+    float sum[8] = {};
+    for (uint32_t j = 0; j < k; ++j) {
+        const uint32_t p = (uint32_t)at[j];
+        if (p >= places) continue;
+        const float w = weights ? weights[(uint64_t)row * k + j] : 1.0f;
+        float v[8];
+        load_slice<T>(ys + (uint64_t)p * width, s * kSlice, width, v);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) sum[c] = fmaf(w, v[c], sum[c]);
+    }
+    store_slice<T>(out + (uint64_t)row * pitch, s * kSlice, width, sum);
+}
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d, 64);
+    return v;
+}
+
+// A wave per token: dout's slices are read once for eight choices at a time, each
+// ys row is read once for its product with dout, and dys written beside it.
+template <class T>
+__global__ __launch_bounds__(kBlock) void combine_backward_kernel(const typename T::raw *dout, uint64_t pitch,
+                                                                  const typename T::raw *ys, uint32_t tokens,
+                                                                  uint32_t width, const int32_t *position, uint32_t k,
+                                                                  uint32_t main, const int32_t *n_kept,
+                                                                  uint32_t places, const float *weights,
+                                                                  typename T::raw *dys, float *dweights) {
+    const uint32_t waves = kBlock / 64;
+    if (blockIdx.x >= main) {
+        clear_rows<T, true, false>((blockIdx.x - main) * waves + threadIdx.x / 64, (gridDim.x - main) * waves, n_kept,
+                                   places, width, (width + kGroup - 1) / kGroup, dys, nullptr, nullptr);
+        return;
+    }
+    const uint32_t t = blockIdx.x * waves + threadIdx.x / 64, lane = threadIdx.x & 63;
+    if (t >= tokens) return;
+    const typename T::raw *d = dout + (uint64_t)t * pitch;
+    for (uint32_t j = 0; j < k; ++j) {
+        const uint32_t p = __builtin_amdgcn_readfirstlane(position[(uint64_t)t * k + j]);
+        const float w = weights[(uint64_t)t * k + j];
+        float dot = 0.0f;
+        if (p < places)
+            for (uint32_t c = lane * kSlice; c < width; c += 64 * kSlice) {
+                float v[8], y[8];
+                load_slice<T>(d, c, width, v);
+                load_slice<T>(ys + (uint64_t)p * width, c, width, y);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    dot = fmaf(v[e], y[e], dot);
+                    y[e] = w * v[e];
+                }
+                store_slice<T>(dys + (uint64_t)p * width, c, width, y);
+            }
+        dot = wave_sum(dot);
+        if (lane == 0) dweights[(uint64_t)t * k + j] = dot;
+    }
+}
+
+// ---- embedding ----
+
+template <class T>
+__global__ __launch_bounds__(kBlock) void embed_kernel(const int32_t *ids, uint32_t total, Div per_row, uint32_t width,
+                                                       const typename T::raw *table, uint64_t table_pitch,
+                                                       uint32_t vocab, float scale, typename T::raw *out,
+                                                       uint64_t pitch) {
+    const uint32_t i = blockIdx.x * kBlock + threadIdx.x;
+    if (i >= total) return;
+    const uint32_t row = quotient(i, per_row), s = i - row * per_row.d;
+    const uint32_t id = (uint32_t)ids[row];
+    float v[8] = {};
+    if (id < vocab) {
+        load_slice<T>(table + (uint64_t)id * table_pitch, s * kSlice, width, v);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) v[c] *= scale;
+    }
+    store_slice<T>(out + (uint64_t)row * pitch, s * kSlice, width, v);
+}
+
+inline uint32_t slices_of(uint64_t width) { return (uint32_t)((width + kSlice - 1) / kSlice); }
+inline uint32_t padded_slices_of(uint64_t width) { return groups_of(width) * (kGroup / kSlice); }
+
+constexpr uint32_t kClearBlocks = 256;    // blocks that look for places past the last choice
+
+}  // namespace pl
+
+using namespace pl;
+
+extern "C" {
+
+int poseidon_stash(const void *x, uint64_t pitch, uint32_t type, uint64_t rows, uint64_t width, int8_t *codes,
+                   uint8_t *scales, void *hip_stream) {
+    PL_TRY(check_sizes(rows, width));
+    PL_TRY(check_matrix(x, pitch, type, rows, width));
+    PL_TRY(check_stash(codes, scales, rows));
+    if (!rows) return POSEIDON_OK;
+    const uint32_t per_row = padded_slices_of(width);
+    PL_TYPE(type, over_rows(rows, per_row, [&](uint64_t r, uint64_t, uint32_t n) {
+        stash_kernel<T><<<blocks_for(n), kBlock, 0, (hipStream_t)hip_stream>>>(
+            (const T::raw *)x + r * pitch, pitch, n, make_div(per_row), (uint32_t)width, codes + r * per_row * kSlice,
+            scales + r * (per_row / 8));
+    }));
+    return launched();
+}
+
+int poseidon_restore(const int8_t *codes, const uint8_t *scales, uint64_t rows, uint64_t width, void *out,
+                     uint64_t out_pitch, uint32_t type, void *hip_stream) {
+    PL_TRY(check_sizes(rows, width));
+    PL_TRY(check_matrix(out, out_pitch, type, rows, width));
+    PL_TRY(check_stash(codes, scales, rows));
+    if (!rows) return POSEIDON_OK;
+    const uint32_t per_row = padded_slices_of(width);
+    PL_TYPE(type, over_rows(rows, per_row, [&](uint64_t r, uint64_t, uint32_t n) {
+        restore_kernel<T><<<blocks_for(n), kBlock, 0, (hipStream_t)hip_stream>>>(
+            codes + r * per_row * kSlice, scales + r * (per_row / 8), n, make_div(per_row), (uint32_t)width,
+            (T::raw *)out + r * out_pitch, out_pitch);
+    }));
+    return launched();
+}
+
+int poseidon_gated_forward(const void *gate, uint64_t gate_pitch, const void *up, uint64_t up_pitch, uint32_t type,
+                           uint64_t rows, uint64_t width, void *out, uint64_t out_pitch, int8_t *gate_codes,
+                           uint8_t *gate_scales, int8_t *up_codes, uint8_t *up_scales, void *hip_stream) {
+    PL_TRY(check_sizes(rows, width));
+    PL_TRY(check_matrix(gate, gate_pitch, type, rows, width));
+    PL_TRY(check_matrix(up, up_pitch, type, rows, width));
+    PL_TRY(check_matrix(out, out_pitch, type, rows, width));
+    const bool keep = gate_codes || gate_scales || up_codes || up_scales;
+    if (keep) {
+        PL_TRY(check_stash(gate_codes, gate_scales, rows));
+        PL_TRY(check_stash(up_codes, up_scales, rows));
+    }
+    if (!rows) return POSEIDON_OK;
+    const uint32_t per_row = padded_slices_of(width);
+    const auto run = [&](auto kernel, auto t) {
+        using T = decltype(t);
+        over_rows(rows, per_row, [&](uint64_t r, uint64_t, uint32_t n) {
+            const uint64_t c = r * per_row * kSlice, b = r * (per_row / 8);
+            kernel<<<blocks_for(n), kBlock, 0, (hipStream_t)hip_stream>>>(
+                (const typename T::raw *)gate + r * gate_pitch, gate_pitch, (const typename T::raw *)up + r * up_pitch,
+                up_pitch, n, make_div(per_row), (uint32_t)width, (typename T::raw *)out + r * out_pitch, out_pitch,
+                keep ? gate_codes + c : nullptr, keep ? gate_scales + b : nullptr, keep ? up_codes + c : nullptr,
+                keep ? up_scales + b : nullptr);
+        });
+    };
+    PL_TYPE(type, keep ? run(gated_forward_kernel<T, true>, T{}) : run(gated_forward_kernel<T, false>, T{}));
+    return launched();
+}
+
+int poseidon_gated_backward(const void *dout, uint64_t dout_pitch, uint32_t type, uint64_t rows, uint64_t width,
+                            const int8_t *gate_codes, const uint8_t *gate_scales, const int8_t *up_codes,
+                            const uint8_t *up_scales, void *dgate, uint64_t dgate_pitch, void *dup, uint64_t dup_pitch,
+                            void *hip_stream) {
+    PL_TRY(check_sizes(rows, width));
+    PL_TRY(check_matrix(dout, dout_pitch, type, rows, width));
+    PL_TRY(check_matrix(dgate, dgate_pitch, type, rows, width));
+    PL_TRY(check_matrix(dup, dup_pitch, type, rows, width));
+    PL_TRY(check_stash(gate_codes, gate_scales, rows));
+    PL_TRY(check_stash(up_codes, up_scales, rows));
+    if (!rows) return POSEIDON_OK;
+    const uint32_t per_row = padded_slices_of(width);
+    PL_TYPE(type, over_rows(rows, per_row, [&](uint64_t r, uint64_t, uint32_t n) {
+        const uint64_t c = r * per_row * kSlice, b = r * (per_row / 8);
+        gated_backward_kernel<T><<<blocks_for(n), kBlock, 0, (hipStream_t)hip_stream>>>(
+            (const T::raw *)dout + r * dout_pitch, dout_pitch, n, make_div(per_row), (uint32_t)width, gate_codes + c,
+            gate_scales + b, up_codes + c, up_scales + b, (T::raw *)dgate + r * dgate_pitch, dgate_pitch,
+            (T::raw *)dup + r * dup_pitch, dup_pitch);
+    }));
+    return launched();
+}
+
+int poseidon_expert_gather(const void *x, uint64_t pitch, uint32_t type, uint64_t tokens, uint64_t width,
+                           const int32_t *position, uint32_t k, const int32_t *n_kept, void *xs, int8_t *codes,
+                           uint8_t *scales, void *hip_stream) {
+    if (!k) return POSEIDON_E_INVAL;
+    if (tokens > POSEIDON_ROWS_MAX / k) return POSEIDON_E_RANGE;
+    const uint64_t places = tokens * k;
+    PL_TRY(check_sizes(places, width));
+    PL_TRY(check_matrix(x, pitch, type, tokens, width));
+    const bool keep = codes || scales;
+    if (tokens && (!position || !n_kept || (!xs && !keep))) return POSEIDON_E_INVAL;
+    if (xs) PL_TRY(check_matrix(xs, width, type, places, width));
+    if (keep) PL_TRY(check_stash(codes, scales, places));
+    if (!tokens) return POSEIDON_OK;
+    const uint32_t per_row = padded_slices_of(width);
+    const auto run = [&](auto kernel, auto t) {
+        using T = decltype(t);
+        over_rows(tokens, per_row, [&](uint64_t r, uint64_t n_rows, uint32_t n) {
+            const bool last = r + n_rows == tokens;
+            kernel<<<blocks_for(n) + (last ? kClearBlocks : 0), kBlock, 0, (hipStream_t)hip_stream>>>(
+                (const typename T::raw *)x + r * pitch, pitch, n, make_div(per_row), (uint32_t)width,
+                position + r * k, k, blocks_for(n), n_kept, (uint32_t)places, (typename T::raw *)xs, codes, scales);
+        });
+    };
+    PL_TYPE(type, !keep ? run(gather_kernel<T, true, false>, T{})
+                  : xs  ? run(gather_kernel<T, true, true>, T{})
+                        : run(gather_kernel<T, false, true>, T{}));
+    return launched();
+}
+
+int poseidon_expert_combine(const void *ys, uint32_t type, uint64_t tokens, uint64_t width, const int32_t *position,
+                            uint32_t k, const float *weights, void *out, uint64_t out_pitch, void *hip_stream) {
+    if (!k) return POSEIDON_E_INVAL;
+    if (tokens > POSEIDON_ROWS_MAX / k) return POSEIDON_E_RANGE;
+    PL_TRY(check_sizes(tokens * k, width));
+    PL_TRY(check_matrix(ys, width, type, tokens, width));
+    PL_TRY(check_matrix(out, out_pitch, type, tokens, width));
+    if (tokens && !position) return POSEIDON_E_INVAL;
+    if (!tokens) return POSEIDON_OK;
+    const uint32_t per_row = slices_of(width);
+    PL_TYPE(type, over_rows(tokens, per_row, [&](uint64_t r, uint64_t, uint32_t n) {
+        combine_kernel<T><<<blocks_for(n), kBlock, 0, (hipStream_t)hip_stream>>>(
+            (const T::raw *)ys, n, make_div(per_row), (uint32_t)width, position + r * k, k,
+            (uint32_t)(tokens * k), weights ? weights + r * k : nullptr, (T::raw *)out + r * out_pitch, out_pitch);
+    }));
+    return launched();
+}
+
+int poseidon_expert_combine_backward(const void *dout, uint64_t dout_pitch, const void *ys, uint32_t type,
+                                     uint64_t tokens, uint64_t width, const int32_t *position, uint32_t k,
+                                     const int32_t *n_kept, const float *weights, void *dys, float *dweights,
+                                     void *hip_stream) {
+    if (!k) return POSEIDON_E_INVAL;
+    if (tokens > POSEIDON_ROWS_MAX / k) return POSEIDON_E_RANGE;
+    const uint64_t places = tokens * k;
+    PL_TRY(check_sizes(places, width));
+    PL_TRY(check_matrix(dout, dout_pitch, type, tokens, width));
+    PL_TRY(check_matrix(ys, width, type, places, width));
+    PL_TRY(check_matrix(dys, width, type, places, width));
+    if (tokens && (!position || !n_kept || !weights || !dweights)) return POSEIDON_E_INVAL;
+    if (!tokens) return POSEIDON_OK;
+    const uint64_t step = 1ull << 24;    // tokens of a launch
+    PL_TYPE(type, for (uint64_t t = 0; t < tokens; t += step) {
+        const uint64_t n = tokens - t < step ? tokens - t : step;
+        const uint32_t main = (uint32_t)((n + kBlock / 64 - 1) / (kBlock / 64));
+        combine_backward_kernel<T>
+            <<<main + (t + n == tokens ? kClearBlocks : 0), kBlock, 0, (hipStream_t)hip_stream>>>(
+                (const T::raw *)dout + t * dout_pitch, dout_pitch, (const T::raw *)ys, (uint32_t)n, (uint32_t)width,
+                position + t * k, k, main, n_kept, (uint32_t)places, weights + t * k, (T::raw *)dys, dweights + t * k);
+    });
+    return launched();
+}
+
+int poseidon_embed(const int32_t *ids, uint64_t tokens, const void *table, uint64_t table_pitch, uint32_t type,
+                   uint64_t vocab, uint64_t width, float scale, void *out, uint64_t out_pitch, void *hip_stream) {
+    PL_TRY(check_sizes(tokens, width));
+    if (vocab > POSEIDON_VOCAB_MAX) return POSEIDON_E_RANGE;
+    PL_TRY(check_matrix(table, table_pitch, type, vocab, width));
+    PL_TRY(check_matrix(out, out_pitch, type, tokens, width));
+    if (tokens && !ids) return POSEIDON_E_INVAL;
+    if (!tokens) return POSEIDON_OK;
+    const uint32_t per_row = slices_of(width);
+    PL_TYPE(type, over_rows(tokens, per_row, [&](uint64_t r, uint64_t, uint32_t n) {
+        embed_kernel<T><<<blocks_for(n), kBlock, 0, (hipStream_t)hip_stream>>>(
+            ids + r, n, make_div(per_row), (uint32_t)width, (const T::raw *)table, table_pitch, (uint32_t)vocab, scale,
+            (T::raw *)out + r * out_pitch, out_pitch);
+    }));
+    return launched();
+}
+
+}  // extern "C"

@@ -1,0 +1,444 @@
+// Sort of tokens by expert, and the gradient of an embedding summed by token.
+//
+// Both sort whole keys stably with a counting sort of up to 9 bits a pass, the
+// low bits first.  A block takes 4096 neighbouring elements, a wave 512 of them,
+// 64 at a time in order; lanes with the same digit find each other with one
+// ballot a bit, so an element's rank among the equal ones before it needs no
+// atomics and the order is the same on every call.
+#include "layers_device.h"
+
+namespace pl {
+
+constexpr uint32_t kSortThreads = 512, kSortRounds = 8, kSortTile = kSortThreads * kSortRounds;
+constexpr uint32_t kSortWaves = kSortThreads / 64, kMaxBits = 9, kMaxBins = 1u << kMaxBits;
+// Up to this many blocks each block adds up the counts of the blocks before it by
+// itself (a bin a thread); above it a kernel of its own turns them into sums once.
+constexpr uint32_t kSelfScan = 128;
+
+struct SortPass {
+    const int32_t *keys;
+    const int32_t *from;       // the elements' indexes, null: 0, 1, 2, ...
+    uint32_t m, n_keys;        // elements; keys outside [0, n_keys) count as n_keys
+    uint32_t shift, bins, bits;
+    uint32_t blocks;
+    uint32_t *counts;          // [blocks][bins]
+    uint32_t *totals;          // [bins], only where a kernel of its own scans
+    int32_t *keys_out;         // null: not needed
+    int32_t *order;            // the elements' indexes in their new order
+    int32_t *position;         // null, or the new place of each element, -1 for key n_keys (single-pass sorts)
+    int32_t *offsets;          // null, or the first place of each digit up to n_keys (single-pass sorts)
+};
+
+__device__ __forceinline__ uint32_t key_at(const SortPass &p, uint32_t i) {
+    const uint32_t k = (uint32_t)p.keys[i];
+    return min(k, p.n_keys);
+}
+
+__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortPass p) {
+    __shared__ uint32_t count[kMaxBins];
+    for (uint32_t b = threadIdx.x; b < p.bins; b += kSortThreads) count[b] = 0;
+    __syncthreads();
+    const uint32_t first = blockIdx.x * kSortTile;
+    for (uint32_t r = 0; r < kSortRounds; ++r) {
+        const uint32_t i = first + r * kSortThreads + threadIdx.x;
+        if (i < p.m) atomicAdd(&count[(key_at(p, i) >> p.shift) & (p.bins - 1)], 1u);
+    }
+    __syncthreads();
+    for (uint32_t b = threadIdx.x; b < p.bins; b += kSortThreads) p.counts[blockIdx.x * p.bins + b] = count[b];
+}
+
+// Exclusive sums over the blocks, a block of threads per bin.
+__global__ __launch_bounds__(256) void sort_scan_kernel(SortPass p) {
+    __shared__ uint32_t part[256];
+    const uint32_t bin = blockIdx.x, tid = threadIdx.x;
+    uint32_t carry = 0;
+    for (uint32_t b0 = 0; b0 < p.blocks; b0 += 256) {
+        const uint32_t b = b0 + tid;
+        const uint32_t v = b < p.blocks ? p.counts[b * p.bins + bin] : 0u;
+        part[tid] = v;
+        __syncthreads();
+        for (uint32_t d = 1; d < 256; d <<= 1) {
+            const uint32_t add = tid >= d ? part[tid - d] : 0u;
+            __syncthreads();
+            part[tid] += add;
+            __syncthreads();
+        }
+        if (b < p.blocks) p.counts[b * p.bins + bin] = carry + part[tid] - v;
+        carry += part[255];
+        __syncthreads();
+    }
+    if (tid == 0) p.totals[bin] = carry;
+}
+
+// Exclusive prefix over the 512 threads' values.
+__device__ __forceinline__ uint32_t block_prefix(uint32_t v, uint32_t *wave_sums) {
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+    uint32_t s = v;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t up = __shfl_up(s, d, 64);
+        if ((int)lane >= d) s += up;
+    }
+    if (lane == 63) wave_sums[wave] = s;
+    __syncthreads();
+    uint32_t before = 0;
+    for (uint32_t w = 0; w < wave; ++w) before += wave_sums[w];
+    __syncthreads();
+    return before + s - v;
+}
+
+__global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortPass p) {
+    __shared__ uint32_t count[kSortWaves][kMaxBins];
+    __shared__ uint32_t wave_sums[kSortWaves];
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
+    for (uint32_t b = tid; b < kSortWaves * kMaxBins; b += kSortThreads) (&count[0][0])[b] = 0;
+    __syncthreads();
+
+    // ranks within the wave's 512 elements
+    const uint32_t first = blockIdx.x * kSortTile + wave * (64 * kSortRounds);
+    uint32_t key[kSortRounds], rank[kSortRounds];
+    const uint64_t below = (1ull << lane) - 1;
+#pragma unroll
+    for (uint32_t r = 0; r < kSortRounds; ++r) {
+        const uint32_t i = first + r * 64 + lane;
+        key[r] = i < p.m ? key_at(p, i) : 0xffffffffu;
+    }
+    volatile uint32_t *mine = count[wave];
+#pragma unroll
+    for (uint32_t r = 0; r < kSortRounds; ++r) {
+        const bool on = first + r * 64 + lane < p.m;
+        const uint32_t digit = (key[r] >> p.shift) & (p.bins - 1);
+        uint64_t same = __ballot(on);
+        for (uint32_t b = 0; b < p.bits; ++b) {
+            const uint64_t set = __ballot((digit >> b) & 1);
+            same &= (digit >> b) & 1 ? set : ~set;
+        }
+        const uint32_t old = mine[digit];
+        const uint32_t before = (uint32_t)__popcll(same & below);
+        rank[r] = old + before;
+        __builtin_amdgcn_wave_barrier();
+        if (on && before == 0) mine[digit] = old + (uint32_t)__popcll(same);
+        __builtin_amdgcn_wave_barrier();
+    }
+    __syncthreads();
+
+    // a bin a thread: where the block's elements of this digit begin
+    uint32_t before = 0, total = 0;
+    if (tid < p.bins) {
+        if (p.blocks == 1) {
+            for (uint32_t w = 0; w < kSortWaves; ++w) total += count[w][tid];
+        } else if (p.totals) {
+            before = p.counts[blockIdx.x * p.bins + tid];
+            total = p.totals[tid];
+        } else {
+            for (uint32_t b = 0; b < p.blocks; ++b) {
+                const uint32_t c = p.counts[b * p.bins + tid];
+                before += b < blockIdx.x ? c : 0u;
+                total += c;
+            }
+        }
+    }
+    const uint32_t start = block_prefix(total, wave_sums);
+    if (tid < p.bins) {
+        if (p.offsets && blockIdx.x == 0 && tid <= p.n_keys) p.offsets[tid] = (int32_t)start;
+        uint32_t at = start + before;
+        for (uint32_t w = 0; w < kSortWaves; ++w) {
+            const uint32_t c = count[w][tid];
+            count[w][tid] = at;
+            at += c;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (uint32_t r = 0; r < kSortRounds; ++r) {
+        const uint32_t i = first + r * 64 + lane;
+        if (i >= p.m) continue;
+        const uint32_t to = count[wave][(key[r] >> p.shift) & (p.bins - 1)] + rank[r];
+        const int32_t index = p.from ? p.from[i] : (int32_t)i;
+        p.order[to] = index;
+        if (p.keys_out) p.keys_out[to] = (int32_t)key[r];
+        if (p.position) p.position[i] = key[r] < p.n_keys ? (int32_t)to : -1;
+    }
+}
+
+inline uint32_t sort_blocks(uint64_t m) { return (uint32_t)((m + kSortTile - 1) / kSortTile); }
+inline uint64_t round_up(uint64_t v, uint64_t to) { return (v + to - 1) / to * to; }
+// counts, then totals
+inline uint64_t sort_counts_bytes(uint64_t m) { return round_up(((uint64_t)sort_blocks(m) + 1) * kMaxBins * 4, 256); }
+
+inline void run_pass(SortPass p, hipStream_t stream) {
+    const bool scan = p.blocks > kSelfScan;
+    if (!scan) p.totals = nullptr;
+    if (p.blocks > 1) sort_count_kernel<<<p.blocks, kSortThreads, 0, stream>>>(p);
+    if (scan) sort_scan_kernel<<<p.bins, 256, 0, stream>>>(p);
+    sort_place_kernel<<<p.blocks, kSortThreads, 0, stream>>>(p);
+}
+
+// ---- gradient of an embedding ----
+
+// Sorted places in chunks of `chunk`; a block takes one chunk and 512 columns
+// (64 lanes of 8).  It adds the rows of dout in sorted order and writes the sum
+// of every token whose places all lie in the chunk.  A token that comes from the chunk
+// before leaves its part in slot 0 of the chunk, one that only goes on into the
+// next chunk in slot 1; embed_join_kernel adds those up in order.
+struct EmbedGrad {
+    const int32_t *keys, *order;
+    uint32_t m, vocab, width, chunk, chunks, accumulate;
+    float scale;
+    const void *dout;
+    uint64_t dout_pitch;
+    void *dtable;
+    uint64_t dtable_pitch;
+    float *parts;              // [chunks][2][padded], padded = width in whole slices
+    uint32_t padded;
+};
+
+template <class G>
+__device__ __forceinline__ void write_sum(const EmbedGrad &e, uint32_t key, uint32_t col, const float (&sum)[8]) {
+    typename G::raw *row = (typename G::raw *)e.dtable + (uint64_t)key * e.dtable_pitch;
+    float v[8] = {};
+    if (e.accumulate) load_slice<G>(row, col, e.width, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = e.accumulate ? fmaf(e.scale, sum[i], v[i]) : e.scale * sum[i];
+    store_slice<G>(row, col, e.width, v);
+}
+
+template <class T, class G>
+__global__ __launch_bounds__(64) void embed_sum_kernel(EmbedGrad e) {
+    const uint32_t chunk = blockIdx.x, col = (blockIdx.y * 64 + threadIdx.x) * kSlice;
+    const uint32_t lo = chunk * e.chunk, hi = min(lo + e.chunk, e.m);
+    if (col >= e.width) return;
+    const typename T::raw *dout = (const typename T::raw *)e.dout;
+    float sum[8] = {};
+    uint32_t begin = lo, key = (uint32_t)e.keys[lo];
+    for (uint32_t a = lo; a < hi; a += 8) {
+        float v[8][8];
+        uint32_t keys[8];
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j) {
+            const uint32_t at = min(a + j, hi - 1);
+            keys[j] = (uint32_t)e.keys[at];
+            load_slice<T>(dout + (uint64_t)(uint32_t)e.order[at] * e.dout_pitch, col, e.width, v[j]);
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j) {
+            const uint32_t at = a + j;
+            if (at >= hi) break;
+            if (keys[j] != key) {          // the token before ends here, within the chunk
+                if (key < e.vocab) {
+                    if (begin == lo && lo > 0 && (uint32_t)e.keys[lo - 1] == key) {
+                        float *part = e.parts + (uint64_t)chunk * 2 * e.padded + col;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) part[i] = sum[i];
+                    } else {
+                        write_sum<G>(e, key, col, sum);
+                    }
+                }
+                begin = at;
+                key = keys[j];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += v[j][i];
+        }
+    }
+    if (key >= e.vocab) return;
+    const bool from = begin == lo && lo > 0 && (uint32_t)e.keys[lo - 1] == key;
+    const bool on = hi < e.m && (uint32_t)e.keys[hi] == key;
+    if (from || on) {
+        float *part = e.parts + ((uint64_t)chunk * 2 + (from ? 0 : 1)) * e.padded + col;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) part[i] = sum[i];
+    } else {
+        write_sum<G>(e, key, col, sum);
+    }
+}
+
+// A block of four waves per chunk and 512 columns; it has work where a token
+// begins in the chunk and goes on past it.  The waves take every fourth of the
+// chunks that follow, and the first adds the four sums.
+template <class G>
+__global__ __launch_bounds__(256) void embed_join_kernel(EmbedGrad e) {
+    __shared__ float share[3][64][kSlice + 1];
+    const uint32_t chunk = blockIdx.x, lo = chunk * e.chunk, hi = min(lo + e.chunk, e.m);
+    if (hi >= e.m) return;
+    const uint32_t key = (uint32_t)e.keys[hi - 1];
+    if (key >= e.vocab || (uint32_t)e.keys[hi] != key) return;
+    if ((uint32_t)e.keys[lo] == key && lo > 0 && (uint32_t)e.keys[lo - 1] == key) return;
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+    uint32_t last = chunk + 1;    // one past the last chunk that begins with the token
+    for (;;) {
+        const uint32_t c = last + lane;
+        const uint64_t same = __ballot(c < e.chunks && (uint32_t)e.keys[min(c, e.chunks - 1) * e.chunk] == key);
+        last += same == ~0ull ? 64u : (uint32_t)__ffsll((unsigned long long)~same) - 1u;
+        if (same != ~0ull) break;
+    }
+    const uint32_t col = (blockIdx.y * 64 + lane) * kSlice;
+    const bool inside = col < e.width;
+    float sum[8] = {};
+    if (inside)
+        for (uint32_t c = chunk + wave; c < last; c += 4) {
+            const float *part = e.parts + ((uint64_t)c * 2 + (c == chunk)) * e.padded + col;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += part[i];
+        }
+    if (wave) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) share[wave - 1][lane][i] = sum[i];
+    }
+    __syncthreads();
+    if (wave || !inside) return;
+#pragma unroll
+    for (int w = 0; w < 3; ++w) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += share[w][lane][i];
+    }
+    write_sum<G>(e, key, col, sum);
+}
+
+template <class G>
+__global__ __launch_bounds__(kBlock) void clear_kernel(typename G::raw *out, uint64_t pitch, uint32_t total,
+                                                       Div per_row, uint32_t width) {
+    const uint32_t i = blockIdx.x * kBlock + threadIdx.x;
+    if (i >= total) return;
+    const uint32_t row = quotient(i, per_row), s = i - row * per_row.d;
+    const float zero[8] = {};
+    store_slice<G>(out + (uint64_t)row * pitch, s * kSlice, width, zero);
+}
+
+// Places a block adds up: few tokens are spread over more blocks.
+// Past 2^25 of them the chunks grow, so that there are at most 2^20.
+inline uint32_t chunk_of(uint64_t tokens) {
+    if (tokens <= 4096) return 8;
+    return tokens <= 1ull << 25 ? 32u : (uint32_t)round_up((tokens + (1u << 20) - 1) >> 20, 8);
+}
+
+struct EmbedWorkspace {
+    uint64_t counts, keys[2], order[2], parts, bytes;    // offsets and size
+};
+
+inline EmbedWorkspace embed_workspace(uint64_t m, uint64_t width) {
+    EmbedWorkspace w;
+    const uint64_t list = round_up(m * 4, 256), padded = (width + kSlice - 1) / kSlice * kSlice;
+    const uint64_t chunks = (m + chunk_of(m) - 1) / chunk_of(m);
+    w.counts = 0;
+    w.keys[0] = sort_counts_bytes(m);
+    w.keys[1] = w.keys[0] + list;
+    w.order[0] = w.keys[1] + list;
+    w.order[1] = w.order[0] + list;
+    w.parts = w.order[1] + list;
+    w.bytes = w.parts + round_up(chunks * 2 * padded * 4, 256);
+    return w;
+}
+
+}  // namespace pl
+
+using namespace pl;
+
+extern "C" {
+
+uint64_t poseidon_expert_sort_workspace(uint64_t tokens, uint32_t k, uint32_t n_experts) {
+    if (!k || !n_experts || n_experts > POSEIDON_EXPERTS_MAX || tokens > POSEIDON_ROWS_MAX / k) return UINT64_MAX;
+    return sort_blocks(tokens * k) > 1 ? sort_counts_bytes(tokens * k) : 0;
+}
+
+int poseidon_expert_sort(const int32_t *choice, uint64_t tokens, uint32_t k, uint32_t n_experts, int32_t *order,
+                         int32_t *position, int32_t *offsets, void *workspace, uint64_t workspace_bytes,
+                         void *hip_stream) {
+    if (!k || !n_experts) return POSEIDON_E_INVAL;
+    if (n_experts > POSEIDON_EXPERTS_MAX || tokens > POSEIDON_ROWS_MAX / k) return POSEIDON_E_RANGE;
+    if (!offsets || (tokens && (!choice || !order || !position))) return POSEIDON_E_INVAL;
+    PL_TRY(check_workspace(workspace, workspace_bytes, poseidon_expert_sort_workspace(tokens, k, n_experts)));
+    const uint32_t m = (uint32_t)(tokens * k);
+    SortPass p = {};
+    p.keys = choice;
+    p.m = m;
+    p.n_keys = n_experts;
+    while ((1u << p.bits) < n_experts + 1) ++p.bits;
+    p.bins = 1u << p.bits;
+    p.blocks = m ? sort_blocks(m) : 1;    // no choices: one block writes the offsets
+    p.counts = (uint32_t *)workspace;
+    p.totals = p.counts + (uint64_t)p.blocks * p.bins;
+    p.order = order;
+    p.position = position;
+    p.offsets = offsets;
+    run_pass(p, (hipStream_t)hip_stream);
+    return launched();
+}
+
+uint64_t poseidon_embed_backward_workspace(uint64_t tokens, uint64_t vocab, uint64_t width) {
+    if (check_sizes(tokens, width) != POSEIDON_OK || vocab > POSEIDON_VOCAB_MAX) return UINT64_MAX;
+    return tokens ? embed_workspace(tokens, width).bytes : 0;
+}
+
+int poseidon_embed_backward(const int32_t *ids, uint64_t tokens, const void *dout, uint64_t dout_pitch, uint32_t type,
+                            uint64_t vocab, uint64_t width, float scale, void *dtable, uint64_t dtable_pitch,
+                            uint32_t dtable_type, uint32_t accumulate, void *workspace, uint64_t workspace_bytes,
+                            void *hip_stream) {
+    PL_TRY(check_sizes(tokens, width));
+    if (vocab > POSEIDON_VOCAB_MAX) return POSEIDON_E_RANGE;
+    PL_TRY(check_matrix(dout, dout_pitch, type, tokens, width));
+    PL_TRY(check_matrix(dtable, dtable_pitch, dtable_type, vocab, width));
+    if (accumulate > 1 || (tokens && !ids)) return POSEIDON_E_INVAL;
+    PL_TRY(check_workspace(workspace, workspace_bytes, poseidon_embed_backward_workspace(tokens, vocab, width)));
+    const hipStream_t stream = (hipStream_t)hip_stream;
+    const uint32_t slices = (uint32_t)((width + kSlice - 1) / kSlice);
+    if (!accumulate)
+        PL_TYPE(dtable_type, over_rows(vocab, slices, [&](uint64_t r, uint64_t, uint32_t n) {
+            clear_kernel<T><<<blocks_for(n), kBlock, 0, stream>>>((T::raw *)dtable + r * dtable_pitch, dtable_pitch, n,
+                                                                  make_div(slices), (uint32_t)width);
+        }));
+    if (!vocab) return POSEIDON_OK;
+    if (!tokens) return accumulate ? POSEIDON_OK : launched();
+
+    const uint32_t m = (uint32_t)tokens;
+    const EmbedWorkspace w = embed_workspace(tokens, width);
+    char *base = (char *)workspace;
+    uint32_t bits = 1;
+    while ((1u << bits) < vocab + 1) ++bits;
+    const uint32_t passes = (bits + kMaxBits - 1) / kMaxBits, each = (bits + passes - 1) / passes;
+    SortPass p = {};
+    p.m = m;
+    p.n_keys = (uint32_t)vocab;
+    p.bits = each;
+    p.bins = 1u << each;
+    p.blocks = sort_blocks(m);
+    p.counts = (uint32_t *)(base + w.counts);
+    for (uint32_t i = 0; i < passes; ++i) {
+        p.totals = p.counts + (uint64_t)p.blocks * p.bins;
+        p.keys = i ? (const int32_t *)(base + w.keys[(i - 1) & 1]) : ids;
+        p.from = i ? (const int32_t *)(base + w.order[(i - 1) & 1]) : nullptr;
+        p.keys_out = (int32_t *)(base + w.keys[i & 1]);
+        p.order = (int32_t *)(base + w.order[i & 1]);
+        p.shift = i * each;
+        run_pass(p, stream);
+    }
+
+    EmbedGrad e = {};
+    e.keys = p.keys_out;
+    e.order = p.order;
+    e.m = m;
+    e.vocab = (uint32_t)vocab;
+    e.width = (uint32_t)width;
+    e.chunk = chunk_of(tokens);
+    e.chunks = (m + e.chunk - 1) / e.chunk;
+    e.accumulate = accumulate;
+    e.scale = scale;
+    e.dout = dout;
+    e.dout_pitch = dout_pitch;
+    e.dtable = dtable;
+    e.dtable_pitch = dtable_pitch;
+    e.parts = (float *)(base + w.parts);
+    e.padded = slices * kSlice;
+    const dim3 grid(e.chunks, (slices + 63) / 64);
+    const auto run = [&](auto t) {
+        using D = decltype(t);
+        PL_TYPE(dtable_type, embed_sum_kernel<D, T><<<grid, 64, 0, stream>>>(e);
+                if (e.chunks > 1) embed_join_kernel<T><<<grid, 256, 0, stream>>>(e));
+    };
+    PL_TYPE(type, run(T{}));
+    return launched();
+}
+
+}  // extern "C"

@@ -1,0 +1,406 @@
+"""ctypes binding of ``include/poseidon_layers.h``: layer operators of a pipeline stage.
+
+Every operator runs in the HIP library ``libposeidon.so``; this module checks
+and marshals arguments and allocates outputs and workspaces with torch.  All
+tensors live on one GPU.  Matrices are 2-D with neighbouring values in a row;
+any row pitch is taken as it is, any other layout of an input is copied first.
+Work is enqueued on ``stream`` (a ``torch.cuda.Stream`` or a raw ``hipStream_t``
+integer; default: torch's current stream of the tensors' GPU), on which the
+outputs are allocated too.  Nothing synchronises.  What is refused raises
+``PoseidonError`` before anything is enqueued.
+"""
+from __future__ import annotations
+
+import ctypes as C
+import functools
+from dataclasses import dataclass
+from typing import Optional, Tuple
+
+import torch
+
+from . import poseidon as P
+from .poseidon import PoseidonError
+
+GROUP = 64
+WIDTH_MAX, ROWS_MAX = 1 << 20, 2 ** 31 - 1
+EXPERTS_MAX, RANGES_MAX, VOCAB_MAX, TILES_MAX = 511, 65535, 2 ** 26 - 1, 1 << 22
+TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+
+_p, _u64, _u32 = C.c_void_p, C.c_uint64, C.c_uint32
+_ARGS = {
+    "poseidon_stash": [_p, _u64, _u32, _u64, _u64, _p, _p, _p],
+    "poseidon_restore": [_p, _p, _u64, _u64, _p, _u64, _u32, _p],
+    "poseidon_gated_forward": [_p, _u64, _p, _u64, _u32, _u64, _u64, _p, _u64, _p, _p, _p, _p, _p],
+    "poseidon_gated_backward": [_p, _u64, _u32, _u64, _u64, _p, _p, _p, _p, _p, _u64, _p, _u64, _p],
+    "poseidon_weight_gradient": [_p, _u64, _u32, _u64, _u64, _p, _p, _u64, _p, _u32, _p, _u32, _u32, _p, _u64, _p],
+    "poseidon_weight_gradient_workspace": [_u64, _u64, _u64, _u32],
+    "poseidon_expert_sort": [_p, _u64, _u32, _u32, _p, _p, _p, _p, _u64, _p],
+    "poseidon_expert_sort_workspace": [_u64, _u32, _u32],
+    "poseidon_expert_gather": [_p, _u64, _u32, _u64, _u64, _p, _u32, _p, _p, _p, _p, _p],
+    "poseidon_expert_combine": [_p, _u32, _u64, _u64, _p, _u32, _p, _p, _u64, _p],
+    "poseidon_expert_combine_backward": [_p, _u64, _p, _u32, _u64, _u64, _p, _u32, _p, _p, _p, _p, _p],
+    "poseidon_embed": [_p, _u64, _p, _u64, _u32, _u64, _u64, C.c_float, _p, _u64, _p],
+    "poseidon_embed_backward": [_p, _u64, _p, _u64, _u32, _u64, _u64, C.c_float, _p, _u64, _u32, _u32, _p, _u64, _p],
+    "poseidon_embed_backward_workspace": [_u64, _u64, _u64],
+}
+EXPORTS = tuple(_ARGS)
+
+_lib = None
+
+
+def lib():
+    """The loaded HIP library, with the layer operators' signatures."""
+    global _lib
+    if _lib is None:
+        L = P.lib()
+        for name, args in _ARGS.items():
+            f = getattr(L, name)
+            f.argtypes = args
+            f.restype = _u64 if name.endswith("_workspace") else C.c_int
+        _lib = L
+    return _lib
+
+
+@dataclass
+class Stash:
+    """Rows kept in 8 bits: int8 codes [rows, groups * 64], uint8 scale bytes [rows, groups], the rows' width and the
+    type they came from."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    width: int
+    dtype: torch.dtype
+
+    @property
+    def rows(self) -> int:
+        return self.scales.shape[0]
+
+    @property
+    def nbytes(self) -> int:
+        return self.codes.numel() + self.scales.numel()
+
+
+@dataclass
+class ExpertPlan:
+    """Order of a batch's choices by expert: order [tokens * k], position [tokens, k] (-1: dropped), offsets
+    [experts + 1], all int32."""
+    order: torch.Tensor
+    position: torch.Tensor
+    offsets: torch.Tensor
+
+
+def _refuse(where: str):
+    raise PoseidonError(P.POSEIDON_E_INVAL, where)
+
+
+def _streamed(f):
+    """Runs f with torch's current stream set to `stream`, and keeps its inputs' memory until that stream is past."""
+
+    @functools.wraps(f)
+    def g(*args, stream=None, **kw):
+        if stream is None:
+            return f(*args, **kw)
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+        with torch.cuda.stream(stream):
+            out = f(*args, **kw)
+        for a in (*args, *kw.values()):
+            parts = [a] if isinstance(a, torch.Tensor) else vars(a).values() if isinstance(a, (Stash, ExpertPlan)) else ()
+            for t in parts:
+                if isinstance(t, torch.Tensor) and t.is_cuda:
+                    t.record_stream(stream)
+        return out
+
+    return g
+
+
+def _call(name: str, device: torch.device, *args):
+    """Calls the library on torch's current stream of `device`; raises what it refuses."""
+    f = getattr(lib(), name)
+    stream = torch.cuda.current_stream(device).cuda_stream
+    if torch.cuda.current_device() == device.index:
+        rc = f(*args, stream)
+    else:
+        with torch.cuda.device(device):
+            rc = f(*args, stream)
+    if rc != P.POSEIDON_OK:
+        raise PoseidonError(rc, name)
+
+
+def _workspace(name: str, device: torch.device, *sizes):
+    """(tensor or None, address, bytes) of the workspace that the sizes need."""
+    n = getattr(lib(), name + "_workspace")(*sizes)
+    if n == 2 ** 64 - 1:
+        raise PoseidonError(P.POSEIDON_E_RANGE, name)
+    if not n:
+        return None, None, 0
+    w = torch.empty(n, dtype=torch.uint8, device=device)
+    return w, w.data_ptr(), n
+
+
+def _rows(x, where: str, device=None, dtype=None, shape=None) -> torch.Tensor:
+    """A matrix operand with neighbouring values in a row (copied if it has none)."""
+    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dim() != 2 or x.dtype not in TYPES:
+        _refuse(f"{where}: not a 2-D float32, float16 or bfloat16 tensor on the GPU")
+    if (device is not None and x.device != device) or (dtype is not None and x.dtype != dtype) or \
+            (shape is not None and tuple(x.shape) != tuple(shape)):
+        _refuse(f"{where}: device, type or shape differs from what the others ask for")
+    return x if _pitched(x) else x.contiguous()
+
+
+def _pitched(x) -> bool:
+    rows, width = x.shape
+    return (width <= 1 or x.stride(1) == 1) and (rows <= 1 or x.stride(0) >= width)
+
+
+def _pitch(x) -> int:
+    return max(x.stride(0), x.shape[1]) if x.shape[0] > 1 else x.shape[1]
+
+
+def _out(out, where: str, device, dtype, shape) -> torch.Tensor:
+    """An output the caller brought, or a new one."""
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(out, torch.Tensor) or out.device != device or out.dtype != dtype or \
+            tuple(out.shape) != tuple(shape) or not (_pitched(out) if out.dim() == 2 else out.is_contiguous()):
+        _refuse(f"{where}: device, type, shape or layout differs from the result's")
+    return out
+
+
+def _whole(x, where: str, device, dtype, shape) -> torch.Tensor:
+    """An operand without gaps (copied if it has some)."""
+    if not isinstance(x, torch.Tensor) or x.device != device or x.dtype != dtype or \
+            (shape is not None and tuple(x.shape) != tuple(shape)):
+        _refuse(f"{where}: not a {dtype} tensor of shape {shape} on {device}")
+    return x.contiguous()
+
+
+def _groups(width: int) -> int:
+    return -(-width // GROUP)
+
+
+def _new_stash(rows: int, width: int, dtype, device) -> Stash:
+    g = _groups(width)
+    return Stash(torch.empty(rows, g * GROUP, dtype=torch.int8, device=device),
+                 torch.empty(rows, g, dtype=torch.uint8, device=device), width, dtype)
+
+
+def _stash(s, where: str, device, rows=None, width=None) -> Stash:
+    if not isinstance(s, Stash) or s.scales.dim() != 2 or (rows is not None and s.rows != rows) or \
+            (width is not None and s.width != width):
+        _refuse(f"{where}: not a Stash of these sizes")
+    n, g = s.rows, _groups(s.width)
+    return Stash(_whole(s.codes, where, device, torch.int8, (n, g * GROUP)),
+                 _whole(s.scales, where, device, torch.uint8, (n, g)), s.width, s.dtype)
+
+
+# ---- activations kept in 8 bits ----
+
+@_streamed
+def poseidon_stash(x) -> Stash:
+    """Rows of x [rows, width] kept in 8 bits."""
+    x = _rows(x, "poseidon_stash: x")
+    n, d = x.shape
+    s = _new_stash(n, d, x.dtype, x.device)
+    _call("poseidon_stash", x.device, x.data_ptr(), _pitch(x), TYPES[x.dtype], n, d, s.codes.data_ptr(),
+          s.scales.data_ptr())
+    return s
+
+
+@_streamed
+def poseidon_restore(stash: Stash, *, dtype=None, out=None) -> torch.Tensor:
+    """What was kept, [rows, width], in its own type or in `dtype`."""
+    dtype = stash.dtype if dtype is None else dtype
+    if dtype not in TYPES or not stash.codes.is_cuda:
+        _refuse("poseidon_restore: stash on the GPU, and a float32, float16 or bfloat16 result")
+    device = stash.codes.device
+    s = _stash(stash, "poseidon_restore: stash", device)
+    out = _out(out, "poseidon_restore: out", device, dtype, (s.rows, s.width))
+    _call("poseidon_restore", device, s.codes.data_ptr(), s.scales.data_ptr(), s.rows, s.width, out.data_ptr(),
+          _pitch(out), TYPES[dtype])
+    return out
+
+
+@_streamed
+def poseidon_gated_forward(gate, up, *, keep: bool = True, out=None) -> Tuple[torch.Tensor, Optional[Stash], Optional[Stash]]:
+    """(silu(gate) * up, gate kept in 8 bits, up kept in 8 bits); without `keep` the latter are None."""
+    gate = _rows(gate, "poseidon_gated_forward: gate")
+    n, d = gate.shape
+    dev, dt = gate.device, gate.dtype
+    up = _rows(up, "poseidon_gated_forward: up", dev, dt, (n, d))
+    out = _out(out, "poseidon_gated_forward: out", dev, dt, (n, d))
+    sg = _new_stash(n, d, dt, dev) if keep else None
+    su = _new_stash(n, d, dt, dev) if keep else None
+    kept = [t.data_ptr() for s in (sg, su) for t in (s.codes, s.scales)] if keep else [None] * 4
+    _call("poseidon_gated_forward", dev, gate.data_ptr(), _pitch(gate), up.data_ptr(), _pitch(up), TYPES[dt], n, d,
+          out.data_ptr(), _pitch(out), *kept)
+    return out, sg, su
+
+
+@_streamed
+def poseidon_gated_backward(dout, gate: Stash, up: Stash, *, dgate=None, dup=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(dgate, dup) at the kept gate and up."""
+    dout = _rows(dout, "poseidon_gated_backward: dout")
+    n, d = dout.shape
+    dev, dt = dout.device, dout.dtype
+    gate = _stash(gate, "poseidon_gated_backward: gate", dev, n, d)
+    up = _stash(up, "poseidon_gated_backward: up", dev, n, d)
+    dgate = _out(dgate, "poseidon_gated_backward: dgate", dev, dt, (n, d))
+    dup = _out(dup, "poseidon_gated_backward: dup", dev, dt, (n, d))
+    _call("poseidon_gated_backward", dev, dout.data_ptr(), _pitch(dout), TYPES[dt], n, d, gate.codes.data_ptr(),
+          gate.scales.data_ptr(), up.codes.data_ptr(), up.scales.data_ptr(), dgate.data_ptr(), _pitch(dgate),
+          dup.data_ptr(), _pitch(dup))
+    return dgate, dup
+
+
+@_streamed
+def poseidon_weight_gradient(dy, x: Stash, *, offsets=None, dtype=torch.float32, out=None,
+                             accumulate: bool = False) -> torch.Tensor:
+    """dy^T x from the kept x: [out_width, in_width], or with int32 offsets [ranges + 1] one for each range of rows,
+    [ranges, out_width, in_width].  With accumulate it is added to `out`."""
+    dy = _rows(dy, "poseidon_weight_gradient: dy")
+    n, o = dy.shape
+    dev = dy.device
+    x = _stash(x, "poseidon_weight_gradient: x", dev, n)
+    if accumulate and out is None:
+        _refuse("poseidon_weight_gradient: accumulate without out")
+    ranges = 1
+    if offsets is not None:
+        offsets = _whole(offsets, "poseidon_weight_gradient: offsets", dev, torch.int32, None)
+        if offsets.dim() != 1 or offsets.numel() < 2:
+            _refuse("poseidon_weight_gradient: offsets: not int32 [ranges + 1]")
+        ranges = offsets.numel() - 1
+    dtype = dtype if out is None else out.dtype
+    if dtype not in TYPES:
+        _refuse("poseidon_weight_gradient: a float32, float16 or bfloat16 result")
+    shape = (o, x.width) if offsets is None else (ranges, o, x.width)
+    out = _out(out, "poseidon_weight_gradient: out", dev, dtype, shape)
+    if not out.is_contiguous():
+        _refuse("poseidon_weight_gradient: out has gaps")
+    w, at, size = _workspace("poseidon_weight_gradient", dev, n, o, x.width, ranges)
+    _call("poseidon_weight_gradient", dev, dy.data_ptr(), _pitch(dy), TYPES[dy.dtype], n, o, x.codes.data_ptr(),
+          x.scales.data_ptr(), x.width, None if offsets is None else offsets.data_ptr(), ranges, out.data_ptr(),
+          TYPES[dtype], int(accumulate), at, size)
+    return out
+
+
+# ---- tokens by expert ----
+
+@_streamed
+def poseidon_expert_sort(choice, n_experts: int) -> ExpertPlan:
+    """Stable order of the choices [tokens, k] (int32) by expert; what is outside [0, n_experts) is dropped."""
+    if not isinstance(choice, torch.Tensor) or not choice.is_cuda or choice.dim() != 2 or choice.dtype != torch.int32:
+        _refuse("poseidon_expert_sort: choice: not an int32 [tokens, k] tensor on the GPU")
+    choice = choice.contiguous()
+    n, k = choice.shape
+    dev = choice.device
+    if not 0 < n_experts <= EXPERTS_MAX or not k:
+        raise PoseidonError(P.POSEIDON_E_INVAL if n_experts < 1 or not k else P.POSEIDON_E_RANGE, "poseidon_expert_sort")
+    plan = ExpertPlan(torch.empty(n * k, dtype=torch.int32, device=dev), torch.empty_like(choice),
+                      torch.empty(n_experts + 1, dtype=torch.int32, device=dev))
+    w, at, size = _workspace("poseidon_expert_sort", dev, n, k, n_experts)
+    _call("poseidon_expert_sort", dev, choice.data_ptr(), n, k, n_experts, plan.order.data_ptr(),
+          plan.position.data_ptr(), plan.offsets.data_ptr(), at, size)
+    return plan
+
+
+def _plan(plan, where: str, device, tokens: int) -> Tuple[torch.Tensor, torch.Tensor, int]:
+    """(position, the number of kept choices as a one-element view, k)"""
+    if not isinstance(plan, ExpertPlan) or plan.position.dim() != 2 or plan.position.shape[0] != tokens or \
+            plan.offsets.dim() != 1 or plan.offsets.numel() < 2:
+        _refuse(f"{where}: not the ExpertPlan of these tokens")
+    position = _whole(plan.position, where, device, torch.int32, None)
+    offsets = _whole(plan.offsets, where, device, torch.int32, None)
+    return position, offsets[-1:], position.shape[1]
+
+
+@_streamed
+def poseidon_expert_gather(x, plan: ExpertPlan, *, keep: bool = False, rows: bool = True):
+    """(x by expert [tokens * k, width], or None without `rows`; the same rows kept in 8 bits, or None without `keep`)."""
+    x = _rows(x, "poseidon_expert_gather: x")
+    n, d = x.shape
+    dev, dt = x.device, x.dtype
+    position, kept, k = _plan(plan, "poseidon_expert_gather: plan", dev, n)
+    xs = torch.empty(n * k, d, dtype=dt, device=dev) if rows else None
+    s = _new_stash(n * k, d, dt, dev) if keep else None
+    if xs is None and s is None:
+        _refuse("poseidon_expert_gather: neither rows nor keep")
+    _call("poseidon_expert_gather", dev, x.data_ptr(), _pitch(x), TYPES[dt], n, d, position.data_ptr(), k,
+          kept.data_ptr(), xs.data_ptr() if rows else None, s.codes.data_ptr() if keep else None,
+          s.scales.data_ptr() if keep else None)
+    return xs, s
+
+
+@_streamed
+def poseidon_expert_combine(ys, plan: ExpertPlan, weights=None, *, out=None) -> torch.Tensor:
+    """sum over a token's choices of weight * ys row, [tokens, width]; without weights (float32 [tokens, k]) each
+    counts once, which is the gradient of the gather."""
+    ys = _rows(ys, "poseidon_expert_combine: ys").contiguous()
+    n = plan.position.shape[0] if isinstance(plan, ExpertPlan) else 0
+    dev, dt, d = ys.device, ys.dtype, ys.shape[1]
+    position, _, k = _plan(plan, "poseidon_expert_combine: plan", dev, n)
+    if ys.shape[0] != n * k:
+        _refuse("poseidon_expert_combine: ys: not a row for each choice")
+    if weights is not None:
+        weights = _whole(weights, "poseidon_expert_combine: weights", dev, torch.float32, (n, k))
+    out = _out(out, "poseidon_expert_combine: out", dev, dt, (n, d))
+    _call("poseidon_expert_combine", dev, ys.data_ptr(), TYPES[dt], n, d, position.data_ptr(), k,
+          None if weights is None else weights.data_ptr(), out.data_ptr(), _pitch(out))
+    return out
+
+
+@_streamed
+def poseidon_expert_combine_backward(dout, ys, plan: ExpertPlan, weights) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(dys [tokens * k, width], dweights float32 [tokens, k]) of poseidon_expert_combine."""
+    dout = _rows(dout, "poseidon_expert_combine_backward: dout")
+    n, d = dout.shape
+    dev, dt = dout.device, dout.dtype
+    position, kept, k = _plan(plan, "poseidon_expert_combine_backward: plan", dev, n)
+    ys = _rows(ys, "poseidon_expert_combine_backward: ys", dev, dt, (n * k, d)).contiguous()
+    weights = _whole(weights, "poseidon_expert_combine_backward: weights", dev, torch.float32, (n, k))
+    dys, dweights = torch.empty_like(ys), torch.empty_like(weights)
+    _call("poseidon_expert_combine_backward", dev, dout.data_ptr(), _pitch(dout), ys.data_ptr(), TYPES[dt], n, d,
+          position.data_ptr(), k, kept.data_ptr(), weights.data_ptr(), dys.data_ptr(), dweights.data_ptr())
+    return dys, dweights
+
+
+# ---- embedding ----
+
+def _ids(ids, where: str, device) -> torch.Tensor:
+    if not isinstance(ids, torch.Tensor) or ids.dim() != 1:
+        _refuse(f"{where}: not an int32 [tokens] tensor")
+    return _whole(ids, where, device, torch.int32, None)
+
+
+@_streamed
+def poseidon_embed(ids, table, scale: float = 1.0, *, out=None) -> torch.Tensor:
+    """scale * table[ids], [tokens, width]; ids (int32) outside the table give zeros."""
+    table = _rows(table, "poseidon_embed: table")
+    v, d = table.shape
+    dev, dt = table.device, table.dtype
+    ids = _ids(ids, "poseidon_embed: ids", dev)
+    n = ids.numel()
+    out = _out(out, "poseidon_embed: out", dev, dt, (n, d))
+    _call("poseidon_embed", dev, ids.data_ptr(), n, table.data_ptr(), _pitch(table), TYPES[dt], v, d, scale,
+          out.data_ptr(), _pitch(out))
+    return out
+
+
+@_streamed
+def poseidon_embed_backward(ids, dout, vocab: int, scale: float = 1.0, *, dtype=torch.float32, out=None,
+                            accumulate: bool = False) -> torch.Tensor:
+    """Gradient [vocab, width] of the table.  With accumulate the sums are added to `out` and the rows of no token
+    are left alone."""
+    dout = _rows(dout, "poseidon_embed_backward: dout")
+    n, d = dout.shape
+    dev = dout.device
+    ids = _ids(ids, "poseidon_embed_backward: ids", dev)
+    if ids.numel() != n or (accumulate and out is None):
+        _refuse("poseidon_embed_backward: ids: not one for each row of dout, or accumulate without out")
+    dtype = dtype if out is None else out.dtype
+    if dtype not in TYPES or vocab < 0:
+        _refuse("poseidon_embed_backward: a float32, float16 or bfloat16 result")
+    out = _out(out, "poseidon_embed_backward: out", dev, dtype, (vocab, d))
+    w, at, size = _workspace("poseidon_embed_backward", dev, n, vocab, d)
+    _call("poseidon_embed_backward", dev, ids.data_ptr(), n, dout.data_ptr(), _pitch(dout), TYPES[dout.dtype], vocab, d,
+          scale, out.data_ptr(), _pitch(out), TYPES[dtype], int(accumulate), at, size)
+    return out

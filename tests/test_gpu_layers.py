@@ -1,0 +1,469 @@
+"""The layer operators on the GPU against the 64-bit oracle.
+
+Bounds, derived before the first run: ROUND is a rounding to nearest relative to the value (half a unit in the last
+place at the lower end of a binade), STEP half of the least step below the normal range, V two roundings in 32 bits.
+A sum of n products in 32 bits is off by at most (n + 2) V times the sum of their absolute values, whatever its
+order.
+"""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from oracle import layers as O  # noqa: E402
+from paper_2609_06086_amd import layers as L  # noqa: E402
+from paper_2609_06086_amd import poseidon as P  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+KIND = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+ROUND = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+STEP = {"f32": 2.0 ** -149, "f16": 2.0 ** -25, "bf16": 2.0 ** -133}
+V = 2.0 ** -23
+
+
+@pytest.fixture(scope="module")
+def dev():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    return torch.device("cuda:0")
+
+
+def _make(rng, shape, kind, dev, spread=2.0, pad=0, shift=0):
+    """Values over a few binades; pad: extra columns of the rows' pitch, shift: values before the first one."""
+    n, d = shape
+    v = rng.normal(size=shape) * np.exp(rng.normal(size=shape) * spread)
+    v = np.clip(v, -2e4, 2e4)
+    flat = torch.full((shift + n * (d + pad) + 8,), float("nan"), dtype=KIND[kind], device=dev)
+    x = flat[shift:shift + n * (d + pad)].view(n, d + pad)[:, :d]
+    x.copy_(torch.from_numpy(v).to(dev))
+    return x
+
+
+def _np(x):
+    return x.double().cpu().numpy()
+
+
+def _check(got, want, slack, kind):
+    """|got - want| <= slack + the rounding to `kind`."""
+    got = _np(got)
+    assert got.shape == want.shape
+    off = np.abs(got - want) - (slack + ROUND[kind] * (np.abs(want) + slack) + STEP[kind])
+    assert (off <= 0).all(), (float(off.max()), np.unravel_index(off.argmax(), off.shape))
+
+
+def _same(got, want):
+    assert np.array_equal(_np(got), want, equal_nan=True)
+
+
+SHAPES = [(1, 1), (1, 64), (3, 7), (5, 8), (2, 63), (4, 65), (33, 200), (17, 1365), (64, 1024), (700, 130)]
+KINDS = ["f32", "f16", "bf16"]
+
+
+# ---- activations kept in 8 bits ----
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("pad, shift", [(0, 0), (3, 1)])
+def test_stash_and_restore(dev, kind, shape, pad, shift):
+    x = _make(np.random.default_rng(1), shape, kind, dev, pad=pad, shift=shift)
+    s = L.poseidon_stash(x)
+    codes, scales = O.stash(_np(x), kind)
+    assert np.array_equal(s.codes.cpu().numpy(), codes) and np.array_equal(s.scales.cpu().numpy(), scales)
+    want = O.restore(codes, scales, shape[1])
+    _same(L.poseidon_restore(s), want)
+    _same(L.poseidon_restore(s, dtype=torch.float32), want)
+    out = torch.full((shape[0], shape[1] + 5), 7.0, dtype=KIND[kind], device=dev)
+    L.poseidon_restore(s, out=out[:, 2:2 + shape[1]])
+    _same(out[:, 2:2 + shape[1]], want)
+    assert (out[:, :2] == 7).all() and (out[:, 2 + shape[1]:] == 7).all()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_stash_of_extreme_values(dev, kind):
+    """Zeros, the largest and smallest values, exact powers and their neighbours, ties, infinities and NaN."""
+    info = torch.finfo(KIND[kind])
+    rows = torch.zeros(16, 128, dtype=torch.float64)
+    rows[1, :] = info.max
+    rows[2, :] = -info.max
+    rows[3, 0] = info.smallest_normal
+    rows[4, 5] = info.smallest_normal * info.eps        # the least value there is
+    rows[5, 0], rows[5, 1] = 127.0, 126.5               # the end of a scale's range, a tie
+    rows[6, 0], rows[6, 1:8] = 127.5, torch.arange(7) + 0.5
+    rows[7, :64] = torch.arange(64) * 0.5 - 16
+    rows[8, 3], rows[9, 70], rows[10, 127] = float("inf"), float("-inf"), float("nan")
+    rows[11, :] = 1.0
+    rows[12, 0], rows[12, 64] = info.max, info.smallest_normal
+    rows[13, :] = torch.arange(128) % 2 * -0.0
+    rows[14, 0], rows[15, 0] = 2.0 ** -14, 254.0
+    x = rows.to(KIND[kind]).to(dev)
+    s = L.poseidon_stash(x)
+    codes, scales = O.stash(_np(x), kind)
+    assert np.array_equal(s.codes.cpu().numpy(), codes) and np.array_equal(s.scales.cpu().numpy(), scales)
+    back = L.poseidon_restore(s)
+    _same(back, O.restore(codes, scales, 128))
+    fine = torch.isfinite(x).view(16, 2, 64).all(2).repeat_interleave(64, 1)
+    assert (torch.isfinite(back) == fine).all()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("shape", SHAPES)
+def test_gated(dev, kind, shape):
+    rng = np.random.default_rng(2)
+    n, d = shape
+    both = _make(rng, (n, 2 * d), kind, dev, spread=1.0, shift=1)
+    gate, up = both[:, :d], both[:, d:]
+    dout = _make(rng, shape, kind, dev, spread=1.0, pad=1)
+    out, sg, su = L.poseidon_gated_forward(gate, up)
+    g, u, w = _np(gate), _np(up), _np(dout)
+    want = O.gated_forward(g, u)
+    # exp of an argument rounded once: off by |g| 2^-24 relative, as is its share of the sigmoid
+    _check(out, want, 8 * V * np.abs(want) * (1 + np.abs(g)), kind)
+    assert torch.equal(out, L.poseidon_gated_forward(gate, up, keep=False)[0])
+    for s, x in ((sg, g), (su, u)):
+        codes, scales = O.stash(x, kind)
+        assert np.array_equal(s.codes.cpu().numpy(), codes) and np.array_equal(s.scales.cpu().numpy(), scales)
+    g, u = (O.restore(*O.stash(x, kind), d) for x in (g, u))
+    dg, du = O.gated_backward(w, g, u)
+    a, b = L.poseidon_gated_backward(dout, sg, su)
+    s = O.sigmoid(g)
+    _check(a, dg, 8 * V * np.abs(w * u * s) * (1 + np.abs(g)) ** 2, kind)
+    _check(b, du, 8 * V * np.abs(du) * (1 + np.abs(g)), kind)
+
+
+def test_gated_with_infinities(dev):
+    """An infinity makes its own output what the formula gives, and its group's gradient NaN; the rest is untouched."""
+    x = torch.ones(2, 128, dtype=torch.bfloat16, device=dev)
+    gate = x.clone()
+    gate[0, 3] = float("inf")
+    out, sg, su = L.poseidon_gated_forward(gate, x)
+    assert torch.isinf(out[0, 3]) and torch.isfinite(out).sum() == 255
+    a, b = L.poseidon_gated_backward(x, sg, su)
+    assert torch.isnan(a[0, :64]).all() and torch.isfinite(a).sum() == 192 and torch.isfinite(b).sum() == 192
+
+
+# ---- weight gradients ----
+
+WIDTHS = [(1, 1), (7, 9), (8, 64), (64, 8), (130, 70), (128, 128), (129, 257), (300, 1365), (1000, 65)]
+
+
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("out_kind", KINDS)
+@pytest.mark.parametrize("widths", WIDTHS)
+@pytest.mark.parametrize("rows", [1, 63, 130, 1100])
+def test_weight_gradient(dev, kind, out_kind, widths, rows):
+    rng = np.random.default_rng(rows)
+    o, i = widths
+    dy = _make(rng, (rows, o), kind, dev, spread=0.5, pad=1, shift=1)
+    x = _make(rng, (rows, i), kind, dev, spread=0.5)
+    s = L.poseidon_stash(x)
+    back = O.restore(*O.stash(_np(x), kind), i)
+    want = O.weight_gradient(_np(dy), back, [0, rows])[0]
+    size = (rows + 2) * V * (np.abs(_np(dy)).T @ np.abs(back))
+    got = L.poseidon_weight_gradient(dy, s, dtype=KIND[out_kind])
+    _check(got, want, size, out_kind)
+    assert torch.equal(got, L.poseidon_weight_gradient(dy, s, dtype=KIND[out_kind]))
+    base = _make(rng, (o, i), out_kind, dev, spread=0.5)
+    acc = base.clone()
+    L.poseidon_weight_gradient(dy, s, out=acc, accumulate=True)
+    _check(acc, want + _np(base), size + V * np.abs(_np(base)), out_kind)
+
+
+RANGES = [[0, 0], [0, 300], [0, 0, 300, 300], [0, 1, 64, 65, 129, 300], [0, 100, 100, 100, 237, 300], [5, 200, 250]]
+
+
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("offsets", RANGES)
+@pytest.mark.parametrize("widths", [(72, 136), (136, 513)])
+def test_weight_gradient_of_ranges(dev, kind, offsets, widths):
+    """Ragged ranges, empty ones (zeros), rows outside every range, and NaN rows next to a range, which it must not read."""
+    rng = np.random.default_rng(3)
+    o, i = widths
+    dy, x = _make(rng, (300, o), kind, dev, spread=0.5), _make(rng, (300, i), kind, dev, spread=0.5)
+    at = torch.tensor(offsets, dtype=torch.int32, device=dev)
+    back = O.restore(*O.stash(_np(x), kind), i)
+    want = O.weight_gradient(_np(dy), back, offsets)
+    size = np.stack([302 * V * (np.abs(_np(dy)[a:b]).T @ np.abs(back[a:b])) for a, b in zip(offsets, offsets[1:])])
+    got = L.poseidon_weight_gradient(dy, L.poseidon_stash(x), offsets=at)
+    _check(got, want, size, "f32")
+    acc = torch.ones_like(got)
+    L.poseidon_weight_gradient(dy, L.poseidon_stash(x), offsets=at, out=acc, accumulate=True)
+    _check(acc, want + 1, size + V, "f32")
+    for r, (a, b) in enumerate(zip(offsets, offsets[1:])):    # the other ranges' rows spoilt
+        dy2, x2 = dy.clone(), x.clone()
+        for t in (dy2, x2):
+            t[:a] = float("nan")
+            t[b:] = float("nan")
+        one = L.poseidon_weight_gradient(dy2, L.poseidon_stash(x2), offsets=at)
+        assert torch.equal(one[r], got[r])
+
+
+def test_weight_gradient_over_tiles_and_splits(dev):
+    """Sizes of each tile and of rows in one or more parts, the sums' bound on each; NaN spreads along its row and column
+    alone."""
+    rng = np.random.default_rng(4)
+    for rows, o, i in ((4096, 256, 256), (5000, 257, 383), (2048, 4096, 2048), (700, 4100, 2050), (9000, 64, 64)):
+        dy, x = _make(rng, (rows, o), "bf16", dev, 0.5), _make(rng, (rows, i), "bf16", dev, 0.5)
+        s = L.poseidon_stash(x)
+        back = L.poseidon_restore(s, dtype=torch.float32).double()
+        want = (dy.double().t().contiguous() @ back).cpu().numpy()
+        size = (rows + 2) * V * (dy.double().abs().t().contiguous() @ back.abs()).cpu().numpy()
+        _check(L.poseidon_weight_gradient(dy, s), want, size, "f32")
+    dy[100, 3], x[200, 7] = float("nan"), float("inf")
+    got = L.poseidon_weight_gradient(dy, L.poseidon_stash(x))
+    bad = torch.zeros(64, 64, dtype=torch.bool, device=dev)
+    bad[3, :] = True
+    bad[:, :64] = True                # the group of the infinity is NaN as a whole
+    assert torch.equal(torch.isnan(got), bad)
+
+
+# ---- experts ----
+
+BATCHES = [(1, 1, 1), (1, 8, 64), (5, 2, 3), (100, 3, 8), (700, 8, 33), (2100, 2, 511), (33000, 4, 256), (300000, 2, 64)]
+
+
+def _sort64(choice, experts):
+    """The oracle's sort, without its lists for long batches."""
+    if choice.size < 20000:
+        return O.expert_sort(choice, experts)
+    key = choice.reshape(-1).astype(np.int64)
+    key[(key < 0) | (key >= experts)] = experts
+    order = np.argsort(key, kind="stable")
+    offsets = np.searchsorted(key[order], np.arange(experts + 1))
+    position = np.full(key.size, -1, np.int64)
+    position[order[:offsets[-1]]] = np.arange(offsets[-1])
+    return order, position.reshape(choice.shape), offsets
+
+
+@pytest.mark.parametrize("tokens, k, experts", BATCHES)
+@pytest.mark.parametrize("how", ["spread", "dropped", "one", "none"])
+def test_expert_sort(dev, tokens, k, experts, how):
+    rng = np.random.default_rng(5)
+    choice = rng.integers(0, experts, size=(tokens, k))
+    if how == "dropped":
+        choice = rng.integers(-2, experts + 2, size=(tokens, k))
+    if how == "one":
+        choice[:] = experts - 1
+    if how == "none":
+        choice[:] = -1
+    plan = L.poseidon_expert_sort(torch.from_numpy(choice.astype(np.int32)).to(dev), experts)
+    for got, want in zip((plan.order, plan.position, plan.offsets), _sort64(choice, experts)):
+        assert np.array_equal(got.cpu().numpy(), want)
+
+
+def test_expert_sort_of_nothing(dev):
+    plan = L.poseidon_expert_sort(torch.zeros(0, 2, dtype=torch.int32, device=dev), 5)
+    assert plan.order.numel() == 0 and (plan.offsets == 0).all()
+
+
+def test_sort_of_many_blocks(dev):
+    """More blocks than add up the counts of the ones before them by themselves."""
+    rng = np.random.default_rng(6)
+    choice = rng.integers(-1, 300, size=(170000, 4))
+    plan = L.poseidon_expert_sort(torch.from_numpy(choice.astype(np.int32)).to(dev), 300)
+    for got, want in zip((plan.order, plan.position, plan.offsets), _sort64(choice, 300)):
+        assert np.array_equal(got.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("tokens, k, experts, width", [(1, 8, 64, 200), (1, 1, 2, 1), (9, 2, 3, 7), (40, 3, 8, 65),
+                                                        (70, 11, 20, 1000), (130, 8, 16, 2056)])
+@pytest.mark.parametrize("how", ["all", "dropped", "none"])
+def test_experts(dev, kind, tokens, k, experts, width, how):
+    rng = np.random.default_rng(7)
+    choice = rng.integers(0 if how == "all" else -experts if how == "dropped" else -1, experts if how != "none" else 0,
+                          size=(tokens, k))
+    order, position, offsets = O.expert_sort(choice, experts)
+    plan = L.poseidon_expert_sort(torch.from_numpy(choice.astype(np.int32)).to(dev), experts)
+    x = _make(rng, (tokens, width), kind, dev, pad=1, shift=1)
+    xs, kept = L.poseidon_expert_gather(x, plan, keep=True)
+    want = O.expert_gather(_np(x), position)
+    _same(xs, want)
+    codes, scales = O.stash(want, kind)
+    assert np.array_equal(kept.codes.cpu().numpy(), codes) and np.array_equal(kept.scales.cpu().numpy(), scales)
+    assert torch.equal(L.poseidon_expert_gather(x, plan)[0], xs)
+    only = L.poseidon_expert_gather(x, plan, keep=True, rows=False)
+    assert only[0] is None and torch.equal(only[1].codes, kept.codes) and torch.equal(only[1].scales, kept.scales)
+
+    ys = _make(rng, (tokens * k, width), kind, dev, spread=1.0)
+    ys[int(offsets[-1]):] = float("nan")            # places of no choice are not read
+    dout = _make(rng, (tokens, width), kind, dev, spread=1.0, pad=3)
+    w = torch.from_numpy(rng.uniform(-1, 1, size=(tokens, k)).astype(np.float32)).to(dev)
+    y, wn, dn = np.nan_to_num(_np(ys)), _np(w), _np(dout)
+    for weights, wv in ((w, wn), (None, np.ones_like(wn))):
+        _check(L.poseidon_expert_combine(ys, plan, weights), O.expert_combine(y, position, wv),
+               (k + 2) * V * O.expert_combine(np.abs(y), position, np.abs(wv)), kind)
+    dys, dw = L.poseidon_expert_combine_backward(dout, ys, plan, w)
+    a, b = O.expert_combine_backward(dn, y, position, wn)
+    _check(dys, a, V * np.abs(a), kind)
+    _check(dw, b, (width + 2) * V * O.expert_combine_backward(np.abs(dn), np.abs(y), position, wn)[1], "f32")
+
+
+# ---- embedding ----
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("out_kind", KINDS)
+@pytest.mark.parametrize("tokens, vocab, width", [(1, 1, 1), (1, 100, 64), (3, 2, 7), (50, 1000, 65), (333, 40, 520),
+                                                   (5000, 7, 130), (4500, 70000, 24)])
+def test_embedding(dev, kind, out_kind, tokens, vocab, width):
+    rng = np.random.default_rng(8)
+    ids = np.minimum((rng.pareto(0.5, size=tokens)).astype(np.int64), vocab - 1)
+    ids[rng.random(tokens) < 0.1] = -1
+    ids[rng.random(tokens) < 0.05] = vocab
+    at = torch.from_numpy(ids.astype(np.int32)).to(dev)
+    table = _make(rng, (vocab, width), kind, dev, pad=1, shift=1)
+    dout = _make(rng, (tokens, width), kind, dev, spread=1.0, pad=2)
+    want = O.embed(ids, _np(table), 1.25)
+    _check(L.poseidon_embed(at, table, 1.25), want, V * np.abs(want), kind)
+    dn = _np(dout)
+    many = max(1, int(np.bincount(ids[(ids >= 0) & (ids < vocab)], minlength=1).max())) if tokens else 1
+    want, size = O.embed_backward(ids, dn, vocab, 1.25), (many + 2) * V * O.embed_backward(ids, np.abs(dn), vocab, 1.25)
+    got = L.poseidon_embed_backward(at, dout, vocab, 1.25, dtype=KIND[out_kind])
+    _check(got, want, size, out_kind)
+    assert torch.equal(got, L.poseidon_embed_backward(at, dout, vocab, 1.25, dtype=KIND[out_kind]))
+    base = _make(rng, (vocab, width), out_kind, dev, spread=0.5, pad=1)
+    acc = base.clone()
+    L.poseidon_embed_backward(at, dout, vocab, 1.25, out=acc, accumulate=True)
+    _check(acc, want + _np(base), size + V * np.abs(_np(base)), out_kind)
+    rest = np.ones(vocab, bool)
+    rest[ids[(ids >= 0) & (ids < vocab)]] = False
+    assert np.array_equal(_np(acc)[rest], _np(base)[rest])
+
+
+@pytest.mark.parametrize("tokens", [8, 9, 4097, 40000])
+def test_embedding_gradient_of_one_token(dev, tokens):
+    """Every place the same token: its sum crosses every chunk."""
+    ids = torch.full((tokens,), 3, dtype=torch.int32, device=dev)
+    dout = torch.ones(tokens, 20, dtype=torch.bfloat16, device=dev)
+    got = L.poseidon_embed_backward(ids, dout, 5, 0.5)
+    assert (got[3] == tokens * 0.5).all() and got.abs().sum() == tokens * 10
+    assert (L.poseidon_embed_backward(ids[:0], dout[:0], 5) == 0).all()
+    assert (L.poseidon_embed_backward(ids - 9, dout, 5) == 0).all()
+
+
+# ---- addresses, streams, graphs ----
+
+def test_offsets_past_32_bits(dev):
+    """More than 2^32 values in a matrix: the last rows are the right ones."""
+    rows, width = 70001, 65536
+    x = torch.zeros(rows, width, dtype=torch.bfloat16, device=dev)
+    tail = torch.randn(3, width, device=dev).bfloat16()
+    x[-3:] = tail
+    s, few = L.poseidon_stash(x), L.poseidon_stash(tail)
+    assert torch.equal(s.codes[-3:], few.codes) and torch.equal(s.scales[-3:], few.scales)
+    back = L.poseidon_restore(s)
+    assert torch.equal(back[-3:], L.poseidon_restore(few)) and back[:-3].count_nonzero() == 0
+    del back
+    out, sg, su = L.poseidon_gated_forward(x, x)
+    a, b = L.poseidon_gated_forward(tail, tail)[:2]
+    assert torch.equal(out[-3:], a) and torch.equal(sg.codes[-3:], b.codes)
+    del out, sg, su
+    ids = torch.tensor([rows - 1, 0, rows - 2], dtype=torch.int32, device=dev)
+    assert torch.equal(L.poseidon_embed(ids, x)[0], tail[2])
+    L.poseidon_embed_backward(ids, tail, rows, out=x, accumulate=True)
+    assert torch.equal(x[-1], tail[2] + tail[0]) and torch.equal(x[-2], tail[1] + tail[2]) and torch.equal(x[0], tail[1])
+    # a weight gradient whose last rows lie past 2^32 codes: 62 zero rows and the last three
+    offsets = torch.tensor([rows - 65, rows], dtype=torch.int32, device=dev)
+    dy = torch.zeros(rows, 8, dtype=torch.bfloat16, device=dev)
+    dy[-3:] = 1.0
+    grad = L.poseidon_weight_gradient(dy, s, offsets=offsets)
+    want = L.poseidon_restore(few, dtype=torch.float32).double().sum(0)
+    assert (grad[0].double() - want).abs().max() <= 8 * V * L.poseidon_restore(few).double().abs().sum(0).max()
+
+
+def _block(x, ids, table, choice, weights, experts):
+    """A small block: embed, sort, gather and keep, gated activation, combine, and everything back."""
+    h = L.poseidon_embed(ids, table, 2.0)
+    plan = L.poseidon_expert_sort(choice, experts)
+    xs, kept = L.poseidon_expert_gather(h + x, plan, keep=True)
+    a, g, u = L.poseidon_gated_forward(xs, xs)
+    y = L.poseidon_expert_combine(a, plan, weights)
+    dys, dw = L.poseidon_expert_combine_backward(y, a, plan, weights)
+    dg, du = L.poseidon_gated_backward(dys, g, u)
+    grad = L.poseidon_weight_gradient(dg, kept, offsets=plan.offsets)
+    dx = L.poseidon_expert_combine(du, plan)
+    return [h, plan.order, xs, a, y, dys, dw, dg, du, grad, dx, L.poseidon_embed_backward(ids, dx, table.shape[0], 2.0),
+            L.poseidon_restore(kept)]
+
+
+def _block_inputs(dev, seed):
+    g = torch.Generator(device=dev)
+    g.manual_seed(seed)
+    n, d, k, e, v = 200, 136, 2, 6, 50
+    return (torch.randn(n, d, generator=g, device=dev).bfloat16(),
+            torch.randint(-1, v, (n,), generator=g, device=dev, dtype=torch.int32),
+            torch.randn(v, d, generator=g, device=dev).bfloat16(),
+            torch.randint(-1, e, (n, k), generator=g, device=dev, dtype=torch.int32),
+            torch.rand(n, k, generator=g, device=dev), e)
+
+
+def test_other_streams(dev):
+    """On a stream of its own, named or current, with inputs made on another: the same bits."""
+    args = _block_inputs(dev, 1)
+    want = _block(*args)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = _block(*args)
+    side.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    for stream in (side, side.cuda_stream, 0):
+        s = L.poseidon_stash(args[0], stream=stream)
+        back = L.poseidon_restore(s, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(back, L.poseidon_restore(L.poseidon_stash(args[0])))
+
+
+def test_capture_and_replay(dev):
+    """The block in a graph, replayed on new inputs with eager work between the replays."""
+    args = _block_inputs(dev, 2)
+    _block(*args)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = _block(*args)
+    for seed in (3, 4, 5):
+        new = _block_inputs(dev, seed)
+        for a, b in zip(args[:5], new[:5]):
+            a.copy_(b)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(got, _block(*new)):
+            assert torch.equal(a, b)
+
+
+def test_refusals_on_the_gpu(dev):
+    """Shapes, types and layouts that do not fit each other."""
+    x = torch.zeros(4, 64, dtype=torch.bfloat16, device=dev)
+    s = L.poseidon_stash(x)
+    plan = L.poseidon_expert_sort(torch.zeros(4, 2, dtype=torch.int32, device=dev), 2)
+    w = torch.zeros(4, 2, device=dev)
+    ids = torch.zeros(4, dtype=torch.int32, device=dev)
+    calls = [
+        lambda: L.poseidon_stash(x[0]), lambda: L.poseidon_stash(x.double()), lambda: L.poseidon_stash(x[:, :0]),
+        lambda: L.poseidon_restore(s, dtype=torch.int8), lambda: L.poseidon_restore(s, out=x[:3]),
+        lambda: L.poseidon_gated_forward(x, x[:3]), lambda: L.poseidon_gated_forward(x, x.half()),
+        lambda: L.poseidon_gated_backward(x[:3], s, s), lambda: L.poseidon_weight_gradient(x.float(), s),
+        lambda: L.poseidon_weight_gradient(x[:3], s), lambda: L.poseidon_weight_gradient(x, s, accumulate=True),
+        lambda: L.poseidon_weight_gradient(x, s, offsets=ids.long()),
+        lambda: L.poseidon_weight_gradient(x, s, out=torch.zeros(64, 128, device=dev)[:, ::2]),
+        lambda: L.poseidon_expert_sort(ids, 2), lambda: L.poseidon_expert_sort(ids.view(2, 2).long(), 2),
+        lambda: L.poseidon_expert_sort(ids.view(2, 2), 0), lambda: L.poseidon_expert_sort(ids.view(2, 2), 512),
+        lambda: L.poseidon_expert_gather(x[:3], plan), lambda: L.poseidon_expert_gather(x, plan, rows=False),
+        lambda: L.poseidon_expert_combine(x, plan, w), lambda: L.poseidon_expert_combine_backward(x, x, plan, w),
+        lambda: L.poseidon_embed(ids.long(), x), lambda: L.poseidon_embed(ids.cpu(), x),
+        lambda: L.poseidon_embed_backward(ids[:3], x, 8), lambda: L.poseidon_embed_backward(ids, x, 8, accumulate=True),
+    ]
+    for f in calls:
+        with pytest.raises(P.PoseidonError) as ei:
+            f()
+        assert ei.value.status in (P.POSEIDON_E_INVAL, P.POSEIDON_E_RANGE)
+
+
+def test_layouts_that_are_copied(dev):
+    """Transposed, broadcast and strided inputs give what their copies give."""
+    x = torch.randn(96, 80, device=dev).bfloat16()
+    for view in (x.t(), x[:, ::2], x[:1].expand(40, 80), x[::3], x[5:6, 3:]):
+        s, c = L.poseidon_stash(view), L.poseidon_stash(view.contiguous())
+        assert torch.equal(s.codes, c.codes) and torch.equal(s.scales, c.scales)
