@@ -53,6 +53,7 @@ extern "C" {
 
 #define POSEIDON_GROUP 64                  /* values that share a scale */
 #define POSEIDON_WIDTH_MAX (1u << 20)      /* values in a row */
+#define POSEIDON_PITCH_MAX (1u << 24)      /* values from row to row */
 #define POSEIDON_ROWS_MAX 0x7fffffffu      /* rows; for experts: tokens * k */
 #define POSEIDON_EXPERTS_MAX 511u          /* experts of poseidon_expert_sort */
 #define POSEIDON_RANGES_MAX 65535u         /* row ranges of poseidon_weight_gradient */

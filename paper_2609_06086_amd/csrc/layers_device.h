@@ -185,7 +185,7 @@ inline int check_sizes(uint64_t rows, uint64_t width) {
 }
 inline int check_matrix(const void *p, uint64_t pitch, uint32_t type, uint64_t rows, uint64_t width) {
     if (!known(type) || pitch < width) return POSEIDON_E_INVAL;
-    if (pitch > (1ull << 32)) return POSEIDON_E_RANGE;
+    if (pitch > POSEIDON_PITCH_MAX) return POSEIDON_E_RANGE;
     return rows && (!p || !aligned(p, size_of(type))) ? POSEIDON_E_INVAL : POSEIDON_OK;
 }
 inline int check_stash(const void *codes, const void *scales, uint64_t rows) {

@@ -67,6 +67,29 @@ __device__ __forceinline__ uint32_t place(uint32_t col, uint32_t oct) {
     return col * 8 + ((oct ^ col ^ (col >> 3)) & 7);
 }
 
+// What a block computes.  Blocks go round the eight XCDs in turn, each with an L2 of
+// its own, so an XCD takes a run of neighbouring tiles; a run goes through
+// the tiles four high, so the 32 blocks that an XCD's CUs hold share 4 column ranges of dy and 8 of x
+// (which has half the bytes) and an L2 fetches a twelfth to an eighth of what its blocks ask for.
+struct Unit {
+    uint32_t range, split, tile_o, tile_i;
+};
+
+__device__ __forceinline__ Unit unit_of(const WeightGrad &g) {
+    const uint32_t tiles = g.tiles_o * g.tiles_i, all = tiles * g.splits;
+    Unit u;
+    u.range = blockIdx.x / all;
+    const uint32_t at = blockIdx.x - u.range * all, xcd = at & 7;
+    uint32_t id = xcd * (all / 8) + min(xcd, all & 7) + at / 8;
+    u.split = id / tiles;
+    id -= u.split * tiles;
+    const uint32_t band = id / (4 * g.tiles_i), high = min(4u, g.tiles_o - 4 * band);
+    id -= band * 4 * g.tiles_i;
+    u.tile_i = id / high;
+    u.tile_o = 4 * band + id - u.tile_i * high;
+    return u;
+}
+
 template <class G>
 __device__ __forceinline__ void put(typename G::raw *grad, uint64_t at, float v, uint32_t accumulate) {
     grad[at] = G::down(accumulate ? G::up(grad[at]) + v : v);
@@ -80,9 +103,9 @@ __global__ __launch_bounds__(WO *WI * 64) void weight_gradient_kernel(WeightGrad
     __shared__ Words4 lds_o[kTileO * 8], lds_i[kTileI * 8];
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64);
 
-    const uint32_t tiles = g.tiles_o * g.tiles_i;
-    const uint32_t tile = blockIdx.x % tiles, split = blockIdx.x / tiles % g.splits, range = blockIdx.x / tiles / g.splits;
-    const uint32_t o0 = tile / g.tiles_i * kTileO, i0 = tile % g.tiles_i * kTileI;
+    const Unit unit = unit_of(g);
+    const uint32_t split = unit.split, range = unit.range;
+    const uint32_t o0 = unit.tile_o * kTileO, i0 = unit.tile_i * kTileI;
     uint32_t begin = 0, end = g.rows;
     if (g.offsets) {
         begin = (uint32_t)min(max(g.offsets[range], 0), (int32_t)g.rows);
@@ -210,6 +233,208 @@ __global__ __launch_bounds__(WO *WI * 64) void weight_gradient_kernel(WeightGrad
         }
 }
 
+// ---- tiles of 256 x 256 ----
+//
+// Four waves of 128 x 128 each: a wave reads 8 KB of LDS for 16 matrix
+// instructions of 32 cycles, half of what LDS delivers, where 8 waves of 128 x 64 would ask for
+// three quarters and the writes come on top.  With 256 sums a lane
+// there is one wave a SIMD, so nothing hides behind another wave: LDS holds two
+// steps, and while the matrix instructions work on one, the rows of
+// the next are turned and unpacked between them and those of the one after are on
+// their way.  Rows past the end come back as zeros from the buffers' bounds.
+
+template <int N>
+struct Int {
+    static constexpr int value = N;
+};
+// f(Int<0>), ..., f(Int<N - 1>)
+template <int N, int I = 0, class F>
+__device__ __forceinline__ void each(F &&f) {
+    if constexpr (I < N) {
+        f(Int<I>{});
+        each<N, I + 1>(f);
+    }
+}
+
+// Byte B of a word, signed, as a float: one instruction.
+template <int B>
+__device__ __forceinline__ float signed_byte(uint32_t w) {
+    float v;
+    if constexpr (B == 0)
+        asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0" : "=v"(v) : "v"(w));
+    else if constexpr (B == 1)
+        asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(v) : "v"(w));
+    else if constexpr (B == 2)
+        asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(v) : "v"(w));
+    else
+        asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(v) : "v"(w));
+    return v;
+}
+
+using Rsrc = __amdgpu_buffer_rsrc_t;
+
+__device__ __forceinline__ Rsrc buffer(const void *p, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, bytes, 0x00027000);
+}
+
+template <class T, class G>
+__global__ __launch_bounds__(256, 1) void weight_gradient_wide_kernel(WeightGrad g) {
+    constexpr uint32_t kTile = 256, kPad = 8;    // a tile's first block may begin up to 7 columns before it
+    constexpr uint32_t kBuf = (kTile + kPad) * 8;
+    __shared__ Words4 lds[4 * kBuf];             // dy's two steps, then x's
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+
+    const Unit unit = unit_of(g);
+    const uint32_t split = unit.split, range = unit.range;
+    const uint32_t o0 = unit.tile_o * kTile, i0 = unit.tile_i * kTile;
+    uint32_t begin = 0, end = g.rows;
+    if (g.offsets) {
+        begin = (uint32_t)min(max(g.offsets[range], 0), (int32_t)g.rows);
+        end = (uint32_t)min(max(g.offsets[range + 1], (int32_t)begin), (int32_t)g.rows);
+    }
+    {   // this split's steps
+        const uint32_t steps = (end - begin + kStep - 1) / kStep, each = (steps + g.splits - 1) / g.splits;
+        const uint32_t from = min(split * each, steps), to = min(from + each, steps);
+        end = min(end, begin + to * kStep);
+        begin += from * kStep;
+    }
+
+    const uint32_t cb = tid % (kTile / 8), oct = tid / (kTile / 8);
+    const uint32_t o_first = o0 + cb * 8, i_first = i0 + cb * 8;
+    const uint32_t o_from = min(o_first, g.out_width - 8);
+    const uint32_t dy_row = (uint32_t)g.dy_pitch * 2, x_row = g.groups * kGroup;    // bytes
+    constexpr uint32_t kNowhere = 0x80000000u;
+    const uint32_t dy_at = o_first < g.out_width ? oct * 8 * dy_row + o_from * 2 : kNowhere;
+    const uint32_t x_at = i_first < x_row ? oct * 8 * x_row + i_first : kNowhere;
+    const uint32_t s_at = i_first < x_row ? oct * 8 * g.groups + i_first / kGroup : kNowhere;
+    const int32_t col0 = o_first < g.out_width ? (int32_t)o_from - (int32_t)o0 : (int32_t)(cb * 8);
+
+    // Two steps' rows are on their way in registers while a third is in LDS.  A row's buffer begins at the row, so
+    // the lanes' offsets are the same for all eight.
+    Words4 dy[2][8];
+    uint2 x[2][8];
+    uint32_t sc[2][8];
+    const auto rows_of = [&](const void *base, uint32_t row, uint32_t t0, uint32_t r) {
+        const uint32_t n = t0 + r < end ? min(end - t0, kStep) - r : 0, t = n ? t0 + r : 0;
+        return buffer((const char *)base + (uint64_t)t * row, n * row);
+    };
+    const auto fetch_dy = [&](int set, uint32_t t0, uint32_t r) {
+        dy[set][r] = __builtin_amdgcn_raw_buffer_load_b128(rows_of(g.dy, dy_row, t0, r), dy_at, 0, 0);
+    };
+    const auto fetch_x = [&](int set, uint32_t t0, uint32_t r) {
+        x[set][r] = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(rows_of(g.codes, x_row, t0, r), x_at, 0, 0));
+        sc[set][r] = __builtin_amdgcn_raw_buffer_load_b8(rows_of(g.scales, g.groups, t0, r), s_at, 0, 0);
+    };
+    const auto write_dy = [&](int set, uint32_t buf, int c) {    // column c of the thread's block
+        Words4 w;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+            w[t] = __builtin_amdgcn_perm(dy[set][2 * t + 1][c / 2], dy[set][2 * t][c / 2],
+                                         c & 1 ? 0x07060302u : 0x05040100u);
+        const uint32_t col = (uint32_t)(col0 + c);
+        lds[buf * kBuf + kPad * 8 + (int32_t)place(col, oct)] = w;
+    };
+    // Rows 2 t and 2 t + 1 of column c; with the last two the column is written.
+    // A group of scale byte 255 has codes 0, and 0 times the infinity that byte stands for is NaN.
+    Words4 turned;
+    const auto unpack_x = [&](int set, uint32_t buf, auto column, int t) {
+        constexpr int c = decltype(column)::value;
+        float v[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int r = 2 * t + h;
+            v[h] = signed_byte<c & 3>(c < 4 ? x[set][r].x : x[set][r].y) * __uint_as_float(sc[set][r] << 23);
+        }
+        turned[t] = pack<T>(v[0], v[1]);
+        if (t == 3) lds[(2 + buf) * kBuf + kPad * 8 + place(cb * 8 + c, oct)] = turned;
+    };
+
+    // word of column (wave's first + 32 m + lane % 32), rows [16 s + 8 (lane / 32), ...): off[s ^ 2 (m & 1)] + 256 m
+    const uint32_t c32 = lane % 32, key = (lane / 32 ^ c32 ^ c32 >> 3) & 7;
+    const uint32_t at_o = kPad * 8 + (wave / 2 * 128 + c32) * 8, at_i = 2 * kBuf + kPad * 8 + (wave % 2 * 128 + c32) * 8;
+    Words4 a[2][4], b[2][4];
+    const auto read = [&](uint32_t buf, int s, int j) {    // one of the eight reads of quarter s
+        const int m = j / 2;
+        const uint32_t w = buf * kBuf + (key ^ (2 * (s ^ 2 * (m & 1)))) + m * 256;
+        if (j & 1)
+            b[s & 1][m] = lds[at_i + w];
+        else
+            a[s & 1][m] = lds[at_o + w];
+    };
+    Acc acc[4][4] = {};
+
+    // A quarter of a step: 16 matrix instructions, and after each a little of the
+    // other work, which the instruction's 32 cycles cover.  Quarters 0 and 1 unpack the next step's x,
+    // quarter 2 turns its dy, quarter 3 reads from the next step's LDS words, written by then.
+    const auto quarter = [&](auto which, auto step, uint32_t t0) {
+        constexpr int s = decltype(which)::value, buf = decltype(step)::value, set = buf ^ 1;
+        const auto piece = [&](auto index) {
+            constexpr int j = decltype(index)::value;
+            acc[j / 4][j % 4] = mfma<T>(a[s & 1][j / 4], b[s & 1][j % 4], acc[j / 4][j % 4]);
+            if constexpr (j < 8) read(s < 3 ? buf : buf ^ 1, (s + 1) & 3, j);
+            if constexpr (s < 2) unpack_x(set, buf ^ 1, Int<s * 4 + j / 4>{}, j % 4);
+            if constexpr (s == 2 && j < 8) write_dy(set, buf ^ 1, j);
+            if constexpr (s == 2 && j >= 8) fetch_x(set, t0 + 3 * kStep, j - 8);
+            if constexpr (s == 3 && j < 8) fetch_dy(set, t0 + 3 * kStep, j);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        each<16>(piece);
+    };
+    // Multiplies the step in LDS buffer `buf`, and writes the next one (set buf ^ 1) to the other.
+    const auto step = [&](auto buf, uint32_t t0) {
+        quarter(Int<0>{}, buf, t0);
+        quarter(Int<1>{}, buf, t0);
+        quarter(Int<2>{}, buf, t0);
+        __syncthreads();    // the other buffer is whole, and this one read
+        quarter(Int<3>{}, buf, t0);
+    };
+
+    if (begin < end) {
+        each<8>([&](auto r) {
+            fetch_x(0, begin, decltype(r)::value);
+            fetch_dy(0, begin, decltype(r)::value);
+        });
+        each<8>([&](auto r) {
+            fetch_x(1, begin + kStep, decltype(r)::value);
+            fetch_dy(1, begin + kStep, decltype(r)::value);
+        });
+        each<8>([&](auto c) {
+            write_dy(0, 0, decltype(c)::value);
+            each<4>([&](auto t) { unpack_x(0, 0, c, decltype(t)::value); });
+        });
+        each<8>([&](auto r) {
+            fetch_x(0, begin + 2 * kStep, decltype(r)::value);
+            fetch_dy(0, begin + 2 * kStep, decltype(r)::value);
+        });
+        __syncthreads();
+        each<8>([&](auto j) { read(0, 0, decltype(j)::value); });
+        for (uint32_t t0 = begin; t0 < end; t0 += 2 * kStep) {
+            step(Int<0>{}, t0);
+            step(Int<1>{}, t0 + kStep);    // all zeros after an odd number of steps
+        }
+    }
+
+    const uint64_t base = (uint64_t)range * g.out_width * g.in_width;
+    const uint32_t wo = wave / 2 * 128, wi = wave % 2 * 128;
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            const uint32_t i = i0 + wi + n * 32 + lane % 32;
+            if (i >= g.in_width) continue;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const uint32_t o = o0 + wo + m * 32 + e / 4 * 8 + lane / 32 * 4 + e % 4;
+                if (o >= g.out_width) continue;
+                const uint64_t at = base + (uint64_t)o * g.in_width + i;
+                if (g.splits > 1)
+                    g.parts[split * g.size + at] = acc[m][n][e];
+                else
+                    put<G>((typename G::raw *)g.grad, at, acc[m][n][e], g.accumulate);
+            }
+        }
+}
+
 // Adds the splits' parts, in order.
 template <class G>
 __global__ __launch_bounds__(kBlock) void weight_gradient_join_kernel(const float *parts, uint64_t size, uint32_t splits,
@@ -277,7 +502,13 @@ int poseidon_weight_gradient(const void *dy, uint64_t dy_pitch, uint32_t type, u
     PL_TRY(check_workspace(workspace, workspace_bytes,
                            poseidon_weight_gradient_workspace(rows, out_width, in_width, n_ranges)));
     const hipStream_t stream = (hipStream_t)hip_stream;
-    const WeightPlan p = weight_plan(rows, out_width, in_width, n_ranges);
+    WeightPlan p = weight_plan(rows, out_width, in_width, n_ranges);
+    // The wide kernel's buffer loads want whole words of dy.
+    const bool wide = p.large && aligned(dy, 4) && dy_pitch % 2 == 0 && out_width % 2 == 0 && out_width >= 8;
+    if (p.large && !wide) {
+        p.tiles_o = (uint32_t)((out_width + 127) / 128);
+        p.tiles_i = (uint32_t)((in_width + 127) / 128);
+    }
     WeightGrad g = {};
     g.dy = dy;
     g.dy_pitch = dy_pitch;
@@ -298,7 +529,7 @@ int poseidon_weight_gradient(const void *dy, uint64_t dy_pitch, uint32_t type, u
     const uint32_t blocks = p.tiles_o * p.tiles_i * p.splits * n_ranges;
     const auto run = [&](auto t) {
         using D = decltype(t);
-        PL_TYPE(grad_type, if (p.large) weight_gradient_kernel<D, T, 2, 4, 4, 2><<<blocks, 512, 0, stream>>>(g);
+        PL_TYPE(grad_type, if (wide) weight_gradient_wide_kernel<D, T><<<blocks, 256, 0, stream>>>(g);
                 else weight_gradient_kernel<D, T, 2, 2, 2, 2><<<blocks, 256, 0, stream>>>(g);
                 if (p.splits > 1) {
                     const uint64_t n = (g.size + kBlock - 1) / kBlock;

@@ -22,7 +22,7 @@ from . import poseidon as P
 from .poseidon import PoseidonError
 
 GROUP = 64
-WIDTH_MAX, ROWS_MAX = 1 << 20, 2 ** 31 - 1
+WIDTH_MAX, PITCH_MAX, ROWS_MAX = 1 << 20, 1 << 24, 2 ** 31 - 1
 EXPERTS_MAX, RANGES_MAX, VOCAB_MAX, TILES_MAX = 511, 65535, 2 ** 26 - 1, 1 << 22
 TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 

@@ -29,9 +29,9 @@ def test_library_exports_every_declared_operator():
 def test_limits_match_the_header():
     def value(name):
         return int(re.search(rf"#define POSEIDON_{name} \(?([0-9a-fx<u ]+)\)?", HEADER).group(1).replace("u", "")
-                   .split("<<")[0], 0) << (20 if name == "WIDTH_MAX" else 0)
+                   .split("<<")[0], 0) << {"WIDTH_MAX": 20, "PITCH_MAX": 24}.get(name, 0)
     assert value("GROUP") == L.GROUP == O.GROUP
-    assert value("WIDTH_MAX") == L.WIDTH_MAX
+    assert value("WIDTH_MAX") == L.WIDTH_MAX and value("PITCH_MAX") == L.PITCH_MAX
     for name in ("ROWS_MAX", "EXPERTS_MAX", "RANGES_MAX", "VOCAB_MAX", "TILES_MAX"):
         assert value(name) == getattr(L, name)
 
