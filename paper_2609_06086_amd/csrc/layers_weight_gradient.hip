@@ -20,7 +20,8 @@ using HalfVec = _Float16 __attribute__((ext_vector_type(8)));
 using BrainVec = __bf16 __attribute__((ext_vector_type(8)));
 using Words4 = uint32_t __attribute__((ext_vector_type(4)));
 
-constexpr uint32_t kStep = 64;    // rows of a step
+constexpr uint32_t kStep = 64;       // rows of a step
+constexpr uint32_t kRanked = 256;    // up to so many ranges are taken by length
 
 template <class T>
 __device__ __forceinline__ Acc mfma(Words4 a, Words4 b, Acc c);
@@ -54,7 +55,7 @@ struct WeightGrad {
     const int8_t *codes;
     const uint8_t *scales;
     const int32_t *offsets;
-    uint32_t tiles_o, tiles_i, splits, accumulate;
+    uint32_t ranges, tiles_o, tiles_i, splits, accumulate;
     void *grad;      // [ranges][out_width][in_width]
     float *parts;    // [splits][ranges][out_width][in_width] where splits > 1
     uint64_t size;   // ranges * out_width * in_width
@@ -90,159 +91,6 @@ __device__ __forceinline__ Unit unit_of(const WeightGrad &g) {
     return u;
 }
 
-template <class G>
-__device__ __forceinline__ void put(typename G::raw *grad, uint64_t at, float v, uint32_t accumulate) {
-    grad[at] = G::down(accumulate ? G::up(grad[at]) + v : v);
-}
-
-// WO x WI waves of MO x MI tiles of 32 x 32 each.
-template <class T, class G, int WO, int WI, int MO, int MI>
-__global__ __launch_bounds__(WO *WI * 64) void weight_gradient_kernel(WeightGrad g) {
-    constexpr uint32_t kTileO = WO * MO * 32, kTileI = WI * MI * 32, kWaves = WO * WI;
-    static_assert(kTileO / 8 * 8 == kWaves / 2 * 64 && kTileI == kTileO, "an 8 x 8 block a thread");
-    __shared__ Words4 lds_o[kTileO * 8], lds_i[kTileI * 8];
-    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64);
-
-    const Unit unit = unit_of(g);
-    const uint32_t split = unit.split, range = unit.range;
-    const uint32_t o0 = unit.tile_o * kTileO, i0 = unit.tile_i * kTileI;
-    uint32_t begin = 0, end = g.rows;
-    if (g.offsets) {
-        begin = (uint32_t)min(max(g.offsets[range], 0), (int32_t)g.rows);
-        end = (uint32_t)min(max(g.offsets[range + 1], (int32_t)begin), (int32_t)g.rows);
-    }
-    {   // this split's steps
-        const uint32_t steps = (end - begin + kStep - 1) / kStep, each = (steps + g.splits - 1) / g.splits;
-        const uint32_t from = min(split * each, steps), to = min(from + each, steps);
-        end = min(end, begin + to * kStep);
-        begin += from * kStep;
-    }
-
-    // the thread's block: column block cb of the tile, rows [8 oct, 8 oct + 8) of a step
-    const bool brings_dy = wave < kWaves / 2;
-    const uint32_t block = (wave % (kWaves / 2)) * 64 + lane;
-    const uint32_t cb = block % (kTileO / 8), oct = block / (kTileO / 8);
-    const typename T::raw *dy = (const typename T::raw *)g.dy;
-    const uint32_t o_first = o0 + cb * 8, i_first = i0 + cb * 8;
-    // the last block of dy's columns is moved back to end with the row
-    const uint32_t o_from = g.out_width >= 8 ? min(o_first, g.out_width - 8) : 0;
-    const bool there = brings_dy ? o_first < g.out_width : i_first < g.groups * kGroup;
-    const int32_t col0 = brings_dy ? (int32_t)o_from - (int32_t)o0 : (int32_t)(cb * 8);
-
-    uint32_t st[8][4];    // dy: 8 rows of 4 words; codes: 8 rows of 2 words, and the scale byte in word 2
-    const auto fetch = [&](uint32_t t0) {
-        if (!there) return;
-#pragma unroll
-        for (uint32_t r = 0; r < 8; ++r) {
-            const uint32_t row = min(t0 + oct * 8 + r, end - 1);
-            if (brings_dy) {
-                const typename T::raw *p = dy + (uint64_t)row * g.dy_pitch + o_from;
-                if (g.out_width >= 8) {
-                    __builtin_memcpy(st[r], p, 16);
-                } else {
-                    typename T::raw v[8];
-#pragma unroll
-                    for (uint32_t c = 0; c < 8; ++c) v[c] = c < g.out_width ? p[c] : T::down(0.0f);
-                    __builtin_memcpy(st[r], v, 16);
-                }
-            } else {
-                const uint2 w = *reinterpret_cast<const uint2 *>(g.codes + (uint64_t)row * (g.groups * kGroup) + i_first);
-                st[r][0] = w.x;
-                st[r][1] = w.y;
-                st[r][2] = g.scales[(uint64_t)row * g.groups + i_first / kGroup];
-            }
-        }
-        if (t0 + kStep > end) {    // rows past the end count as zeros
-#pragma unroll
-            for (uint32_t r = 0; r < 8; ++r) {
-                const bool in = t0 + oct * 8 + r < end;
-#pragma unroll
-                for (int w = 0; w < 4; ++w) st[r][w] = in ? st[r][w] : 0u;
-            }
-        }
-    };
-    const auto write = [&]() {
-        if (!there) return;
-        if (brings_dy) {
-#pragma unroll
-            for (int c = 0; c < 8; ++c) {
-                Words4 w;
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-                    w[t] = __builtin_amdgcn_perm(st[2 * t + 1][c / 2], st[2 * t][c / 2], c & 1 ? 0x07060302u : 0x05040100u);
-                if (col0 + c >= 0) lds_o[place((uint32_t)(col0 + c), oct)] = w;
-            }
-        } else {
-            float scale[8];
-#pragma unroll
-            for (int r = 0; r < 8; ++r) scale[r] = scale_of(st[r][2]);
-#pragma unroll
-            for (int c = 0; c < 8; ++c) {
-                float v[8];
-#pragma unroll
-                for (int r = 0; r < 8; ++r) v[r] = (float)(int8_t)(st[r][c / 4] >> (8 * (c & 3))) * scale[r];
-                Words4 w;
-#pragma unroll
-                for (int t = 0; t < 4; ++t) w[t] = pack<T>(v[2 * t], v[2 * t + 1]);
-                lds_i[place((uint32_t)(col0 + c), oct)] = w;
-            }
-        }
-    };
-
-    const uint32_t wo = wave / WI * (MO * 32), wi = wave % WI * (MI * 32);
-    Acc acc[MO][MI] = {};
-    if (begin < end) fetch(begin);
-    for (uint32_t t0 = begin; t0 < end; t0 += kStep) {
-        __syncthreads();
-        write();
-        __syncthreads();
-        if (t0 + kStep < end) fetch(t0 + kStep);
-#pragma unroll
-        for (uint32_t s = 0; s < kStep / 16; ++s) {
-            Words4 a[MO], b[MI];
-            const uint32_t oc = s * 2 + lane / 32;
-#pragma unroll
-            for (int m = 0; m < MO; ++m) a[m] = lds_o[place(wo + m * 32 + lane % 32, oc)];
-#pragma unroll
-            for (int n = 0; n < MI; ++n) b[n] = lds_i[place(wi + n * 32 + lane % 32, oc)];
-#pragma unroll
-            for (int m = 0; m < MO; ++m)
-#pragma unroll
-                for (int n = 0; n < MI; ++n) acc[m][n] = mfma<T>(a[m], b[n], acc[m][n]);
-        }
-    }
-
-    // value 4 q + e of a tile: row 8 q + 4 (lane / 32) + e, column lane % 32
-    const uint64_t base = (uint64_t)range * g.out_width * g.in_width;
-#pragma unroll
-    for (int m = 0; m < MO; ++m)
-#pragma unroll
-        for (int n = 0; n < MI; ++n) {
-            const uint32_t i = i0 + wi + n * 32 + lane % 32;
-            if (i >= g.in_width) continue;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const uint32_t o = o0 + wo + m * 32 + e / 4 * 8 + lane / 32 * 4 + e % 4;
-                if (o >= g.out_width) continue;
-                const uint64_t at = base + (uint64_t)o * g.in_width + i;
-                if (g.splits > 1)
-                    g.parts[split * g.size + at] = acc[m][n][e];
-                else
-                    put<G>((typename G::raw *)g.grad, at, acc[m][n][e], g.accumulate);
-            }
-        }
-}
-
-// ---- tiles of 256 x 256 ----
-//
-// Four waves of 128 x 128 each: a wave reads 8 KB of LDS for 16 matrix
-// instructions of 32 cycles, half of what LDS delivers, where 8 waves of 128 x 64 would ask for
-// three quarters and the writes come on top.  With 256 sums a lane
-// there is one wave a SIMD, so nothing hides behind another wave: LDS holds two
-// steps, and while the matrix instructions work on one, the rows of
-// the next are turned and unpacked between them and those of the one after are on
-// their way.  Rows past the end come back as zeros from the buffers' bounds.
-
 template <int N>
 struct Int {
     static constexpr int value = N;
@@ -277,62 +125,117 @@ __device__ __forceinline__ Rsrc buffer(const void *p, uint32_t bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, bytes, 0x00027000);
 }
 
-template <class T, class G>
-__global__ __launch_bounds__(256, 1) void weight_gradient_wide_kernel(WeightGrad g) {
-    constexpr uint32_t kTile = 256, kPad = 8;    // a tile's first block may begin up to 7 columns before it
+// Four waves on a tile of 32 C x 32 C, 16 C x 16 C a wave, in steps of 64 rows.
+// A thread brings 8 rows of C columns of each operand.
+//
+// C = 8, 256 x 256: a wave reads 8 KB of LDS for 16 matrix instructions of 32 cycles, half of what LDS
+// delivers (8 waves of 128 x 64 would ask for three quarters, and the writes come on top).  With 256
+// sums a lane there is one wave a SIMD, so nothing hides behind another wave: LDS holds two
+// steps, and while the matrix instructions work on one, the rows of the next are turned and
+// unpacked between them; those of the two after are on their way in registers (with only one of them the
+// waits for memory took half of the time).
+// C = 4, 128 x 128: 64 sums a lane and half of the LDS, so that two blocks share a CU.
+//
+// Rows past the end come back as zeros from the buffers' bounds.  ALIGNED: dy's rows begin and end on whole
+// words, as buffer loads want; else they are read with plain loads, which take any address, and masked.
+template <class T, class G, int C, bool ALIGNED>
+__global__ __launch_bounds__(256, C == 8 ? 1 : 2) void weight_gradient_kernel(WeightGrad g) {
+    constexpr uint32_t kTile = 32 * C, kPad = 8;    // a tile's first block may begin up to 7 columns before it
     constexpr uint32_t kBuf = (kTile + kPad) * 8;
-    __shared__ Words4 lds[4 * kBuf];             // dy's two steps, then x's
+    constexpr int M = C / 2, kPieces = M * M;       // a wave's tiles of 32 x 32 along a side, and in all
+    using Row = uint32_t __attribute__((ext_vector_type(C / 2)));    // C values of dy
+    using Codes = uint32_t __attribute__((ext_vector_type(C / 4)));
+    __shared__ Words4 lds[4 * kBuf];                // dy's two steps, then x's
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64);
 
     const Unit unit = unit_of(g);
-    const uint32_t split = unit.split, range = unit.range;
-    const uint32_t o0 = unit.tile_o * kTile, i0 = unit.tile_i * kTile;
-    uint32_t begin = 0, end = g.rows;
+    uint32_t range = unit.range, begin = 0, end = g.rows;
     if (g.offsets) {
-        begin = (uint32_t)min(max(g.offsets[range], 0), (int32_t)g.rows);
-        end = (uint32_t)min(max(g.offsets[range + 1], (int32_t)begin), (int32_t)g.rows);
+        const auto bound = [&](uint32_t r) { return (uint32_t)min(max(g.offsets[r], 0), (int32_t)g.rows); };
+        if (g.ranges <= kRanked) {
+            // the longest range first, so that no long one is left for the end
+            uint32_t *length = (uint32_t *)lds;
+            const uint32_t mine = tid < g.ranges ? max(bound(tid + 1), bound(tid)) - bound(tid) : 0;
+            length[tid] = mine;
+            __syncthreads();
+            uint32_t rank = 0;
+            for (uint32_t r = 0; r < g.ranges; ++r) rank += length[r] > mine || (length[r] == mine && r < tid);
+            __syncthreads();
+            if (tid < g.ranges && rank == unit.range) length[0] = tid;
+            __syncthreads();
+            range = __builtin_amdgcn_readfirstlane(length[0]);
+            __syncthreads();
+        }
+        begin = __builtin_amdgcn_readfirstlane(bound(range));
+        end = max(begin, (uint32_t)__builtin_amdgcn_readfirstlane(bound(range + 1)));
     }
     {   // this split's steps
         const uint32_t steps = (end - begin + kStep - 1) / kStep, each = (steps + g.splits - 1) / g.splits;
-        const uint32_t from = min(split * each, steps), to = min(from + each, steps);
+        const uint32_t from = min(unit.split * each, steps), to = min(from + each, steps);
         end = min(end, begin + to * kStep);
         begin += from * kStep;
     }
 
-    const uint32_t cb = tid % (kTile / 8), oct = tid / (kTile / 8);
-    const uint32_t o_first = o0 + cb * 8, i_first = i0 + cb * 8;
-    const uint32_t o_from = min(o_first, g.out_width - 8);
+    const uint32_t o0 = unit.tile_o * kTile, i0 = unit.tile_i * kTile;
+    const uint32_t cb = tid % 32, oct = tid / 32;
+    const uint32_t o_first = o0 + cb * C, i_first = i0 + cb * C;
+    // the last block of dy's columns is moved back to end with the row
+    const uint32_t o_from = g.out_width >= C ? min(o_first, g.out_width - C) : 0;
     const uint32_t dy_row = (uint32_t)g.dy_pitch * 2, x_row = g.groups * kGroup;    // bytes
     constexpr uint32_t kNowhere = 0x80000000u;
     const uint32_t dy_at = o_first < g.out_width ? oct * 8 * dy_row + o_from * 2 : kNowhere;
     const uint32_t x_at = i_first < x_row ? oct * 8 * x_row + i_first : kNowhere;
     const uint32_t s_at = i_first < x_row ? oct * 8 * g.groups + i_first / kGroup : kNowhere;
-    const int32_t col0 = o_first < g.out_width ? (int32_t)o_from - (int32_t)o0 : (int32_t)(cb * 8);
+    const int32_t col0 = o_first < g.out_width ? (int32_t)o_from - (int32_t)o0 : (int32_t)(cb * C);
 
-    // Two steps' rows are on their way in registers while a third is in LDS.  A row's buffer begins at the row, so
-    // the lanes' offsets are the same for all eight.
-    Words4 dy[2][8];
-    uint2 x[2][8];
+    // A row's buffer begins at the row, so the lanes' offsets are the same for all eight.
+    Row dy[2][8];
+    Codes x[2][8];
     uint32_t sc[2][8];
     const auto rows_of = [&](const void *base, uint32_t row, uint32_t t0, uint32_t r) {
         const uint32_t n = t0 + r < end ? min(end - t0, kStep) - r : 0, t = n ? t0 + r : 0;
         return buffer((const char *)base + (uint64_t)t * row, n * row);
     };
     const auto fetch_dy = [&](int set, uint32_t t0, uint32_t r) {
-        dy[set][r] = __builtin_amdgcn_raw_buffer_load_b128(rows_of(g.dy, dy_row, t0, r), dy_at, 0, 0);
+        if constexpr (C == 8) {
+            static_assert(ALIGNED);
+            dy[set][r] = __builtin_amdgcn_raw_buffer_load_b128(rows_of(g.dy, dy_row, t0, r), dy_at, 0, 0);
+        } else if constexpr (ALIGNED) {
+            dy[set][r] = __builtin_amdgcn_raw_buffer_load_b64(rows_of(g.dy, dy_row, t0, r), dy_at, 0, 0);
+        } else {
+            const uint32_t row = min(t0 + oct * 8 + r, end - 1);
+            const uint16_t *p = (const uint16_t *)g.dy + row * g.dy_pitch + o_from;
+            if (g.out_width >= C) {
+                __builtin_memcpy(&dy[set][r], p, sizeof(Row));
+            } else {
+#pragma unroll
+                for (int w = 0; w < C / 2; ++w)
+                    dy[set][r][w] = (2 * w < g.out_width ? p[2 * w] : 0u) |
+                                    (2 * w + 1 < g.out_width ? (uint32_t)p[2 * w + 1] << 16 : 0u);
+            }
+        }
     };
     const auto fetch_x = [&](int set, uint32_t t0, uint32_t r) {
-        x[set][r] = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(rows_of(g.codes, x_row, t0, r), x_at, 0, 0));
+        const Rsrc codes = rows_of(g.codes, x_row, t0, r);
+        if constexpr (C == 8)
+            x[set][r] = __builtin_amdgcn_raw_buffer_load_b64(codes, x_at, 0, 0);
+        else
+            x[set][r][0] = __builtin_amdgcn_raw_buffer_load_b32(codes, x_at, 0, 0);
         sc[set][r] = __builtin_amdgcn_raw_buffer_load_b8(rows_of(g.scales, g.groups, t0, r), s_at, 0, 0);
     };
-    const auto write_dy = [&](int set, uint32_t buf, int c) {    // column c of the thread's block
+    // Column c of the thread's block, of the rows that begin at t0.
+    const auto write_dy = [&](int set, uint32_t buf, uint32_t t0, int c) {
         Words4 w;
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
-            w[t] = __builtin_amdgcn_perm(dy[set][2 * t + 1][c / 2], dy[set][2 * t][c / 2],
-                                         c & 1 ? 0x07060302u : 0x05040100u);
-        const uint32_t col = (uint32_t)(col0 + c);
-        lds[buf * kBuf + kPad * 8 + (int32_t)place(col, oct)] = w;
+        for (int t = 0; t < 4; ++t) {
+            uint32_t lo = dy[set][2 * t][c / 2], hi = dy[set][2 * t + 1][c / 2];
+            if constexpr (!ALIGNED) {
+                lo = t0 + oct * 8 + 2 * t < end ? lo : 0u;
+                hi = t0 + oct * 8 + 2 * t + 1 < end ? hi : 0u;
+            }
+            w[t] = __builtin_amdgcn_perm(hi, lo, c & 1 ? 0x07060302u : 0x05040100u);
+        }
+        lds[buf * kBuf + kPad * 8 + (int32_t)place((uint32_t)(col0 + c), oct)] = w;
     };
     // Rows 2 t and 2 t + 1 of column c; with the last two the column is written.
     // A group of scale byte 255 has codes 0, and 0 times the infinity that byte stands for is NaN.
@@ -343,17 +246,18 @@ __global__ __launch_bounds__(256, 1) void weight_gradient_wide_kernel(WeightGrad
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int r = 2 * t + h;
-            v[h] = signed_byte<c & 3>(c < 4 ? x[set][r].x : x[set][r].y) * __uint_as_float(sc[set][r] << 23);
+            v[h] = signed_byte<c & 3>(x[set][r][c / 4]) * __uint_as_float(sc[set][r] << 23);
         }
         turned[t] = pack<T>(v[0], v[1]);
-        if (t == 3) lds[(2 + buf) * kBuf + kPad * 8 + place(cb * 8 + c, oct)] = turned;
+        if (t == 3) lds[(2 + buf) * kBuf + kPad * 8 + place(cb * C + c, oct)] = turned;
     };
 
-    // word of column (wave's first + 32 m + lane % 32), rows [16 s + 8 (lane / 32), ...): off[s ^ 2 (m & 1)] + 256 m
+    // The words of column (wave's first + 32 m + lane % 32), rows [16 s + 8 (lane / 32), ...).
     const uint32_t c32 = lane % 32, key = (lane / 32 ^ c32 ^ c32 >> 3) & 7;
-    const uint32_t at_o = kPad * 8 + (wave / 2 * 128 + c32) * 8, at_i = 2 * kBuf + kPad * 8 + (wave % 2 * 128 + c32) * 8;
-    Words4 a[2][4], b[2][4];
-    const auto read = [&](uint32_t buf, int s, int j) {    // one of the eight reads of quarter s
+    const uint32_t at_o = kPad * 8 + (wave / 2 * (16 * C) + c32) * 8;
+    const uint32_t at_i = 2 * kBuf + kPad * 8 + (wave % 2 * (16 * C) + c32) * 8;
+    Words4 a[2][M], b[2][M];
+    const auto read = [&](uint32_t buf, int s, int j) {    // one of the 2 M reads of quarter s
         const int m = j / 2;
         const uint32_t w = buf * kBuf + (key ^ (2 * (s ^ 2 * (m & 1)))) + m * 256;
         if (j & 1)
@@ -361,24 +265,33 @@ __global__ __launch_bounds__(256, 1) void weight_gradient_wide_kernel(WeightGrad
         else
             a[s & 1][m] = lds[at_o + w];
     };
-    Acc acc[4][4] = {};
+    Acc acc[M][M] = {};
 
-    // A quarter of a step: 16 matrix instructions, and after each a little of the
-    // other work, which the instruction's 32 cycles cover.  Quarters 0 and 1 unpack the next step's x,
-    // quarter 2 turns its dy, quarter 3 reads from the next step's LDS words, written by then.
+    // A quarter of a step: M x M matrix instructions, and after each a little of the other work, which the
+    // instruction's 32 cycles cover.  Quarters 0 and 1 unpack the next step's x, quarter 2 turns its dy,
+    // quarter 3 reads from the next step's LDS words, written by then; the next rows are
+    // asked for as soon as their registers are free.
     const auto quarter = [&](auto which, auto step, uint32_t t0) {
         constexpr int s = decltype(which)::value, buf = decltype(step)::value, set = buf ^ 1;
         const auto piece = [&](auto index) {
             constexpr int j = decltype(index)::value;
-            acc[j / 4][j % 4] = mfma<T>(a[s & 1][j / 4], b[s & 1][j % 4], acc[j / 4][j % 4]);
-            if constexpr (j < 8) read(s < 3 ? buf : buf ^ 1, (s + 1) & 3, j);
-            if constexpr (s < 2) unpack_x(set, buf ^ 1, Int<s * 4 + j / 4>{}, j % 4);
-            if constexpr (s == 2 && j < 8) write_dy(set, buf ^ 1, j);
-            if constexpr (s == 2 && j >= 8) fetch_x(set, t0 + 3 * kStep, j - 8);
-            if constexpr (s == 3 && j < 8) fetch_dy(set, t0 + 3 * kStep, j);
+            acc[j / M][j % M] = mfma<T>(a[s & 1][j / M], b[s & 1][j % M], acc[j / M][j % M]);
+            if constexpr (j < 2 * M) read(s < 3 ? buf : buf ^ 1, (s + 1) & 3, j);
+            if constexpr (s < 2) {
+                constexpr int kUnits = 2 * C / kPieces;    // of C columns of four, over two quarters
+                each<kUnits>([&](auto part) {
+                    constexpr int unit = s * 2 * C + j * kUnits + decltype(part)::value;
+                    unpack_x(set, buf ^ 1, Int<unit / 4>{}, unit % 4);
+                });
+            }
+            if constexpr (s == 2 && j < C) write_dy(set, buf ^ 1, t0 + kStep, j);
+            if constexpr (s == 2 && C == 8 && j >= 8) fetch_x(set, t0 + 3 * kStep, j - 8);
+            if constexpr (s == 2 && C == 4) each<2>([&](auto r) { fetch_x(set, t0 + 3 * kStep, 2 * j + decltype(r)::value); });
+            if constexpr (s == 3 && C == 8 && j < 8) fetch_dy(set, t0 + 3 * kStep, j);
+            if constexpr (s == 3 && C == 4) each<2>([&](auto r) { fetch_dy(set, t0 + 3 * kStep, 2 * j + decltype(r)::value); });
             __builtin_amdgcn_sched_barrier(0);
         };
-        each<16>(piece);
+        each<kPieces>(piece);
     };
     // Multiplies the step in LDS buffer `buf`, and writes the next one (set buf ^ 1) to the other.
     const auto step = [&](auto buf, uint32_t t0) {
@@ -390,49 +303,61 @@ __global__ __launch_bounds__(256, 1) void weight_gradient_wide_kernel(WeightGrad
     };
 
     if (begin < end) {
-        each<8>([&](auto r) {
-            fetch_x(0, begin, decltype(r)::value);
-            fetch_dy(0, begin, decltype(r)::value);
-        });
-        each<8>([&](auto r) {
-            fetch_x(1, begin + kStep, decltype(r)::value);
-            fetch_dy(1, begin + kStep, decltype(r)::value);
-        });
-        each<8>([&](auto c) {
-            write_dy(0, 0, decltype(c)::value);
+        const auto fetch = [&](int set, uint32_t t0) {
+            each<8>([&](auto r) {
+                fetch_x(set, t0, decltype(r)::value);
+                fetch_dy(set, t0, decltype(r)::value);
+            });
+        };
+        fetch(0, begin);
+        fetch(1, begin + kStep);
+        each<C>([&](auto c) {
+            write_dy(0, 0, begin, decltype(c)::value);
             each<4>([&](auto t) { unpack_x(0, 0, c, decltype(t)::value); });
         });
-        each<8>([&](auto r) {
-            fetch_x(0, begin + 2 * kStep, decltype(r)::value);
-            fetch_dy(0, begin + 2 * kStep, decltype(r)::value);
-        });
+        fetch(0, begin + 2 * kStep);
         __syncthreads();
-        each<8>([&](auto j) { read(0, 0, decltype(j)::value); });
+        each<2 * M>([&](auto j) { read(0, 0, decltype(j)::value); });
         for (uint32_t t0 = begin; t0 < end; t0 += 2 * kStep) {
             step(Int<0>{}, t0);
             step(Int<1>{}, t0 + kStep);    // all zeros after an odd number of steps
         }
     }
 
-    const uint64_t base = (uint64_t)range * g.out_width * g.in_width;
-    const uint32_t wo = wave / 2 * 128, wi = wave % 2 * 128;
-#pragma unroll
-    for (int m = 0; m < 4; ++m)
-#pragma unroll
-        for (int n = 0; n < 4; ++n) {
-            const uint32_t i = i0 + wi + n * 32 + lane % 32;
-            if (i >= g.in_width) continue;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const uint32_t o = o0 + wo + m * 32 + e / 4 * 8 + lane / 32 * 4 + e % 4;
-                if (o >= g.out_width) continue;
-                const uint64_t at = base + (uint64_t)o * g.in_width + i;
-                if (g.splits > 1)
-                    g.parts[split * g.size + at] = acc[m][n][e];
-                else
-                    put<G>((typename G::raw *)g.grad, at, acc[m][n][e], g.accumulate);
-            }
-        }
+    // Value e of a tile: row 8 (e / 4) + 4 (lane / 32) + e % 4, column lane % 32.  Rows and columns past the
+    // gradient's are dropped by the buffer's bounds.
+    const auto write = [&](auto type, void *to, bool add) {
+        using R = decltype(type);
+        constexpr uint32_t kSize = sizeof(typename R::raw);
+        const uint32_t row = g.in_width * kSize;
+        typename R::raw *base = (typename R::raw *)to + (uint64_t)range * g.out_width * g.in_width;
+        each<kPieces>([&](auto index) {
+            constexpr int m = decltype(index)::value / M, n = decltype(index)::value % M;
+            const uint32_t i = i0 + wave % 2 * (16 * C) + n * 32 + lane % 32;
+            const uint32_t at = i < g.in_width ? lane / 32 * 4 * row + i * kSize : kNowhere;
+            each<16>([&](auto element) {
+                constexpr int e = decltype(element)::value;
+                const uint32_t o = o0 + wave / 2 * (16 * C) + m * 32 + e / 4 * 8 + e % 4;
+                const uint32_t left = o < g.out_width ? min(g.out_width - o, 8u) : 0;
+                const Rsrc r = buffer(base + (uint64_t)(left ? o : 0) * g.in_width, left * row);
+                float v = acc[m][n][e];
+                if constexpr (kSize == 4) {
+                    if (add) v += __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0));
+                    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), r, at, 0, 0);
+                } else {
+                    if (add)
+                        v += R::up(__builtin_bit_cast(typename R::raw, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0)));
+                    __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, R::down(v)), r, at, 0, 0);
+                }
+            });
+        });
+    };
+    if (g.splits > 1)
+        write(F32{}, g.parts + unit.split * g.size, false);
+    else if (g.accumulate)
+        write(G{}, g.grad, true);
+    else
+        write(G{}, g.grad, false);
 }
 
 // Adds the splits' parts, in order.
@@ -440,9 +365,9 @@ template <class G>
 __global__ __launch_bounds__(kBlock) void weight_gradient_join_kernel(const float *parts, uint64_t size, uint32_t splits,
                                                                       uint32_t accumulate, typename G::raw *grad) {
     for (uint64_t i = (uint64_t)blockIdx.x * kBlock + threadIdx.x; i < size; i += (uint64_t)gridDim.x * kBlock) {
-        float sum = 0.0f;
+        float sum = accumulate ? G::up(grad[i]) : 0.0f;
         for (uint32_t s = 0; s < splits; ++s) sum += parts[s * size + i];
-        put<G>(grad, i, sum, accumulate);
+        grad[i] = G::down(sum);
     }
 }
 
@@ -503,9 +428,9 @@ int poseidon_weight_gradient(const void *dy, uint64_t dy_pitch, uint32_t type, u
                            poseidon_weight_gradient_workspace(rows, out_width, in_width, n_ranges)));
     const hipStream_t stream = (hipStream_t)hip_stream;
     WeightPlan p = weight_plan(rows, out_width, in_width, n_ranges);
-    // The wide kernel's buffer loads want whole words of dy.
-    const bool wide = p.large && aligned(dy, 4) && dy_pitch % 2 == 0 && out_width % 2 == 0 && out_width >= 8;
-    if (p.large && !wide) {
+    const bool whole = aligned(dy, 4) && dy_pitch % 2 == 0 && out_width % 2 == 0 && out_width >= 8;
+    if (p.large && !whole) {    // plain loads' addresses do not fit beside 256 sums
+        p.large = false;
         p.tiles_o = (uint32_t)((out_width + 127) / 128);
         p.tiles_i = (uint32_t)((in_width + 127) / 128);
     }
@@ -519,6 +444,7 @@ int poseidon_weight_gradient(const void *dy, uint64_t dy_pitch, uint32_t type, u
     g.codes = codes;
     g.scales = scales;
     g.offsets = offsets;
+    g.ranges = n_ranges;
     g.tiles_o = p.tiles_o;
     g.tiles_i = p.tiles_i;
     g.splits = p.splits;
@@ -529,8 +455,9 @@ int poseidon_weight_gradient(const void *dy, uint64_t dy_pitch, uint32_t type, u
     const uint32_t blocks = p.tiles_o * p.tiles_i * p.splits * n_ranges;
     const auto run = [&](auto t) {
         using D = decltype(t);
-        PL_TYPE(grad_type, if (wide) weight_gradient_wide_kernel<D, T><<<blocks, 256, 0, stream>>>(g);
-                else weight_gradient_kernel<D, T, 2, 2, 2, 2><<<blocks, 256, 0, stream>>>(g);
+        PL_TYPE(grad_type, if (p.large) weight_gradient_kernel<D, T, 8, true><<<blocks, 256, 0, stream>>>(g);
+                else if (whole) weight_gradient_kernel<D, T, 4, true><<<blocks, 256, 0, stream>>>(g);
+                else weight_gradient_kernel<D, T, 4, false><<<blocks, 256, 0, stream>>>(g);
                 if (p.splits > 1) {
                     const uint64_t n = (g.size + kBlock - 1) / kBlock;
                     weight_gradient_join_kernel<T><<<(uint32_t)(n < 4096 ? n : 4096), kBlock, 0, stream>>>(
