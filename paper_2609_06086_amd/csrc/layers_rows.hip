@@ -8,22 +8,22 @@ namespace pl {
 // ---- activations kept in 8 bits ----
 
 // Codes and scale bytes have no gaps, so a lane's slice is slice i of both.
-template <class T>
+template <class T, bool STREAM>
 __global__ __launch_bounds__(kBlock) void stash_kernel(const typename T::raw *x, uint64_t pitch, uint32_t total,
                                                        Div per_row, uint32_t width, int8_t *codes, uint8_t *scales) {
     const uint32_t i = blockIdx.x * kBlock + threadIdx.x;
     if (i >= total) return;    // whole groups of 8 lanes: total is a multiple of 8
     const uint32_t row = quotient(i, per_row), s = i - row * per_row.d;
     float v[8];
-    load_slice<T>(x + (uint64_t)row * pitch, s * kSlice, width, v);
+    load_slice<T, STREAM>(x + (uint64_t)row * pitch, s * kSlice, width, v);
     const uint32_t byte = scale_byte<T>(v);
     uint32_t w[2];
     codes_of(v, byte, w);
-    reinterpret_cast<uint2 *>(codes)[i] = make_uint2(w[0], w[1]);
+    store_codes<STREAM>(codes, i, w);
     if (!(i & 7)) scales[i >> 3] = (uint8_t)byte;
 }
 
-template <class T>
+template <class T, bool STREAM>
 __global__ __launch_bounds__(kBlock) void restore_kernel(const int8_t *codes, const uint8_t *scales, uint32_t total,
                                                          Div per_row, uint32_t width, typename T::raw *out,
                                                          uint64_t pitch) {
@@ -31,10 +31,10 @@ __global__ __launch_bounds__(kBlock) void restore_kernel(const int8_t *codes, co
     if (i >= total) return;
     const uint32_t row = quotient(i, per_row), s = i - row * per_row.d;
     uint32_t w[2];
-    load_codes(codes, i, w);
+    load_codes<STREAM>(codes, i, w);
     float v[8];
     values_of(w, scale_of(scales[i >> 3]), v);
-    store_slice<T>(out + (uint64_t)row * pitch, s * kSlice, width, v);
+    store_slice<T, STREAM>(out + (uint64_t)row * pitch, s * kSlice, width, v);
 }
 
 // ---- gated activation ----
@@ -49,7 +49,7 @@ __device__ __forceinline__ float sigmoid(float z) {
         return 1.0f / (1.0f + expf(-z));
 }
 
-template <class T, bool KEEP>
+template <class T, bool KEEP, bool STREAM>
 __global__ __launch_bounds__(kBlock) void gated_forward_kernel(
     const typename T::raw *gate, uint64_t gate_pitch, const typename T::raw *up, uint64_t up_pitch, uint32_t total,
     Div per_row, uint32_t width, typename T::raw *out, uint64_t out_pitch, int8_t *gate_codes, uint8_t *gate_scales,
@@ -58,18 +58,18 @@ __global__ __launch_bounds__(kBlock) void gated_forward_kernel(
     if (i >= total) return;
     const uint32_t row = quotient(i, per_row), s = i - row * per_row.d;
     float g[8], u[8], h[8];
-    load_slice<T>(gate + (uint64_t)row * gate_pitch, s * kSlice, width, g);
-    load_slice<T>(up + (uint64_t)row * up_pitch, s * kSlice, width, u);
+    load_slice<T, STREAM>(gate + (uint64_t)row * gate_pitch, s * kSlice, width, g);
+    load_slice<T, STREAM>(up + (uint64_t)row * up_pitch, s * kSlice, width, u);
 #pragma unroll
     for (int j = 0; j < 8; ++j) h[j] = g[j] * sigmoid<T>(g[j]) * u[j];
-    store_slice<T>(out + (uint64_t)row * out_pitch, s * kSlice, width, h);
+    store_slice<T, STREAM>(out + (uint64_t)row * out_pitch, s * kSlice, width, h);
     if constexpr (KEEP) {
         uint32_t w[2];
         const uint32_t bg = scale_byte<T>(g), bu = scale_byte<T>(u);
         codes_of(g, bg, w);
-        reinterpret_cast<uint2 *>(gate_codes)[i] = make_uint2(w[0], w[1]);
+        store_codes<STREAM>(gate_codes, i, w);
         codes_of(u, bu, w);
-        reinterpret_cast<uint2 *>(up_codes)[i] = make_uint2(w[0], w[1]);
+        store_codes<STREAM>(up_codes, i, w);
         if (!(i & 7)) {
             gate_scales[i >> 3] = (uint8_t)bg;
             up_scales[i >> 3] = (uint8_t)bu;
@@ -77,7 +77,7 @@ __global__ __launch_bounds__(kBlock) void gated_forward_kernel(
     }
 }
 
-template <class T>
+template <class T, bool STREAM>
 __global__ __launch_bounds__(kBlock) void gated_backward_kernel(
     const typename T::raw *dout, uint64_t dout_pitch, uint32_t total, Div per_row, uint32_t width,
     const int8_t *gate_codes, const uint8_t *gate_scales, const int8_t *up_codes, const uint8_t *up_scales,
@@ -86,11 +86,11 @@ __global__ __launch_bounds__(kBlock) void gated_backward_kernel(
     if (i >= total) return;
     const uint32_t row = quotient(i, per_row), s = i - row * per_row.d;
     uint32_t wg[2], wu[2];
-    load_codes(gate_codes, i, wg);
-    load_codes(up_codes, i, wu);
+    load_codes<STREAM>(gate_codes, i, wg);
+    load_codes<STREAM>(up_codes, i, wu);
     const float sg = scale_of(gate_scales[i >> 3]), su = scale_of(up_scales[i >> 3]);
     float d[8], g[8], u[8];
-    load_slice<T>(dout + (uint64_t)row * dout_pitch, s * kSlice, width, d);
+    load_slice<T, STREAM>(dout + (uint64_t)row * dout_pitch, s * kSlice, width, d);
     values_of(wg, sg, g);
     values_of(wu, su, u);
 #pragma unroll
@@ -100,8 +100,8 @@ __global__ __launch_bounds__(kBlock) void gated_backward_kernel(
         g[j] = ds * u[j] * slope;
         u[j] = for_up;
     }
-    store_slice<T>(dgate + (uint64_t)row * dgate_pitch, s * kSlice, width, g);
-    store_slice<T>(dup + (uint64_t)row * dup_pitch, s * kSlice, width, u);
+    store_slice<T, STREAM>(dgate + (uint64_t)row * dgate_pitch, s * kSlice, width, g);
+    store_slice<T, STREAM>(dup + (uint64_t)row * dup_pitch, s * kSlice, width, u);
 }
 
 // ---- experts ----
@@ -117,7 +117,8 @@ __device__ __forceinline__ void clear_rows(uint32_t wave, uint32_t waves, const 
         for (uint32_t s = lane; s < groups * 8; s += 64) {
             if constexpr (WRITE) store_slice<T>(out + r * width, s * kSlice, width, zero);
             if constexpr (KEEP) {
-                reinterpret_cast<uint2 *>(codes)[r * (groups * 8) + s] = make_uint2(0, 0);
+                const uint32_t none[2] = {};
+                store_codes<false>(codes, r * (groups * 8) + s, none);
                 if (!(s & 7)) scales[r * groups + (s >> 3)] = (uint8_t)T::kLow;
             }
         }
@@ -125,7 +126,7 @@ __device__ __forceinline__ void clear_rows(uint32_t wave, uint32_t waves, const 
 
 // A lane reads its slice of a token once and writes it to each of the token's
 // places; the rounding to 8 bits is done once too.  Blocks from `main` on clear the places past the last choice.
-template <class T, bool WRITE, bool KEEP>
+template <class T, bool WRITE, bool KEEP, bool STREAM>
 __global__ __launch_bounds__(kBlock) void gather_kernel(const typename T::raw *x, uint64_t pitch, uint32_t total,
                                                         Div per_row, uint32_t width, const int32_t *position,
                                                         uint32_t k, uint32_t main, const int32_t *n_kept,
@@ -141,7 +142,7 @@ __global__ __launch_bounds__(kBlock) void gather_kernel(const typename T::raw *x
     if (i >= total) return;
     const uint32_t row = quotient(i, per_row), s = i - row * per_row.d;
     float v[8];
-    load_slice<T>(x + (uint64_t)row * pitch, s * kSlice, width, v);
+    load_slice<T, STREAM>(x + (uint64_t)row * pitch, s * kSlice, width, v);
     uint32_t w[2] = {0, 0}, byte = 0;
     if constexpr (KEEP) {
         byte = scale_byte<T>(v);
@@ -151,35 +152,53 @@ __global__ __launch_bounds__(kBlock) void gather_kernel(const typename T::raw *x
     for (uint32_t j = 0; j < k; ++j) {
         const uint32_t p = (uint32_t)at[j];
         if (p >= places) continue;
-        if constexpr (WRITE) store_slice<T>(xs + (uint64_t)p * width, s * kSlice, width, v);
+        if constexpr (WRITE) store_slice<T, STREAM>(xs + (uint64_t)p * width, s * kSlice, width, v);
         if constexpr (KEEP) {
-            reinterpret_cast<uint2 *>(codes)[(uint64_t)p * per_row.d + s] = make_uint2(w[0], w[1]);
+            store_codes<STREAM>(codes, (uint64_t)p * per_row.d + s, w);
             if (!(s & 7)) scales[((uint64_t)p * per_row.d + s) >> 3] = (uint8_t)byte;
         }
     }
 }
 
-// A lane sums its slice over the token's places, in the order of the choices.
-template <class T>
+// A lane sums its slice over the token's places, in the order of the choices; the
+// rows of eight choices are asked for before the first is added.
+template <class T, bool STREAM>
 __global__ __launch_bounds__(kBlock) void combine_kernel(const typename T::raw *ys, uint32_t total, Div per_row,
                                                          uint32_t width, const int32_t *position, uint32_t k,
                                                          uint32_t places, const float *weights, typename T::raw *out,
                                                          uint64_t pitch) {
+    constexpr uint32_t kAhead = 2;
     const uint32_t i = blockIdx.x * kBlock + threadIdx.x;
     if (i >= total) return;
     const uint32_t row = quotient(i, per_row), s = i - row * per_row.d;
     const int32_t *at = position + (uint64_t)row * k;
     float sum[8] = {};
-    for (uint32_t j = 0; j < k; ++j) {
-        const uint32_t p = (uint32_t)at[j];
-        if (p >= places) continue;
-        const float w = weights ? weights[(uint64_t)row * k + j] : 1.0f;
-        float v[8];
-        load_slice<T>(ys + (uint64_t)p * width, s * kSlice, width, v);
+    for (uint32_t j0 = 0; j0 < k; j0 += kAhead) {
+        uint32_t p[kAhead];
+        float w[kAhead];
+        Slice<T> y[kAhead];
 #pragma unroll
-        for (int c = 0; c < 8; ++c) sum[c] = fmaf(w, v[c], sum[c]);
+        for (uint32_t j = 0; j < kAhead; ++j) {
+            if (j0 + j >= k) break;
+            p[j] = (uint32_t)at[j0 + j];
+            w[j] = weights ? weights[(uint64_t)row * k + j0 + j] : 1.0f;
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < kAhead; ++j) {
+            if (j0 + j >= k) break;
+            y[j] = load_words<T, STREAM>(ys + (uint64_t)(p[j] < places ? p[j] : 0) * width, s * kSlice, width);
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < kAhead; ++j) {
+            if (j0 + j >= k) break;
+            if (p[j] >= places) continue;
+            float v[8];
+            values<T>(y[j], v);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) sum[c] = fmaf(w[j], v[c], sum[c]);
+        }
     }
-    store_slice<T>(out + (uint64_t)row * pitch, s * kSlice, width, sum);
+    store_slice<T, STREAM>(out + (uint64_t)row * pitch, s * kSlice, width, sum);
 }
 
 __device__ __forceinline__ float wave_sum(float v) {
@@ -188,15 +207,16 @@ __device__ __forceinline__ float wave_sum(float v) {
     return v;
 }
 
-// A wave per token: dout's slices are read once for eight choices at a time, each
-// ys row is read once for its product with dout, and dys written beside it.
-template <class T>
+// A wave per token: each ys row is read once for its product with dout, and dys written
+// beside it; dout comes from memory for the first choice and from cache for the others.
+template <class T, bool STREAM>
 __global__ __launch_bounds__(kBlock) void combine_backward_kernel(const typename T::raw *dout, uint64_t pitch,
                                                                   const typename T::raw *ys, uint32_t tokens,
                                                                   uint32_t width, const int32_t *position, uint32_t k,
                                                                   uint32_t main, const int32_t *n_kept,
                                                                   uint32_t places, const float *weights,
                                                                   typename T::raw *dys, float *dweights) {
+    constexpr uint32_t kAhead = 4;    // slices of a row asked for at a time
     const uint32_t waves = kBlock / 64;
     if (blockIdx.x >= main) {
         clear_rows<T, true, false>((blockIdx.x - main) * waves + threadIdx.x / 64, (gridDim.x - main) * waves, n_kept,
@@ -211,16 +231,25 @@ __global__ __launch_bounds__(kBlock) void combine_backward_kernel(const typename
         const float w = weights[(uint64_t)t * k + j];
         float dot = 0.0f;
         if (p < places)
-            for (uint32_t c = lane * kSlice; c < width; c += 64 * kSlice) {
-                float v[8], y[8];
-                load_slice<T>(d, c, width, v);
-                load_slice<T>(ys + (uint64_t)p * width, c, width, y);
+            for (uint32_t c0 = lane * kSlice; c0 < width; c0 += kAhead * 64 * kSlice) {
+                Slice<T> dw[kAhead], yw[kAhead];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    dot = fmaf(v[e], y[e], dot);
-                    y[e] = w * v[e];
+                for (uint32_t a = 0; a < kAhead; ++a) {    // past the row: zeros
+                    dw[a] = load_words<T>(d, c0 + a * 64 * kSlice, width);
+                    yw[a] = load_words<T, STREAM>(ys + (uint64_t)p * width, c0 + a * 64 * kSlice, width);
                 }
-                store_slice<T>(dys + (uint64_t)p * width, c, width, y);
+#pragma unroll
+                for (uint32_t a = 0; a < kAhead; ++a) {
+                    float v[8], y[8];
+                    values<T>(dw[a], v);
+                    values<T>(yw[a], y);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        dot = fmaf(v[e], y[e], dot);
+                        y[e] = w * v[e];
+                    }
+                    store_slice<T, STREAM>(dys + (uint64_t)p * width, c0 + a * 64 * kSlice, width, y);
+                }
             }
         dot = wave_sum(dot);
         if (lane == 0) dweights[(uint64_t)t * k + j] = dot;
@@ -229,7 +258,7 @@ __global__ __launch_bounds__(kBlock) void combine_backward_kernel(const typename
 
 // ---- embedding ----
 
-template <class T>
+template <class T, bool STREAM>
 __global__ __launch_bounds__(kBlock) void embed_kernel(const int32_t *ids, uint32_t total, Div per_row, uint32_t width,
                                                        const typename T::raw *table, uint64_t table_pitch,
                                                        uint32_t vocab, float scale, typename T::raw *out,
@@ -244,7 +273,7 @@ __global__ __launch_bounds__(kBlock) void embed_kernel(const int32_t *ids, uint3
 #pragma unroll
         for (int c = 0; c < 8; ++c) v[c] *= scale;
     }
-    store_slice<T>(out + (uint64_t)row * pitch, s * kSlice, width, v);
+    store_slice<T, STREAM>(out + (uint64_t)row * pitch, s * kSlice, width, v);
 }
 
 inline uint32_t slices_of(uint64_t width) { return (uint32_t)((width + kSlice - 1) / kSlice); }
@@ -265,11 +294,11 @@ int poseidon_stash(const void *x, uint64_t pitch, uint32_t type, uint64_t rows, 
     PL_TRY(check_stash(codes, scales, rows));
     if (!rows) return POSEIDON_OK;
     const uint32_t per_row = padded_slices_of(width);
-    PL_TYPE(type, over_rows(rows, per_row, [&](uint64_t r, uint64_t, uint32_t n) {
-        stash_kernel<T><<<blocks_for(n), kBlock, 0, (hipStream_t)hip_stream>>>(
+    PL_STREAM(rows * width * (size_of(type) + 1), PL_TYPE(type, over_rows(rows, per_row, [&](uint64_t r, uint64_t, uint32_t n) {
+        stash_kernel<T, STREAM><<<blocks_for(n), kBlock, 0, (hipStream_t)hip_stream>>>(
             (const T::raw *)x + r * pitch, pitch, n, make_div(per_row), (uint32_t)width, codes + r * per_row * kSlice,
             scales + r * (per_row / 8));
-    }));
+    })));
     return launched();
 }
 
@@ -280,11 +309,11 @@ int poseidon_restore(const int8_t *codes, const uint8_t *scales, uint64_t rows, 
     PL_TRY(check_stash(codes, scales, rows));
     if (!rows) return POSEIDON_OK;
     const uint32_t per_row = padded_slices_of(width);
-    PL_TYPE(type, over_rows(rows, per_row, [&](uint64_t r, uint64_t, uint32_t n) {
-        restore_kernel<T><<<blocks_for(n), kBlock, 0, (hipStream_t)hip_stream>>>(
+    PL_STREAM(rows * width * (size_of(type) + 1), PL_TYPE(type, over_rows(rows, per_row, [&](uint64_t r, uint64_t, uint32_t n) {
+        restore_kernel<T, STREAM><<<blocks_for(n), kBlock, 0, (hipStream_t)hip_stream>>>(
             codes + r * per_row * kSlice, scales + r * (per_row / 8), n, make_div(per_row), (uint32_t)width,
             (T::raw *)out + r * out_pitch, out_pitch);
-    }));
+    })));
     return launched();
 }
 
@@ -313,7 +342,8 @@ int poseidon_gated_forward(const void *gate, uint64_t gate_pitch, const void *up
                 keep ? up_scales + b : nullptr);
         });
     };
-    PL_TYPE(type, keep ? run(gated_forward_kernel<T, true>, T{}) : run(gated_forward_kernel<T, false>, T{}));
+    PL_STREAM(rows * width * (3 * size_of(type) + 2), PL_TYPE(type, keep ? run(gated_forward_kernel<T, true, STREAM>, T{})
+                                                                         : run(gated_forward_kernel<T, false, STREAM>, T{})));
     return launched();
 }
 
@@ -329,13 +359,13 @@ int poseidon_gated_backward(const void *dout, uint64_t dout_pitch, uint32_t type
     PL_TRY(check_stash(up_codes, up_scales, rows));
     if (!rows) return POSEIDON_OK;
     const uint32_t per_row = padded_slices_of(width);
-    PL_TYPE(type, over_rows(rows, per_row, [&](uint64_t r, uint64_t, uint32_t n) {
+    PL_STREAM(rows * width * (3 * size_of(type) + 2), PL_TYPE(type, over_rows(rows, per_row, [&](uint64_t r, uint64_t, uint32_t n) {
         const uint64_t c = r * per_row * kSlice, b = r * (per_row / 8);
-        gated_backward_kernel<T><<<blocks_for(n), kBlock, 0, (hipStream_t)hip_stream>>>(
+        gated_backward_kernel<T, STREAM><<<blocks_for(n), kBlock, 0, (hipStream_t)hip_stream>>>(
             (const T::raw *)dout + r * dout_pitch, dout_pitch, n, make_div(per_row), (uint32_t)width, gate_codes + c,
             gate_scales + b, up_codes + c, up_scales + b, (T::raw *)dgate + r * dgate_pitch, dgate_pitch,
             (T::raw *)dup + r * dup_pitch, dup_pitch);
-    }));
+    })));
     return launched();
 }
 
@@ -362,9 +392,10 @@ int poseidon_expert_gather(const void *x, uint64_t pitch, uint32_t type, uint64_
                 position + r * k, k, blocks_for(n), n_kept, (uint32_t)places, (typename T::raw *)xs, codes, scales);
         });
     };
-    PL_TYPE(type, !keep ? run(gather_kernel<T, true, false>, T{})
-                  : xs  ? run(gather_kernel<T, true, true>, T{})
-                        : run(gather_kernel<T, false, true>, T{}));
+    PL_STREAM(places * width * ((xs ? size_of(type) : 0) + keep),
+              PL_TYPE(type, !keep ? run(gather_kernel<T, true, false, STREAM>, T{})
+                            : xs  ? run(gather_kernel<T, true, true, STREAM>, T{})
+                                  : run(gather_kernel<T, false, true, STREAM>, T{})));
     return launched();
 }
 
@@ -378,11 +409,11 @@ int poseidon_expert_combine(const void *ys, uint32_t type, uint64_t tokens, uint
     if (tokens && !position) return POSEIDON_E_INVAL;
     if (!tokens) return POSEIDON_OK;
     const uint32_t per_row = slices_of(width);
-    PL_TYPE(type, over_rows(tokens, per_row, [&](uint64_t r, uint64_t, uint32_t n) {
-        combine_kernel<T><<<blocks_for(n), kBlock, 0, (hipStream_t)hip_stream>>>(
+    PL_STREAM(tokens * (k + 1) * width * size_of(type), PL_TYPE(type, over_rows(tokens, per_row, [&](uint64_t r, uint64_t, uint32_t n) {
+        combine_kernel<T, STREAM><<<blocks_for(n), kBlock, 0, (hipStream_t)hip_stream>>>(
             (const T::raw *)ys, n, make_div(per_row), (uint32_t)width, position + r * k, k,
             (uint32_t)(tokens * k), weights ? weights + r * k : nullptr, (T::raw *)out + r * out_pitch, out_pitch);
-    }));
+    })));
     return launched();
 }
 
@@ -400,14 +431,14 @@ int poseidon_expert_combine_backward(const void *dout, uint64_t dout_pitch, cons
     if (tokens && (!position || !n_kept || !weights || !dweights)) return POSEIDON_E_INVAL;
     if (!tokens) return POSEIDON_OK;
     const uint64_t step = 1ull << 24;    // tokens of a launch
-    PL_TYPE(type, for (uint64_t t = 0; t < tokens; t += step) {
+    PL_STREAM(tokens * (2 * k + 1) * width * size_of(type), PL_TYPE(type, for (uint64_t t = 0; t < tokens; t += step) {
         const uint64_t n = tokens - t < step ? tokens - t : step;
         const uint32_t main = (uint32_t)((n + kBlock / 64 - 1) / (kBlock / 64));
-        combine_backward_kernel<T>
+        combine_backward_kernel<T, STREAM>
             <<<main + (t + n == tokens ? kClearBlocks : 0), kBlock, 0, (hipStream_t)hip_stream>>>(
                 (const T::raw *)dout + t * dout_pitch, dout_pitch, (const T::raw *)ys, (uint32_t)n, (uint32_t)width,
                 position + t * k, k, main, n_kept, (uint32_t)places, weights + t * k, (T::raw *)dys, dweights + t * k);
-    });
+    }));
     return launched();
 }
 
@@ -420,11 +451,11 @@ int poseidon_embed(const int32_t *ids, uint64_t tokens, const void *table, uint6
     if (tokens && !ids) return POSEIDON_E_INVAL;
     if (!tokens) return POSEIDON_OK;
     const uint32_t per_row = slices_of(width);
-    PL_TYPE(type, over_rows(tokens, per_row, [&](uint64_t r, uint64_t, uint32_t n) {
-        embed_kernel<T><<<blocks_for(n), kBlock, 0, (hipStream_t)hip_stream>>>(
+    PL_STREAM(tokens * width * 2 * size_of(type), PL_TYPE(type, over_rows(tokens, per_row, [&](uint64_t r, uint64_t, uint32_t n) {
+        embed_kernel<T, STREAM><<<blocks_for(n), kBlock, 0, (hipStream_t)hip_stream>>>(
             ids + r, n, make_div(per_row), (uint32_t)width, (const T::raw *)table, table_pitch, (uint32_t)vocab, scale,
             (T::raw *)out + r * out_pitch, out_pitch);
-    }));
+    })));
     return launched();
 }
 

@@ -27,15 +27,40 @@ struct SortPass {
     int32_t *order;            // the elements' indexes in their new order
     int32_t *position;         // null, or the new place of each element, -1 for key n_keys (single-pass sorts)
     int32_t *offsets;          // null, or the first place of each digit up to n_keys (single-pass sorts)
+    uint32_t passes;           // of a sort of one block, which runs them all in LDS
 };
+
+// Memory to fill with zeros beside a sort, which keeps few CUs busy: `rows` rows of `bytes` (an even number).
+struct Clear {
+    char *to;
+    uint64_t rows, bytes, pitch;
+};
+
+// Block `block`: a row, or of one row (a table without gaps) a piece of 16 bytes a thread.  Many blocks of one
+// store a thread fill at 6.7 TB/s, blocks that go on through the memory in strides at 4.4 to 5.6.
+__device__ __forceinline__ void clear(const Clear &c, uint32_t block) {
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    const bool flat = c.rows == 1;
+    const uint64_t step = (uint64_t)kSortThreads * 16;
+    char *row = c.to + (flat ? 0 : block * c.pitch);
+    for (uint64_t at = (flat ? block * step : 0) + threadIdx.x * 16u; at < c.bytes; at += step) {
+        if (at + 16 <= c.bytes) {
+            __builtin_memcpy(row + at, &zero, 16);
+        } else {
+            for (uint64_t i = at; i < c.bytes; i += 2) *(uint16_t *)(row + i) = 0;
+        }
+        if (flat) break;
+    }
+}
 
 __device__ __forceinline__ uint32_t key_at(const SortPass &p, uint32_t i) {
     const uint32_t k = (uint32_t)p.keys[i];
     return min(k, p.n_keys);
 }
 
-__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortPass p) {
+__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortPass p, Clear c) {
     __shared__ uint32_t count[kMaxBins];
+    if (blockIdx.x >= p.blocks) return clear(c, blockIdx.x - p.blocks);
     for (uint32_t b = threadIdx.x; b < p.bins; b += kSortThreads) count[b] = 0;
     __syncthreads();
     const uint32_t first = blockIdx.x * kSortTile;
@@ -87,77 +112,106 @@ __device__ __forceinline__ uint32_t block_prefix(uint32_t v, uint32_t *wave_sums
     return before + s - v;
 }
 
-__global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortPass p) {
+// A pass.  SOLO: all of the elements are in one block, which runs every pass and
+// passes keys and indexes on through LDS.
+template <bool SOLO>
+__global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortPass p, Clear c) {
     __shared__ uint32_t count[kSortWaves][kMaxBins];
     __shared__ uint32_t wave_sums[kSortWaves];
+    __shared__ uint32_t moved[SOLO ? 2 : 1][SOLO ? kSortTile : 1];
+    if (blockIdx.x >= p.blocks) return clear(c, blockIdx.x - p.blocks);
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
-    for (uint32_t b = tid; b < kSortWaves * kMaxBins; b += kSortThreads) (&count[0][0])[b] = 0;
-    __syncthreads();
-
-    // ranks within the wave's 512 elements
     const uint32_t first = blockIdx.x * kSortTile + wave * (64 * kSortRounds);
-    uint32_t key[kSortRounds], rank[kSortRounds];
+    const uint32_t rounds = first < p.m ? min((p.m - first + 63) / 64, kSortRounds) : 0;    // of this wave
     const uint64_t below = (1ull << lane) - 1;
+    uint32_t key[kSortRounds], index[kSortRounds];
 #pragma unroll
     for (uint32_t r = 0; r < kSortRounds; ++r) {
         const uint32_t i = first + r * 64 + lane;
         key[r] = i < p.m ? key_at(p, i) : 0xffffffffu;
+        index[r] = i < p.m && p.from ? (uint32_t)p.from[i] : i;
     }
-    volatile uint32_t *mine = count[wave];
-#pragma unroll
-    for (uint32_t r = 0; r < kSortRounds; ++r) {
-        const bool on = first + r * 64 + lane < p.m;
-        const uint32_t digit = (key[r] >> p.shift) & (p.bins - 1);
-        uint64_t same = __ballot(on);
-        for (uint32_t b = 0; b < p.bits; ++b) {
-            const uint64_t set = __ballot((digit >> b) & 1);
-            same &= (digit >> b) & 1 ? set : ~set;
-        }
-        const uint32_t old = mine[digit];
-        const uint32_t before = (uint32_t)__popcll(same & below);
-        rank[r] = old + before;
-        __builtin_amdgcn_wave_barrier();
-        if (on && before == 0) mine[digit] = old + (uint32_t)__popcll(same);
-        __builtin_amdgcn_wave_barrier();
-    }
-    __syncthreads();
+    for (uint32_t pass = 0; pass < (SOLO ? p.passes : 1u); ++pass) {
+        const uint32_t shift = SOLO ? pass * p.bits : p.shift;
+        const bool last = !SOLO || pass + 1 == p.passes;
+        for (uint32_t w = 0; w < kSortWaves; ++w)
+            if (tid < p.bins) count[w][tid] = 0;
+        __syncthreads();
 
-    // a bin a thread: where the block's elements of this digit begin
-    uint32_t before = 0, total = 0;
-    if (tid < p.bins) {
-        if (p.blocks == 1) {
-            for (uint32_t w = 0; w < kSortWaves; ++w) total += count[w][tid];
-        } else if (p.totals) {
-            before = p.counts[blockIdx.x * p.bins + tid];
-            total = p.totals[tid];
-        } else {
-            for (uint32_t b = 0; b < p.blocks; ++b) {
-                const uint32_t c = p.counts[b * p.bins + tid];
-                before += b < blockIdx.x ? c : 0u;
-                total += c;
+        // ranks within the wave's 512 elements
+        uint32_t rank[kSortRounds];
+        volatile uint32_t *mine = count[wave];
+#pragma unroll
+        for (uint32_t r = 0; r < kSortRounds; ++r) {
+            if (r >= rounds) break;
+            const bool on = first + r * 64 + lane < p.m;
+            const uint32_t digit = (key[r] >> shift) & (p.bins - 1);
+            uint64_t same = __ballot(on);
+            for (uint32_t b = 0; b < p.bits; ++b) {
+                const uint64_t set = __ballot((digit >> b) & 1);
+                same &= (digit >> b) & 1 ? set : ~set;
+            }
+            const uint32_t old = mine[digit];
+            const uint32_t before = (uint32_t)__popcll(same & below);
+            rank[r] = old + before;
+            __builtin_amdgcn_wave_barrier();
+            if (on && before == 0) mine[digit] = old + (uint32_t)__popcll(same);
+            __builtin_amdgcn_wave_barrier();
+        }
+        __syncthreads();
+
+        // a bin a thread: where the block's elements of this digit begin
+        uint32_t before = 0, total = 0;
+        if (tid < p.bins) {
+            if (p.blocks == 1) {
+#pragma unroll
+                for (uint32_t w = 0; w < kSortWaves; ++w) total += count[w][tid];
+            } else if (p.totals) {
+                before = p.counts[blockIdx.x * p.bins + tid];
+                total = p.totals[tid];
+            } else {
+                for (uint32_t b = 0; b < p.blocks; ++b) {
+                    const uint32_t n = p.counts[b * p.bins + tid];
+                    before += b < blockIdx.x ? n : 0u;
+                    total += n;
+                }
             }
         }
-    }
-    const uint32_t start = block_prefix(total, wave_sums);
-    if (tid < p.bins) {
-        if (p.offsets && blockIdx.x == 0 && tid <= p.n_keys) p.offsets[tid] = (int32_t)start;
-        uint32_t at = start + before;
-        for (uint32_t w = 0; w < kSortWaves; ++w) {
-            const uint32_t c = count[w][tid];
-            count[w][tid] = at;
-            at += c;
-        }
-    }
-    __syncthreads();
+        const uint32_t start = block_prefix(total, wave_sums);
+        if (tid < p.bins) {
+            if (p.offsets && blockIdx.x == 0 && tid <= p.n_keys) p.offsets[tid] = (int32_t)start;
+            uint32_t at = start + before;
 #pragma unroll
-    for (uint32_t r = 0; r < kSortRounds; ++r) {
-        const uint32_t i = first + r * 64 + lane;
-        if (i >= p.m) continue;
-        const uint32_t to = count[wave][(key[r] >> p.shift) & (p.bins - 1)] + rank[r];
-        const int32_t index = p.from ? p.from[i] : (int32_t)i;
-        p.order[to] = index;
-        if (p.keys_out) p.keys_out[to] = (int32_t)key[r];
-        if (p.position) p.position[i] = key[r] < p.n_keys ? (int32_t)to : -1;
+            for (uint32_t w = 0; w < kSortWaves; ++w) {
+                const uint32_t n = count[w][tid];
+                count[w][tid] = at;
+                at += n;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (uint32_t r = 0; r < kSortRounds; ++r) {
+            const uint32_t i = first + r * 64 + lane;
+            if (r >= rounds || i >= p.m) continue;
+            const uint32_t to = count[wave][(key[r] >> shift) & (p.bins - 1)] + rank[r];
+            if (!last) {
+                moved[0][to] = key[r];
+                moved[SOLO][to] = index[r];
+                continue;
+            }
+            p.order[to] = (int32_t)index[r];
+            if (p.keys_out) p.keys_out[to] = (int32_t)key[r];
+            if (p.position) p.position[i] = key[r] < p.n_keys ? (int32_t)to : -1;
+        }
+        if (last) break;
+        __syncthreads();
+#pragma unroll
+        for (uint32_t r = 0; r < kSortRounds; ++r) {
+            const uint32_t i = first + r * 64 + lane;
+            if (r >= rounds || i >= p.m) continue;
+            key[r] = moved[0][i];
+            index[r] = moved[SOLO][i];
+        }
     }
 }
 
@@ -166,18 +220,64 @@ inline uint64_t round_up(uint64_t v, uint64_t to) { return (v + to - 1) / to * t
 // counts, then totals
 inline uint64_t sort_counts_bytes(uint64_t m) { return round_up(((uint64_t)sort_blocks(m) + 1) * kMaxBins * 4, 256); }
 
-inline void run_pass(SortPass p, hipStream_t stream) {
+// Blocks that clear beside a sort's, and part i of n of a clear.
+inline uint32_t clear_blocks(const Clear &c) {
+    const uint64_t step = (uint64_t)kSortThreads * 16;
+    return (uint32_t)(c.rows == 1 ? (c.bytes + step - 1) / step : c.rows);
+}
+inline Clear part_of(const Clear &c, uint64_t i, uint64_t n) {
+    Clear p = c;
+    if (c.rows == 1) {
+        const uint64_t units = c.bytes / 256, from = units * i / n * 256;
+        p.to += from;
+        p.bytes = (i + 1 == n ? c.bytes : units * (i + 1) / n * 256) - from;
+    } else {
+        const uint64_t from = c.rows * i / n;
+        p.to += from * c.pitch;
+        p.rows = c.rows * (i + 1) / n - from;
+    }
+    return p;
+}
+
+// Passes of `bits` bits over p.keys, with the clear spread over their launches.  lists: where passes but
+// the last leave keys and indexes, and the last one its keys.
+struct SortLists {
+    int32_t *keys[2], *order[2];
+};
+
+inline void sort(SortPass p, const SortLists &lists, const Clear &c, hipStream_t stream) {
+    if (p.blocks == 1) {
+        sort_place_kernel<true><<<1 + clear_blocks(c), kSortThreads, 0, stream>>>(p, c);
+        return;
+    }
     const bool scan = p.blocks > kSelfScan;
-    if (!scan) p.totals = nullptr;
-    if (p.blocks > 1) sort_count_kernel<<<p.blocks, kSortThreads, 0, stream>>>(p);
-    if (scan) sort_scan_kernel<<<p.bins, 256, 0, stream>>>(p);
-    sort_place_kernel<<<p.blocks, kSortThreads, 0, stream>>>(p);
+    uint32_t *const totals = p.counts + (uint64_t)p.blocks * p.bins;
+    p.totals = scan ? totals : nullptr;
+    int32_t *const order = p.order, *const keys = p.keys_out;
+    for (uint32_t i = 0; i < p.passes; ++i) {
+        const bool last = i + 1 == p.passes;
+        if (i) {
+            p.keys = lists.keys[(i - 1) & 1];
+            p.from = lists.order[(i - 1) & 1];
+        }
+        p.keys_out = last ? keys : lists.keys[i & 1];
+        p.order = last ? order : lists.order[i & 1];
+        p.shift = i * p.bits;
+        const Clear a = part_of(c, 2 * i, 2 * p.passes), b = part_of(c, 2 * i + 1, 2 * p.passes);
+        sort_count_kernel<<<p.blocks + clear_blocks(a), kSortThreads, 0, stream>>>(p, a);
+        if (scan) {
+            SortPass q = p;
+            q.totals = totals;
+            sort_scan_kernel<<<p.bins, 256, 0, stream>>>(q);
+        }
+        sort_place_kernel<false><<<p.blocks + clear_blocks(b), kSortThreads, 0, stream>>>(p, b);
+    }
 }
 
 // ---- gradient of an embedding ----
 
 // Sorted places in chunks of `chunk`; a block takes one chunk and 512 columns
-// (64 lanes of 8).  It adds the rows of dout in sorted order and writes the sum
+// (64 lanes of 8).  Eight rows of dout are on their way while eight are added, in sorted order; it writes the sum
 // of every token whose places all lie in the chunk.  A token that comes from the chunk
 // before leaves its part in slot 0 of the chunk, one that only goes on into the
 // next chunk in slot 1; embed_join_kernel adds those up in order.
@@ -203,56 +303,66 @@ __device__ __forceinline__ void write_sum(const EmbedGrad &e, uint32_t key, uint
     store_slice<G>(row, col, e.width, v);
 }
 
-template <class T, class G>
+template <class T, class G, bool STREAM>
 __global__ __launch_bounds__(64) void embed_sum_kernel(EmbedGrad e) {
-    const uint32_t chunk = blockIdx.x, col = (blockIdx.y * 64 + threadIdx.x) * kSlice;
+    constexpr uint32_t kAhead = 8;    // rows asked for at a time
+    const uint32_t lane = threadIdx.x, chunk = blockIdx.x, col = (blockIdx.y * 64 + lane) * kSlice;
     const uint32_t lo = chunk * e.chunk, hi = min(lo + e.chunk, e.m);
-    if (col >= e.width) return;
     const typename T::raw *dout = (const typename T::raw *)e.dout;
+    const uint32_t before = lo > 0 ? (uint32_t)e.keys[lo - 1] : e.vocab, after = hi < e.m ? (uint32_t)e.keys[hi] : e.vocab;
+    float *parts = e.parts + (uint64_t)chunk * 2 * e.padded + col;
+    const bool inside = col < e.width;
     float sum[8] = {};
-    uint32_t begin = lo, key = (uint32_t)e.keys[lo];
-    for (uint32_t a = lo; a < hi; a += 8) {
-        float v[8][8];
-        uint32_t keys[8];
+    uint32_t key = (uint32_t)__builtin_amdgcn_readfirstlane(e.keys[lo]);
+    bool from = before == key;    // the token comes from the chunk before
+    const auto flush = [&](bool on) {
+        if (key < e.vocab && inside) {
+            if (from || on) {
+                float *part = parts + (from ? 0 : e.padded);
 #pragma unroll
-        for (uint32_t j = 0; j < 8; ++j) {
-            const uint32_t at = min(a + j, hi - 1);
-            keys[j] = (uint32_t)e.keys[at];
-            load_slice<T>(dout + (uint64_t)(uint32_t)e.order[at] * e.dout_pitch, col, e.width, v[j]);
-        }
-#pragma unroll
-        for (uint32_t j = 0; j < 8; ++j) {
-            const uint32_t at = a + j;
-            if (at >= hi) break;
-            if (keys[j] != key) {          // the token before ends here, within the chunk
-                if (key < e.vocab) {
-                    if (begin == lo && lo > 0 && (uint32_t)e.keys[lo - 1] == key) {
-                        float *part = e.parts + (uint64_t)chunk * 2 * e.padded + col;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) part[i] = sum[i];
-                    } else {
-                        write_sum<G>(e, key, col, sum);
-                    }
-                }
-                begin = at;
-                key = keys[j];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
+                for (int i = 0; i < 8; ++i) part[i] = sum[i];
+            } else {
+                write_sum<G>(e, key, col, sum);
             }
+        }
+        from = false;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum[i] += v[j][i];
+        for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
+    };
+    for (uint32_t a = lo; a < hi; a += 64) {    // a lane holds one of 64 places
+        const uint32_t here = min(a + lane, hi - 1);
+        const int32_t keys = e.keys[here], rows = e.order[here];
+        const uint32_t n = min(hi - a, 64u);
+        Slice<T> next[kAhead];
+        const auto fetch = [&](uint32_t first) {
+#pragma unroll
+            for (uint32_t j = 0; j < kAhead; ++j) {
+                const uint32_t row = (uint32_t)__builtin_amdgcn_readlane(rows, min(first + j, n - 1));
+                next[j] = load_words<T, STREAM>(dout + (uint64_t)row * e.dout_pitch, col, e.width);
+            }
+        };
+        fetch(0);
+        for (uint32_t first = 0; first < n; first += kAhead) {
+            Slice<T> now[kAhead];
+#pragma unroll
+            for (uint32_t j = 0; j < kAhead; ++j) now[j] = next[j];
+            if (first + kAhead < n) fetch(first + kAhead);
+#pragma unroll
+            for (uint32_t j = 0; j < kAhead; ++j) {
+                if (first + j >= n) break;
+                const uint32_t k = (uint32_t)__builtin_amdgcn_readlane(keys, first + j);
+                if (k != key) {
+                    flush(false);
+                    key = k;
+                }
+                float v[8];
+                values<T>(now[j], v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum[i] += v[i];
+            }
         }
     }
-    if (key >= e.vocab) return;
-    const bool from = begin == lo && lo > 0 && (uint32_t)e.keys[lo - 1] == key;
-    const bool on = hi < e.m && (uint32_t)e.keys[hi] == key;
-    if (from || on) {
-        float *part = e.parts + ((uint64_t)chunk * 2 + (from ? 0 : 1)) * e.padded + col;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) part[i] = sum[i];
-    } else {
-        write_sum<G>(e, key, col, sum);
-    }
+    flush(after == key);
 }
 
 // A block of four waves per chunk and 512 columns; it has work where a token
@@ -295,16 +405,6 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedGrad e) {
         for (int i = 0; i < 8; ++i) sum[i] += share[w][lane][i];
     }
     write_sum<G>(e, key, col, sum);
-}
-
-template <class G>
-__global__ __launch_bounds__(kBlock) void clear_kernel(typename G::raw *out, uint64_t pitch, uint32_t total,
-                                                       Div per_row, uint32_t width) {
-    const uint32_t i = blockIdx.x * kBlock + threadIdx.x;
-    if (i >= total) return;
-    const uint32_t row = quotient(i, per_row), s = i - row * per_row.d;
-    const float zero[8] = {};
-    store_slice<G>(out + (uint64_t)row * pitch, s * kSlice, width, zero);
 }
 
 // Places a block adds up: few tokens are spread over more blocks.
@@ -358,12 +458,12 @@ int poseidon_expert_sort(const int32_t *choice, uint64_t tokens, uint32_t k, uin
     while ((1u << p.bits) < n_experts + 1) ++p.bits;
     p.bins = 1u << p.bits;
     p.blocks = m ? sort_blocks(m) : 1;    // no choices: one block writes the offsets
+    p.passes = 1;
     p.counts = (uint32_t *)workspace;
-    p.totals = p.counts + (uint64_t)p.blocks * p.bins;
     p.order = order;
     p.position = position;
     p.offsets = offsets;
-    run_pass(p, (hipStream_t)hip_stream);
+    sort(p, {}, {}, (hipStream_t)hip_stream);
     return launched();
 }
 
@@ -384,36 +484,38 @@ int poseidon_embed_backward(const int32_t *ids, uint64_t tokens, const void *dou
     PL_TRY(check_workspace(workspace, workspace_bytes, poseidon_embed_backward_workspace(tokens, vocab, width)));
     const hipStream_t stream = (hipStream_t)hip_stream;
     const uint32_t slices = (uint32_t)((width + kSlice - 1) / kSlice);
-    if (!accumulate)
-        PL_TYPE(dtable_type, over_rows(vocab, slices, [&](uint64_t r, uint64_t, uint32_t n) {
-            clear_kernel<T><<<blocks_for(n), kBlock, 0, stream>>>((T::raw *)dtable + r * dtable_pitch, dtable_pitch, n,
-                                                                  make_div(slices), (uint32_t)width);
-        }));
-    if (!vocab) return POSEIDON_OK;
-    if (!tokens) return accumulate ? POSEIDON_OK : launched();
+    if (!vocab || (!tokens && accumulate)) return POSEIDON_OK;
+    const uint64_t size = size_of(dtable_type);
+    Clear c = {(char *)dtable, vocab, width * size, dtable_pitch * size};
+    if (accumulate) c.rows = 0;
+    if (c.rows && dtable_pitch == width) {
+        c.bytes *= c.rows;
+        c.rows = 1;
+    }
 
     const uint32_t m = (uint32_t)tokens;
     const EmbedWorkspace w = embed_workspace(tokens, width);
     char *base = (char *)workspace;
     uint32_t bits = 1;
     while ((1u << bits) < vocab + 1) ++bits;
-    const uint32_t passes = (bits + kMaxBits - 1) / kMaxBits, each = (bits + passes - 1) / passes;
     SortPass p = {};
+    p.keys = ids;
     p.m = m;
     p.n_keys = (uint32_t)vocab;
-    p.bits = each;
-    p.bins = 1u << each;
-    p.blocks = sort_blocks(m);
+    p.passes = (bits + kMaxBits - 1) / kMaxBits;
+    p.bits = (bits + p.passes - 1) / p.passes;
+    p.bins = 1u << p.bits;
+    p.blocks = m ? sort_blocks(m) : 1;
     p.counts = (uint32_t *)(base + w.counts);
-    for (uint32_t i = 0; i < passes; ++i) {
-        p.totals = p.counts + (uint64_t)p.blocks * p.bins;
-        p.keys = i ? (const int32_t *)(base + w.keys[(i - 1) & 1]) : ids;
-        p.from = i ? (const int32_t *)(base + w.order[(i - 1) & 1]) : nullptr;
-        p.keys_out = (int32_t *)(base + w.keys[i & 1]);
-        p.order = (int32_t *)(base + w.order[i & 1]);
-        p.shift = i * each;
-        run_pass(p, stream);
+    SortLists lists;
+    for (uint32_t i = 0; i < 2; ++i) {
+        lists.keys[i] = (int32_t *)(base + w.keys[i]);
+        lists.order[i] = (int32_t *)(base + w.order[i]);
     }
+    p.keys_out = lists.keys[(p.passes - 1) & 1];
+    p.order = lists.order[(p.passes - 1) & 1];
+    sort(p, lists, c, stream);
+    if (!m) return launched();
 
     EmbedGrad e = {};
     e.keys = p.keys_out;
@@ -434,8 +536,8 @@ int poseidon_embed_backward(const int32_t *ids, uint64_t tokens, const void *dou
     const dim3 grid(e.chunks, (slices + 63) / 64);
     const auto run = [&](auto t) {
         using D = decltype(t);
-        PL_TYPE(dtable_type, embed_sum_kernel<D, T><<<grid, 64, 0, stream>>>(e);
-                if (e.chunks > 1) embed_join_kernel<T><<<grid, 256, 0, stream>>>(e));
+        PL_STREAM(tokens * width * size_of(type), PL_TYPE(dtable_type, embed_sum_kernel<D, T, STREAM><<<grid, 64, 0, stream>>>(e);
+                                                          if (e.chunks > 1) embed_join_kernel<T><<<grid, 256, 0, stream>>>(e)));
     };
     PL_TYPE(type, run(T{}));
     return launched();

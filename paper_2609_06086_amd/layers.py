@@ -45,20 +45,25 @@ _ARGS = {
 }
 EXPORTS = tuple(_ARGS)
 
-_lib = None
+_functions = {}
 
 
 def lib():
     """The loaded HIP library, with the layer operators' signatures."""
-    global _lib
-    if _lib is None:
-        L = P.lib()
+    L = P.lib()
+    if not _functions:
         for name, args in _ARGS.items():
             f = getattr(L, name)
             f.argtypes = args
             f.restype = _u64 if name.endswith("_workspace") else C.c_int
-        _lib = L
-    return _lib
+            _functions[name] = f
+    return L
+
+
+def _function(name: str):
+    if not _functions:
+        lib()
+    return _functions[name]
 
 
 @dataclass
@@ -115,20 +120,19 @@ def _streamed(f):
 
 def _call(name: str, device: torch.device, *args):
     """Calls the library on torch's current stream of `device`; raises what it refuses."""
-    f = getattr(lib(), name)
-    stream = torch.cuda.current_stream(device).cuda_stream
-    if torch.cuda.current_device() == device.index:
-        rc = f(*args, stream)
+    index = device.index
+    if torch._C._cuda_getDevice() == index:
+        rc = _function(name)(*args, torch._C._cuda_getCurrentRawStream(index))
     else:
         with torch.cuda.device(device):
-            rc = f(*args, stream)
+            rc = _function(name)(*args, torch._C._cuda_getCurrentRawStream(index))
     if rc != P.POSEIDON_OK:
         raise PoseidonError(rc, name)
 
 
 def _workspace(name: str, device: torch.device, *sizes):
     """(tensor or None, address, bytes) of the workspace that the sizes need."""
-    n = getattr(lib(), name + "_workspace")(*sizes)
+    n = _function(name + "_workspace")(*sizes)
     if n == 2 ** 64 - 1:
         raise PoseidonError(P.POSEIDON_E_RANGE, name)
     if not n:
@@ -142,7 +146,7 @@ def _rows(x, where: str, device=None, dtype=None, shape=None) -> torch.Tensor:
     if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dim() != 2 or x.dtype not in TYPES:
         _refuse(f"{where}: not a 2-D float32, float16 or bfloat16 tensor on the GPU")
     if (device is not None and x.device != device) or (dtype is not None and x.dtype != dtype) or \
-            (shape is not None and tuple(x.shape) != tuple(shape)):
+            (shape is not None and x.shape != shape):
         _refuse(f"{where}: device, type or shape differs from what the others ask for")
     return x if _pitched(x) else x.contiguous()
 
@@ -161,7 +165,7 @@ def _out(out, where: str, device, dtype, shape) -> torch.Tensor:
     if out is None:
         return torch.empty(shape, dtype=dtype, device=device)
     if not isinstance(out, torch.Tensor) or out.device != device or out.dtype != dtype or \
-            tuple(out.shape) != tuple(shape) or not (_pitched(out) if out.dim() == 2 else out.is_contiguous()):
+            out.shape != shape or not (_pitched(out) if out.dim() == 2 else out.is_contiguous()):
         _refuse(f"{where}: device, type, shape or layout differs from the result's")
     return out
 
@@ -169,9 +173,9 @@ def _out(out, where: str, device, dtype, shape) -> torch.Tensor:
 def _whole(x, where: str, device, dtype, shape) -> torch.Tensor:
     """An operand without gaps (copied if it has some)."""
     if not isinstance(x, torch.Tensor) or x.device != device or x.dtype != dtype or \
-            (shape is not None and tuple(x.shape) != tuple(shape)):
+            (shape is not None and x.shape != shape):
         _refuse(f"{where}: not a {dtype} tensor of shape {shape} on {device}")
-    return x.contiguous()
+    return x if x.is_contiguous() else x.contiguous()
 
 
 def _groups(width: int) -> int:
@@ -185,12 +189,13 @@ def _new_stash(rows: int, width: int, dtype, device) -> Stash:
 
 
 def _stash(s, where: str, device, rows=None, width=None) -> Stash:
-    if not isinstance(s, Stash) or s.scales.dim() != 2 or (rows is not None and s.rows != rows) or \
+    if not isinstance(s, Stash) or s.scales.dim() != 2 or (rows is not None and s.scales.shape[0] != rows) or \
             (width is not None and s.width != width):
         _refuse(f"{where}: not a Stash of these sizes")
-    n, g = s.rows, _groups(s.width)
-    return Stash(_whole(s.codes, where, device, torch.int8, (n, g * GROUP)),
-                 _whole(s.scales, where, device, torch.uint8, (n, g)), s.width, s.dtype)
+    n, g = s.scales.shape[0], _groups(s.width)
+    codes = _whole(s.codes, where, device, torch.int8, (n, g * GROUP))
+    scales = _whole(s.scales, where, device, torch.uint8, (n, g))
+    return s if codes is s.codes and scales is s.scales else Stash(codes, scales, s.width, s.dtype)
 
 
 # ---- activations kept in 8 bits ----
