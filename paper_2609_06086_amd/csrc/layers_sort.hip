@@ -277,7 +277,7 @@ inline void sort(SortPass p, const SortLists &lists, const Clear &c, hipStream_t
 // ---- gradient of an embedding ----
 
 // Sorted places in chunks of `chunk`; a block takes one chunk and 512 columns
-// (64 lanes of 8).  Eight rows of dout are on their way while eight are added, in sorted order; it writes the sum
+// (64 lanes of 8).  Four rows of dout are on their way while four are added, in sorted order; it writes the sum
 // of every token whose places all lie in the chunk.  A token that comes from the chunk
 // before leaves its part in slot 0 of the chunk, one that only goes on into the
 // next chunk in slot 1; embed_join_kernel adds those up in order.
@@ -305,7 +305,7 @@ __device__ __forceinline__ void write_sum(const EmbedGrad &e, uint32_t key, uint
 
 template <class T, class G, bool STREAM>
 __global__ __launch_bounds__(64) void embed_sum_kernel(EmbedGrad e) {
-    constexpr uint32_t kAhead = 8;    // rows asked for at a time
+    constexpr uint32_t kAhead = 4;    // rows asked for at a time
     const uint32_t lane = threadIdx.x, chunk = blockIdx.x, col = (blockIdx.y * 64 + lane) * kSlice;
     const uint32_t lo = chunk * e.chunk, hi = min(lo + e.chunk, e.m);
     const typename T::raw *dout = (const typename T::raw *)e.dout;

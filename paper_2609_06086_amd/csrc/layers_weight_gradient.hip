@@ -20,8 +20,7 @@ using HalfVec = _Float16 __attribute__((ext_vector_type(8)));
 using BrainVec = __bf16 __attribute__((ext_vector_type(8)));
 using Words4 = uint32_t __attribute__((ext_vector_type(4)));
 
-constexpr uint32_t kStep = 64;       // rows of a step
-constexpr uint32_t kRanked = 256;    // up to so many ranges are taken by length
+constexpr uint32_t kStep = 64;    // rows of a step
 
 template <class T>
 __device__ __forceinline__ Acc mfma(Words4 a, Words4 b, Acc c);
@@ -48,17 +47,36 @@ __device__ __forceinline__ uint32_t pack<F16>(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(lo, hi));
 }
 
+constexpr uint32_t kNone = 0xffffffffu;
+
+// A run of a range's rows that a block takes, and where its sums go: a slot of
+// the workspace, or kNone: the gradient itself.
+struct Run {
+    uint32_t range, begin, end, slot;
+};
+// A range that was split: its slots are added up at the end.
+struct Split {
+    uint32_t range, slot, runs;
+};
+// What weight_plan_kernel makes of the offsets.
+struct RunTable {
+    uint32_t runs, splits;
+};
+
 struct WeightGrad {
     const void *dy;
     uint64_t dy_pitch;
     uint32_t rows, out_width, in_width, groups;
     const int8_t *codes;
     const uint8_t *scales;
-    const int32_t *offsets;
-    uint32_t ranges, tiles_o, tiles_i, splits, accumulate;
-    void *grad;      // [ranges][out_width][in_width]
-    float *parts;    // [splits][ranges][out_width][in_width] where splits > 1
-    uint64_t size;   // ranges * out_width * in_width
+    uint32_t tiles_o, tiles_i, accumulate;
+    uint32_t of_one;               // without a table: runs of the one range
+    const int32_t *offsets;        // its bounds, null: all rows
+    const RunTable *table;
+    const Run *runs;
+    const Split *splits;
+    void *grad;                    // [ranges][out_width][in_width]
+    float *parts;                  // [slots][out_width][in_width]
 };
 
 // Word (4 rows' worth of banks) of rows [8 oct, 8 oct + 8) of an LDS column: columns are
@@ -73,22 +91,101 @@ __device__ __forceinline__ uint32_t place(uint32_t col, uint32_t oct) {
 // the tiles four high, so the 32 blocks that an XCD's CUs hold share 4 column ranges of dy and 8 of x
 // (which has half the bytes) and an L2 fetches a twelfth to an eighth of what its blocks ask for.
 struct Unit {
-    uint32_t range, split, tile_o, tile_i;
+    uint32_t run, tile_o, tile_i;
 };
 
 __device__ __forceinline__ Unit unit_of(const WeightGrad &g) {
-    const uint32_t tiles = g.tiles_o * g.tiles_i, all = tiles * g.splits;
-    Unit u;
-    u.range = blockIdx.x / all;
-    const uint32_t at = blockIdx.x - u.range * all, xcd = at & 7;
+    const uint32_t tiles = g.tiles_o * g.tiles_i, all = g.table ? tiles : gridDim.x;
+    const uint32_t before = blockIdx.x / all, at = blockIdx.x - before * all, xcd = at & 7;
     uint32_t id = xcd * (all / 8) + min(xcd, all & 7) + at / 8;
-    u.split = id / tiles;
-    id -= u.split * tiles;
+    Unit u;
+    u.run = id / tiles;
+    id -= u.run * tiles;
+    u.run += before;
     const uint32_t band = id / (4 * g.tiles_i), high = min(4u, g.tiles_o - 4 * band);
     id -= band * 4 * g.tiles_i;
     u.tile_i = id / high;
     u.tile_o = 4 * band + id - u.tile_i * high;
     return u;
+}
+
+// The runs of ragged ranges: a range of more than `most` steps becomes several of about the
+// same length, and of up to kRanked runs the longest come first, so that none is left for the
+// end.  One block.  An empty range is a run too, which writes its zeros.
+constexpr uint32_t kPlanThreads = 1024, kRanked = 1024;
+
+struct RunPlan {
+    const int32_t *offsets;
+    uint32_t rows, ranges, most;
+    uint32_t max_runs, max_splits, max_slots;
+    RunTable *table;
+    Run *runs;
+    Split *splits;
+};
+
+__global__ __launch_bounds__(kPlanThreads) void weight_plan_kernel(RunPlan p) {
+    __shared__ uint32_t sums[3][kPlanThreads];
+    __shared__ uint32_t length[kRanked];
+    const uint32_t tid = threadIdx.x, each = (p.ranges + kPlanThreads - 1) / kPlanThreads;
+    const uint32_t first = min(tid * each, p.ranges), last = min(first + each, p.ranges);
+    const auto bound = [&](uint32_t r) { return (uint32_t)min(max(p.offsets[r], 0), (int32_t)p.rows); };
+    const auto steps_of = [&](uint32_t begin, uint32_t end) { return end > begin ? (end - begin + kStep - 1) / kStep : 0u; };
+
+    // how many runs, split ranges and slots the thread's ranges need, and those before it
+    uint32_t need[3] = {}, at[3];
+    for (uint32_t r = first; r < last; ++r) {
+        const uint32_t n = max(1u, (steps_of(bound(r), bound(r + 1)) + p.most - 1) / p.most);
+        need[0] += n;
+        need[1] += n > 1;
+        need[2] += n > 1 ? n : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < 3; ++i) sums[i][tid] = need[i];
+    __syncthreads();
+    for (uint32_t d = 1; d < kPlanThreads; d <<= 1) {
+        uint32_t add[3];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) add[i] = tid >= d ? sums[i][tid - d] : 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 3; ++i) sums[i][tid] += add[i];
+        __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < 3; ++i) at[i] = sums[i][tid] - need[i];
+    const uint32_t all = sums[0][kPlanThreads - 1], ranked = all <= kRanked;
+
+    // Offsets that do not ascend could ask for more than there is: what does not fit is left out.
+    const auto each_run = [&](auto f) {
+        uint32_t n0 = at[0], n1 = at[1], n2 = at[2];
+        for (uint32_t r = first; r < last; ++r) {
+            const uint32_t begin = bound(r), end = max(begin, bound(r + 1)), steps = steps_of(begin, end);
+            uint32_t n = max(1u, (steps + p.most - 1) / p.most);
+            if (n > 1 && (n1 >= p.max_splits || n2 + n > p.max_slots)) n = 1;
+            const uint32_t part = (steps + n - 1) / n;
+            for (uint32_t i = 0; i < n; ++i) {
+                const uint32_t from = min(begin + i * part * kStep, end), to = min(from + part * kStep, end);
+                f(n0++, Run{r, from, to, n > 1 ? n2 + i : kNone});
+            }
+            if (n > 1) {
+                p.splits[n1++] = Split{r, n2, n};
+                n2 += n;
+            }
+        }
+    };
+    if (tid == 0) *p.table = RunTable{min(all, p.max_runs), min(sums[1][kPlanThreads - 1], p.max_splits)};
+    if (ranked) {
+        each_run([&](uint32_t i, const Run &r) { length[i] = r.end - r.begin; });
+        __syncthreads();
+    }
+    each_run([&](uint32_t i, const Run &r) {
+        uint32_t rank = i;
+        if (ranked) {
+            rank = 0;
+            for (uint32_t j = 0; j < all; ++j) rank += length[j] > length[i] || (length[j] == length[i] && j < i);
+        }
+        if (rank < p.max_runs) p.runs[rank] = r;
+    });
 }
 
 template <int N>
@@ -136,8 +233,9 @@ __device__ __forceinline__ Rsrc buffer(const void *p, uint32_t bytes) {
 // waits for memory took half of the time).
 // C = 4, 128 x 128: 64 sums a lane and half of the LDS, so that two blocks share a CU.
 //
-// Rows past the end come back as zeros from the buffers' bounds.  ALIGNED: dy's rows begin and end on whole
-// words, as buffer loads want; else they are read with plain loads, which take any address, and masked.
+// Rows past the end come back as zeros from the buffers' bounds.  ALIGNED: dy's rows begin on whole words, as
+// buffer loads want, and are a multiple of 8 wide; else they are read with plain loads, which take any address, and
+// masked.
 template <class T, class G, int C, bool ALIGNED>
 __global__ __launch_bounds__(256, C == 8 ? 1 : 2) void weight_gradient_kernel(WeightGrad g) {
     constexpr uint32_t kTile = 32 * C, kPad = 8;    // a tile's first block may begin up to 7 columns before it
@@ -149,59 +247,58 @@ __global__ __launch_bounds__(256, C == 8 ? 1 : 2) void weight_gradient_kernel(We
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64);
 
     const Unit unit = unit_of(g);
-    uint32_t range = unit.range, begin = 0, end = g.rows;
-    if (g.offsets) {
-        const auto bound = [&](uint32_t r) { return (uint32_t)min(max(g.offsets[r], 0), (int32_t)g.rows); };
-        if (g.ranges <= kRanked) {
-            // the longest range first, so that no long one is left for the end
-            uint32_t *length = (uint32_t *)lds;
-            const uint32_t mine = tid < g.ranges ? max(bound(tid + 1), bound(tid)) - bound(tid) : 0;
-            length[tid] = mine;
-            __syncthreads();
-            uint32_t rank = 0;
-            for (uint32_t r = 0; r < g.ranges; ++r) rank += length[r] > mine || (length[r] == mine && r < tid);
-            __syncthreads();
-            if (tid < g.ranges && rank == unit.range) length[0] = tid;
-            __syncthreads();
-            range = __builtin_amdgcn_readfirstlane(length[0]);
-            __syncthreads();
+    Run run;
+    if (g.table) {
+        if (unit.run >= g.table->runs) return;
+        run = g.runs[unit.run];
+        if (run.begin == run.end && run.slot == kNone && g.accumulate) return;
+    } else {
+        uint32_t begin = 0, end = g.rows;
+        if (g.offsets) {
+            begin = (uint32_t)min(max(g.offsets[0], 0), (int32_t)g.rows);
+            end = (uint32_t)min(max(g.offsets[1], (int32_t)begin), (int32_t)g.rows);
         }
-        begin = __builtin_amdgcn_readfirstlane(bound(range));
-        end = max(begin, (uint32_t)__builtin_amdgcn_readfirstlane(bound(range + 1)));
+        const uint32_t steps = (end - begin + kStep - 1) / kStep, each = (steps + g.of_one - 1) / g.of_one;
+        run.range = 0;
+        run.begin = min(begin + min(unit.run * each, steps) * kStep, end);
+        run.end = min(run.begin + each * kStep, end);
+        run.slot = g.of_one > 1 ? unit.run : kNone;
     }
-    {   // this split's steps
-        const uint32_t steps = (end - begin + kStep - 1) / kStep, each = (steps + g.splits - 1) / g.splits;
-        const uint32_t from = min(unit.split * each, steps), to = min(from + each, steps);
-        end = min(end, begin + to * kStep);
-        begin += from * kStep;
-    }
+    const uint32_t begin = run.begin, end = run.end;
 
     const uint32_t o0 = unit.tile_o * kTile, i0 = unit.tile_i * kTile;
     const uint32_t cb = tid % 32, oct = tid / 32;
     const uint32_t o_first = o0 + cb * C, i_first = i0 + cb * C;
-    // the last block of dy's columns is moved back to end with the row
-    const uint32_t o_from = g.out_width >= C ? min(o_first, g.out_width - C) : 0;
+    // not ALIGNED: the last block of dy's columns is moved back to end with the row
+    const uint32_t o_from = ALIGNED ? o_first : g.out_width >= C ? min(o_first, g.out_width - C) : 0;
     const uint32_t dy_row = (uint32_t)g.dy_pitch * 2, x_row = g.groups * kGroup;    // bytes
     constexpr uint32_t kNowhere = 0x80000000u;
     const uint32_t dy_at = o_first < g.out_width ? oct * 8 * dy_row + o_from * 2 : kNowhere;
     const uint32_t x_at = i_first < x_row ? oct * 8 * x_row + i_first : kNowhere;
     const uint32_t s_at = i_first < x_row ? oct * 8 * g.groups + i_first / kGroup : kNowhere;
-    const int32_t col0 = o_first < g.out_width ? (int32_t)o_from - (int32_t)o0 : (int32_t)(cb * C);
+    const int32_t col0 = !ALIGNED && o_first < g.out_width ? (int32_t)o_from - (int32_t)o0 : (int32_t)(cb * C);
+    // where a column's rows go in LDS: that of the block's column c is that of its column 0, xor c, 8 c further
+    const uint32_t to = kPad * 8 + (place(cb * C, oct));
 
-    // A row's buffer begins at the row, so the lanes' offsets are the same for all eight.
+    // The rows from t0 on as buffers that end with the step or the range; a thread's rows are scalar offsets apart, which
+    // the bounds check counts (a descriptor for each row took as long to make as the matrix instructions to run).
     Row dy[2][8];
     Codes x[2][8];
     uint32_t sc[2][8];
-    const auto rows_of = [&](const void *base, uint32_t row, uint32_t t0, uint32_t r) {
-        const uint32_t n = t0 + r < end ? min(end - t0, kStep) - r : 0, t = n ? t0 + r : 0;
-        return buffer((const char *)base + (uint64_t)t * row, n * row);
+    Rsrc from_dy, from_codes, from_scales;
+    const auto aim = [&](uint32_t t0) {
+        const uint32_t n = t0 < end ? min(end - t0, kStep) : 0;
+        const uint64_t t = n ? t0 : 0;
+        if constexpr (ALIGNED) from_dy = buffer((const char *)g.dy + t * dy_row, n * dy_row);
+        from_codes = buffer(g.codes + t * x_row, n * x_row);
+        from_scales = buffer(g.scales + t * g.groups, n * g.groups);
     };
     const auto fetch_dy = [&](int set, uint32_t t0, uint32_t r) {
         if constexpr (C == 8) {
             static_assert(ALIGNED);
-            dy[set][r] = __builtin_amdgcn_raw_buffer_load_b128(rows_of(g.dy, dy_row, t0, r), dy_at, 0, 0);
+            dy[set][r] = __builtin_amdgcn_raw_buffer_load_b128(from_dy, dy_at, r * dy_row, 0);
         } else if constexpr (ALIGNED) {
-            dy[set][r] = __builtin_amdgcn_raw_buffer_load_b64(rows_of(g.dy, dy_row, t0, r), dy_at, 0, 0);
+            dy[set][r] = __builtin_amdgcn_raw_buffer_load_b64(from_dy, dy_at, r * dy_row, 0);
         } else {
             const uint32_t row = min(t0 + oct * 8 + r, end - 1);
             const uint16_t *p = (const uint16_t *)g.dy + row * g.dy_pitch + o_from;
@@ -215,13 +312,12 @@ __global__ __launch_bounds__(256, C == 8 ? 1 : 2) void weight_gradient_kernel(We
             }
         }
     };
-    const auto fetch_x = [&](int set, uint32_t t0, uint32_t r) {
-        const Rsrc codes = rows_of(g.codes, x_row, t0, r);
+    const auto fetch_x = [&](int set, uint32_t r) {
         if constexpr (C == 8)
-            x[set][r] = __builtin_amdgcn_raw_buffer_load_b64(codes, x_at, 0, 0);
+            x[set][r] = __builtin_amdgcn_raw_buffer_load_b64(from_codes, x_at, r * x_row, 0);
         else
-            x[set][r][0] = __builtin_amdgcn_raw_buffer_load_b32(codes, x_at, 0, 0);
-        sc[set][r] = __builtin_amdgcn_raw_buffer_load_b8(rows_of(g.scales, g.groups, t0, r), s_at, 0, 0);
+            x[set][r][0] = __builtin_amdgcn_raw_buffer_load_b32(from_codes, x_at, r * x_row, 0);
+        sc[set][r] = __builtin_amdgcn_raw_buffer_load_b8(from_scales, s_at, r * g.groups, 0);
     };
     // Column c of the thread's block, of the rows that begin at t0.
     const auto write_dy = [&](int set, uint32_t buf, uint32_t t0, int c) {
@@ -235,10 +331,13 @@ __global__ __launch_bounds__(256, C == 8 ? 1 : 2) void weight_gradient_kernel(We
             }
             w[t] = __builtin_amdgcn_perm(hi, lo, c & 1 ? 0x07060302u : 0x05040100u);
         }
-        lds[buf * kBuf + kPad * 8 + (int32_t)place((uint32_t)(col0 + c), oct)] = w;
+        if constexpr (ALIGNED)
+            lds[buf * kBuf + (to ^ c) + c * 8] = w;
+        else
+            lds[buf * kBuf + kPad * 8 + (int32_t)place((uint32_t)(col0 + c), oct)] = w;
     };
     // Rows 2 t and 2 t + 1 of column c; with the last two the column is written.
-    // A group of scale byte 255 has codes 0, and 0 times the infinity that byte stands for is NaN.
+    // A group of scale byte 255 has codes 0, and 0 times the infinity that its bits are as a float is NaN.
     Words4 turned;
     const auto unpack_x = [&](int set, uint32_t buf, auto column, int t) {
         constexpr int c = decltype(column)::value;
@@ -246,10 +345,11 @@ __global__ __launch_bounds__(256, C == 8 ? 1 : 2) void weight_gradient_kernel(We
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int r = 2 * t + h;
-            v[h] = signed_byte<c & 3>(x[set][r][c / 4]) * __uint_as_float(sc[set][r] << 23);
+            if constexpr (c == 0) sc[set][r] <<= 23;    // the scale as a float
+            v[h] = signed_byte<c & 3>(x[set][r][c / 4]) * __uint_as_float(sc[set][r]);
         }
         turned[t] = pack<T>(v[0], v[1]);
-        if (t == 3) lds[(2 + buf) * kBuf + kPad * 8 + place(cb * C + c, oct)] = turned;
+        if (t == 3) lds[(2 + buf) * kBuf + (to ^ c) + c * 8] = turned;
     };
 
     // The words of column (wave's first + 32 m + lane % 32), rows [16 s + 8 (lane / 32), ...).
@@ -285,8 +385,8 @@ __global__ __launch_bounds__(256, C == 8 ? 1 : 2) void weight_gradient_kernel(We
                 });
             }
             if constexpr (s == 2 && j < C) write_dy(set, buf ^ 1, t0 + kStep, j);
-            if constexpr (s == 2 && C == 8 && j >= 8) fetch_x(set, t0 + 3 * kStep, j - 8);
-            if constexpr (s == 2 && C == 4) each<2>([&](auto r) { fetch_x(set, t0 + 3 * kStep, 2 * j + decltype(r)::value); });
+            if constexpr (s == 2 && C == 8 && j >= 8) fetch_x(set, j - 8);
+            if constexpr (s == 2 && C == 4) each<2>([&](auto r) { fetch_x(set, 2 * j + decltype(r)::value); });
             if constexpr (s == 3 && C == 8 && j < 8) fetch_dy(set, t0 + 3 * kStep, j);
             if constexpr (s == 3 && C == 4) each<2>([&](auto r) { fetch_dy(set, t0 + 3 * kStep, 2 * j + decltype(r)::value); });
             __builtin_amdgcn_sched_barrier(0);
@@ -297,6 +397,7 @@ __global__ __launch_bounds__(256, C == 8 ? 1 : 2) void weight_gradient_kernel(We
     const auto step = [&](auto buf, uint32_t t0) {
         quarter(Int<0>{}, buf, t0);
         quarter(Int<1>{}, buf, t0);
+        aim(t0 + 3 * kStep);
         quarter(Int<2>{}, buf, t0);
         __syncthreads();    // the other buffer is whole, and this one read
         quarter(Int<3>{}, buf, t0);
@@ -304,8 +405,9 @@ __global__ __launch_bounds__(256, C == 8 ? 1 : 2) void weight_gradient_kernel(We
 
     if (begin < end) {
         const auto fetch = [&](int set, uint32_t t0) {
+            aim(t0);
             each<8>([&](auto r) {
-                fetch_x(set, t0, decltype(r)::value);
+                fetch_x(set, decltype(r)::value);
                 fetch_dy(set, t0, decltype(r)::value);
             });
         };
@@ -326,70 +428,98 @@ __global__ __launch_bounds__(256, C == 8 ? 1 : 2) void weight_gradient_kernel(We
 
     // Value e of a tile: row 8 (e / 4) + 4 (lane / 32) + e % 4, column lane % 32.  Rows and columns past the
     // gradient's are dropped by the buffer's bounds.
-    const auto write = [&](auto type, void *to, bool add) {
+    const auto write = [&](auto type, void *result, uint32_t range, bool add) {
         using R = decltype(type);
         constexpr uint32_t kSize = sizeof(typename R::raw);
-        const uint32_t row = g.in_width * kSize;
-        typename R::raw *base = (typename R::raw *)to + (uint64_t)range * g.out_width * g.in_width;
+        const uint32_t row = g.in_width * kSize, o = o0 + wave / 2 * (16 * C);
+        const uint32_t rows = o < g.out_width ? min(g.out_width - o, 16u * C) : 0;
+        const Rsrc r = buffer((typename R::raw *)result + ((uint64_t)range * g.out_width + (rows ? o : 0)) * g.in_width, rows * row);
         each<kPieces>([&](auto index) {
             constexpr int m = decltype(index)::value / M, n = decltype(index)::value % M;
             const uint32_t i = i0 + wave % 2 * (16 * C) + n * 32 + lane % 32;
             const uint32_t at = i < g.in_width ? lane / 32 * 4 * row + i * kSize : kNowhere;
             each<16>([&](auto element) {
                 constexpr int e = decltype(element)::value;
-                const uint32_t o = o0 + wave / 2 * (16 * C) + m * 32 + e / 4 * 8 + e % 4;
-                const uint32_t left = o < g.out_width ? min(g.out_width - o, 8u) : 0;
-                const Rsrc r = buffer(base + (uint64_t)(left ? o : 0) * g.in_width, left * row);
+                const uint32_t down = (m * 32 + e / 4 * 8 + e % 4) * row;
                 float v = acc[m][n][e];
                 if constexpr (kSize == 4) {
-                    if (add) v += __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0));
-                    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), r, at, 0, 0);
+                    if (add) v += __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, at, down, 0));
+                    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), r, at, down, 0);
                 } else {
                     if (add)
-                        v += R::up(__builtin_bit_cast(typename R::raw, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0)));
-                    __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, R::down(v)), r, at, 0, 0);
+                        v += R::up(__builtin_bit_cast(typename R::raw, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, at, down, 0)));
+                    __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, R::down(v)), r, at, down, 0);
                 }
             });
         });
     };
-    if (g.splits > 1)
-        write(F32{}, g.parts + unit.split * g.size, false);
+    if (run.slot != kNone)
+        write(F32{}, g.parts, run.slot, false);
     else if (g.accumulate)
-        write(G{}, g.grad, true);
+        write(G{}, g.grad, run.range, true);
     else
-        write(G{}, g.grad, false);
+        write(G{}, g.grad, run.range, false);
 }
 
-// Adds the splits' parts, in order.
+// Adds a split range's slots, in order.
 template <class G>
-__global__ __launch_bounds__(kBlock) void weight_gradient_join_kernel(const float *parts, uint64_t size, uint32_t splits,
-                                                                      uint32_t accumulate, typename G::raw *grad) {
+__global__ __launch_bounds__(kBlock) void weight_join_kernel(WeightGrad g) {
+    Split s = {0, 0, g.of_one};
+    if (g.table) {
+        if (blockIdx.y >= g.table->splits) return;
+        s = g.splits[blockIdx.y];
+    }
+    const uint64_t size = (uint64_t)g.out_width * g.in_width;
+    const float *parts = g.parts + s.slot * size;
+    typename G::raw *grad = (typename G::raw *)g.grad + s.range * size;
     for (uint64_t i = (uint64_t)blockIdx.x * kBlock + threadIdx.x; i < size; i += (uint64_t)gridDim.x * kBlock) {
-        float sum = accumulate ? G::up(grad[i]) : 0.0f;
-        for (uint32_t s = 0; s < splits; ++s) sum += parts[s * size + i];
+        float sum = g.accumulate ? G::up(grad[i]) : 0.0f;
+        for (uint32_t r = 0; r < s.runs; ++r) sum += parts[r * size + i];
         grad[i] = G::down(sum);
     }
 }
 
 struct WeightPlan {
     bool large;
-    uint32_t tiles_o, tiles_i, splits;
+    uint32_t tiles_o, tiles_i;
+    uint32_t each;                                // ragged: steps of a run at most
+    uint64_t max_runs, max_splits, max_slots;     // one range: exact
+    uint64_t table, runs, splits, bytes;          // offsets of the workspace, after the slots
 };
 
-// Tiles of 256 x 256 where those give every second CU one, else tiles of 128 x 128; then the rows of each
-// range are split until there are about 512 blocks, each with 8 steps or more if the ranges were equal.
-inline WeightPlan weight_plan(uint64_t rows, uint64_t out_width, uint64_t in_width, uint32_t n_ranges) {
-    WeightPlan p;
-    const uint64_t at256 = ((out_width + 255) / 256) * ((in_width + 255) / 256) * n_ranges;
-    p.large = at256 >= 128;
-    const uint32_t side = p.large ? 256 : 128;
+// Tiles of 256 x 256 where the 256 CUs get 16 steps or more each (1077 TFLOP/s on long sums, 686 with tiles of
+// 128 x 128, which fill the chip with less).  One range: its rows are split until every CU has a block (two of the
+// small tiles), each of 16 (8) steps or more.  Ragged ranges: runs of at most half of a CU's share.
+inline WeightPlan weight_plan(uint64_t rows, uint64_t out_width, uint64_t in_width, uint32_t n_ranges, bool whole) {
+    WeightPlan p = {};
+    const bool ragged = n_ranges > 1;
+    const uint64_t steps = (rows + kStep - 1) / kStep;
+    const auto tiles = [&](uint64_t side) { return ((out_width + side - 1) / side) * ((in_width + side - 1) / side); };
+    p.large = whole && steps * tiles(256) >= 256 * 16;
+    const uint64_t side = p.large ? 256 : 128, each = p.large ? 16 : 8, n = tiles(side);
     p.tiles_o = (uint32_t)((out_width + side - 1) / side);
     p.tiles_i = (uint32_t)((in_width + side - 1) / side);
-    const uint64_t units = (uint64_t)p.tiles_o * p.tiles_i * n_ranges;
-    const uint64_t by_rows = rows / n_ranges / (8 * kStep);
-    uint64_t s = (p.large ? 256 : 512) / units;
-    s = s < by_rows ? s : by_rows;
-    p.splits = (uint32_t)(s < 1 ? 1 : s);
+    if (ragged) {
+        const uint64_t half = steps * n / 512;
+        p.each = (uint32_t)(half < each ? each : half);
+        p.max_splits = steps / p.each;
+        p.max_runs = n_ranges + p.max_splits;
+        p.max_slots = 2 * p.max_splits;
+    } else {
+        uint64_t runs = (p.large ? 256 : 512) / n, most = steps / each;
+        runs = runs < most ? runs : most;
+        p.max_runs = runs < 2 ? 1 : runs;
+        p.max_splits = p.max_runs > 1;
+        p.max_slots = p.max_runs > 1 ? p.max_runs : 0;
+    }
+    const auto up = [](uint64_t v) { return (v + 255) / 256 * 256; };
+    p.bytes = up(p.max_slots * out_width * in_width * 4);
+    if (ragged) {
+        p.table = p.bytes;
+        p.runs = p.table + up(sizeof(RunTable));
+        p.splits = p.runs + up(p.max_runs * sizeof(Run));
+        p.bytes = p.splits + up(p.max_splits * sizeof(Split));
+    }
     return p;
 }
 
@@ -398,8 +528,9 @@ inline int check_weight(uint64_t rows, uint64_t out_width, uint64_t in_width, ui
     PL_TRY(check_sizes(rows, in_width));
     if (!n_ranges) return POSEIDON_E_INVAL;
     if (n_ranges > POSEIDON_RANGES_MAX) return POSEIDON_E_RANGE;
+    // blocks of one launch
     const uint64_t tiles = ((out_width + 127) / 128) * ((in_width + 127) / 128);
-    return tiles * n_ranges > POSEIDON_TILES_MAX ? POSEIDON_E_RANGE : POSEIDON_OK;    // blocks of one launch
+    return tiles * n_ranges > POSEIDON_TILES_MAX ? POSEIDON_E_RANGE : POSEIDON_OK;
 }
 
 }  // namespace pl
@@ -410,8 +541,10 @@ extern "C" {
 
 uint64_t poseidon_weight_gradient_workspace(uint64_t rows, uint64_t out_width, uint64_t in_width, uint32_t n_ranges) {
     if (check_weight(rows, out_width, in_width, n_ranges) != POSEIDON_OK) return UINT64_MAX;
-    const WeightPlan p = weight_plan(rows, out_width, in_width, n_ranges);
-    return p.splits > 1 ? p.splits * (uint64_t)n_ranges * out_width * in_width * 4 : 0;
+    // the most that any layout of dy needs
+    const uint64_t a = weight_plan(rows, out_width, in_width, n_ranges, false).bytes;
+    const uint64_t b = weight_plan(rows, out_width, in_width, n_ranges, true).bytes;
+    return a < b ? b : a;
 }
 
 int poseidon_weight_gradient(const void *dy, uint64_t dy_pitch, uint32_t type, uint64_t rows, uint64_t out_width,
@@ -427,13 +560,9 @@ int poseidon_weight_gradient(const void *dy, uint64_t dy_pitch, uint32_t type, u
     PL_TRY(check_workspace(workspace, workspace_bytes,
                            poseidon_weight_gradient_workspace(rows, out_width, in_width, n_ranges)));
     const hipStream_t stream = (hipStream_t)hip_stream;
-    WeightPlan p = weight_plan(rows, out_width, in_width, n_ranges);
-    const bool whole = aligned(dy, 4) && dy_pitch % 2 == 0 && out_width % 2 == 0 && out_width >= 8;
-    if (p.large && !whole) {    // plain loads' addresses do not fit beside 256 sums
-        p.large = false;
-        p.tiles_o = (uint32_t)((out_width + 127) / 128);
-        p.tiles_i = (uint32_t)((in_width + 127) / 128);
-    }
+    const bool whole = aligned(dy, 4) && dy_pitch % 2 == 0 && out_width % 8 == 0;
+    const WeightPlan p = weight_plan(rows, out_width, in_width, n_ranges, whole);
+    char *base = (char *)workspace;
     WeightGrad g = {};
     g.dy = dy;
     g.dy_pitch = dy_pitch;
@@ -443,26 +572,30 @@ int poseidon_weight_gradient(const void *dy, uint64_t dy_pitch, uint32_t type, u
     g.groups = groups_of(in_width);
     g.codes = codes;
     g.scales = scales;
-    g.offsets = offsets;
-    g.ranges = n_ranges;
     g.tiles_o = p.tiles_o;
     g.tiles_i = p.tiles_i;
-    g.splits = p.splits;
     g.accumulate = accumulate;
+    g.of_one = (uint32_t)p.max_runs;
     g.grad = grad;
-    g.parts = (float *)workspace;
-    g.size = (uint64_t)n_ranges * out_width * in_width;
-    const uint32_t blocks = p.tiles_o * p.tiles_i * p.splits * n_ranges;
+    g.parts = (float *)base;
+    g.offsets = offsets;
+    if (n_ranges > 1) {
+        RunPlan r = {offsets, (uint32_t)rows, n_ranges, p.each, (uint32_t)p.max_runs, (uint32_t)p.max_splits,
+                     (uint32_t)p.max_slots, (RunTable *)(base + p.table), (Run *)(base + p.runs), (Split *)(base + p.splits)};
+        g.table = r.table;
+        g.runs = r.runs;
+        g.splits = r.splits;
+        weight_plan_kernel<<<1, kPlanThreads, 0, stream>>>(r);
+    }
+    const uint32_t blocks = (uint32_t)(p.tiles_o * p.tiles_i * p.max_runs);
+    const uint64_t joins = (out_width * in_width + kBlock - 1) / kBlock;
+    const dim3 join((uint32_t)(joins < 4096 ? joins : 4096), (uint32_t)p.max_splits);
     const auto run = [&](auto t) {
         using D = decltype(t);
         PL_TYPE(grad_type, if (p.large) weight_gradient_kernel<D, T, 8, true><<<blocks, 256, 0, stream>>>(g);
                 else if (whole) weight_gradient_kernel<D, T, 4, true><<<blocks, 256, 0, stream>>>(g);
                 else weight_gradient_kernel<D, T, 4, false><<<blocks, 256, 0, stream>>>(g);
-                if (p.splits > 1) {
-                    const uint64_t n = (g.size + kBlock - 1) / kBlock;
-                    weight_gradient_join_kernel<T><<<(uint32_t)(n < 4096 ? n : 4096), kBlock, 0, stream>>>(
-                        g.parts, g.size, g.splits, g.accumulate, (T::raw *)grad);
-                });
+                if (p.max_splits) weight_join_kernel<T><<<join, kBlock, 0, stream>>>(g));
     };
     if (type == POSEIDON_F16)
         run(F16{});
