@@ -1,8 +1,8 @@
 // Sort of tokens by expert, and the gradient of an embedding summed by token.
 //
 // Both sort whole keys stably with a counting sort of up to 9 bits a pass, the
-// low bits first.  A block takes 4096 neighbouring elements, a wave 512 of them,
-// 64 at a time in order; lanes with the same digit find each other with one
+// low bits first.  A block of eight waves takes up to 4096 neighbouring elements, a wave an eighth
+// of them, 64 at a time in order; lanes with the same digit find each other with one
 // ballot a bit, so an element's rank among the equal ones before it needs no
 // atomics and the order is the same on every call.
 #include "layers_device.h"
@@ -20,7 +20,7 @@ struct SortPass {
     const int32_t *from;       // the elements' indexes, null: 0, 1, 2, ...
     uint32_t m, n_keys;        // elements; keys outside [0, n_keys) count as n_keys
     uint32_t shift, bins, bits;
-    uint32_t blocks;
+    uint32_t blocks, rounds;   // of 64 elements a wave: a block takes 512 * rounds
     uint32_t *counts;          // [blocks][bins]
     uint32_t *totals;          // [bins], only where a kernel of its own scans
     int32_t *keys_out;         // null: not needed
@@ -63,8 +63,8 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortPass p, Cl
     if (blockIdx.x >= p.blocks) return clear(c, blockIdx.x - p.blocks);
     for (uint32_t b = threadIdx.x; b < p.bins; b += kSortThreads) count[b] = 0;
     __syncthreads();
-    const uint32_t first = blockIdx.x * kSortTile;
-    for (uint32_t r = 0; r < kSortRounds; ++r) {
+    const uint32_t first = blockIdx.x * (kSortThreads * p.rounds);
+    for (uint32_t r = 0; r < p.rounds; ++r) {
         const uint32_t i = first + r * kSortThreads + threadIdx.x;
         if (i < p.m) atomicAdd(&count[(key_at(p, i) >> p.shift) & (p.bins - 1)], 1u);
     }
@@ -121,15 +121,16 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortPass p, Cl
     __shared__ uint32_t moved[SOLO ? 2 : 1][SOLO ? kSortTile : 1];
     if (blockIdx.x >= p.blocks) return clear(c, blockIdx.x - p.blocks);
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
-    const uint32_t first = blockIdx.x * kSortTile + wave * (64 * kSortRounds);
-    const uint32_t rounds = first < p.m ? min((p.m - first + 63) / 64, kSortRounds) : 0;    // of this wave
+    const uint32_t first = (blockIdx.x * kSortWaves + wave) * (64 * p.rounds);
+    const uint32_t rounds = first < p.m ? min((p.m - first + 63) / 64, p.rounds) : 0;    // of this wave
     const uint64_t below = (1ull << lane) - 1;
     uint32_t key[kSortRounds], index[kSortRounds];
 #pragma unroll
     for (uint32_t r = 0; r < kSortRounds; ++r) {
         const uint32_t i = first + r * 64 + lane;
-        key[r] = i < p.m ? key_at(p, i) : 0xffffffffu;
-        index[r] = i < p.m && p.from ? (uint32_t)p.from[i] : i;
+        const bool on = r < rounds && i < p.m;
+        key[r] = on ? key_at(p, i) : 0xffffffffu;
+        index[r] = on && p.from ? (uint32_t)p.from[i] : i;
     }
     for (uint32_t pass = 0; pass < (SOLO ? p.passes : 1u); ++pass) {
         const uint32_t shift = SOLO ? pass * p.bits : p.shift;
@@ -138,7 +139,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortPass p, Cl
             if (tid < p.bins) count[w][tid] = 0;
         __syncthreads();
 
-        // ranks within the wave's 512 elements
+        // ranks within the wave's elements
         uint32_t rank[kSortRounds];
         volatile uint32_t *mine = count[wave];
 #pragma unroll
@@ -162,20 +163,34 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortPass p, Cl
 
         // a bin a thread: where the block's elements of this digit begin
         uint32_t before = 0, total = 0;
-        if (tid < p.bins) {
-            if (p.blocks == 1) {
+        if constexpr (SOLO) {
+            if (tid < p.bins) {
 #pragma unroll
                 for (uint32_t w = 0; w < kSortWaves; ++w) total += count[w][tid];
-            } else if (p.totals) {
+            }
+        } else if (p.totals) {
+            if (tid < p.bins) {
                 before = p.counts[blockIdx.x * p.bins + tid];
                 total = p.totals[tid];
-            } else {
-                for (uint32_t b = 0; b < p.blocks; ++b) {
-                    const uint32_t n = p.counts[b * p.bins + tid];
-                    before += b < blockIdx.x ? n : 0u;
-                    total += n;
-                }
             }
+        } else {    // the blocks' counts, shared by as many groups of threads as there is room for
+            __shared__ uint32_t part[2][kSortThreads];
+            const uint32_t bin = tid & (p.bins - 1), group = tid / p.bins, groups = kSortThreads / p.bins;
+#pragma unroll 8
+            for (uint32_t b = group; b < p.blocks; b += groups) {
+                const uint32_t n = p.counts[b * p.bins + bin];
+                before += b < blockIdx.x ? n : 0u;
+                total += n;
+            }
+            part[0][tid] = before;
+            part[1][tid] = total;
+            __syncthreads();
+            before = total = 0;
+            if (tid < p.bins)
+                for (uint32_t i = 0; i < groups; ++i) {
+                    before += part[0][i * p.bins + tid];
+                    total += part[1][i * p.bins + tid];
+                }
         }
         const uint32_t start = block_prefix(total, wave_sums);
         if (tid < p.bins) {
@@ -215,7 +230,16 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortPass p, Cl
     }
 }
 
-inline uint32_t sort_blocks(uint64_t m) { return (uint32_t)((m + kSortTile - 1) / kSortTile); }
+// Few elements are spread over the eight waves of one block; then over blocks, of more elements each as they
+// get many.
+inline uint32_t sort_rounds(uint64_t m) {
+    if (m <= kSortTile) return m ? (uint32_t)((m + kSortThreads - 1) / kSortThreads) : 1;
+    return m <= 1u << 15 ? 2 : m <= 1u << 17 ? 4 : kSortRounds;
+}
+inline uint32_t sort_blocks(uint64_t m) {
+    const uint64_t each = kSortThreads * sort_rounds(m);
+    return (uint32_t)((m + each - 1) / each);
+}
 inline uint64_t round_up(uint64_t v, uint64_t to) { return (v + to - 1) / to * to; }
 // counts, then totals
 inline uint64_t sort_counts_bytes(uint64_t m) { return round_up(((uint64_t)sort_blocks(m) + 1) * kMaxBins * 4, 256); }
@@ -458,6 +482,7 @@ int poseidon_expert_sort(const int32_t *choice, uint64_t tokens, uint32_t k, uin
     while ((1u << p.bits) < n_experts + 1) ++p.bits;
     p.bins = 1u << p.bits;
     p.blocks = m ? sort_blocks(m) : 1;    // no choices: one block writes the offsets
+    p.rounds = sort_rounds(m);
     p.passes = 1;
     p.counts = (uint32_t *)workspace;
     p.order = order;
@@ -506,6 +531,7 @@ int poseidon_embed_backward(const int32_t *ids, uint64_t tokens, const void *dou
     p.bits = (bits + p.passes - 1) / p.passes;
     p.bins = 1u << p.bits;
     p.blocks = m ? sort_blocks(m) : 1;
+    p.rounds = sort_rounds(m);
     p.counts = (uint32_t *)(base + w.counts);
     SortLists lists;
     for (uint32_t i = 0; i < 2; ++i) {
