@@ -66,22 +66,54 @@ def _function(name: str):
     return _functions[name]
 
 
-@dataclass
 class Stash:
     """Rows kept in 8 bits: int8 codes [rows, groups * 64], uint8 scale bytes [rows, groups], the rows' width and the
-    type they came from."""
-    codes: torch.Tensor
-    scales: torch.Tensor
-    width: int
-    dtype: torch.dtype
+    type they came from.  The operators make theirs in one piece of memory, of which codes and scales are views."""
+    __slots__ = ("rows", "width", "dtype", "_codes", "_scales", "_memory")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, width: int, dtype: torch.dtype):
+        self.rows, self.width, self.dtype = scales.shape[0], width, dtype
+        self._codes, self._scales, self._memory = codes, scales, None
+
+    @classmethod
+    def empty(cls, rows: int, width: int, dtype: torch.dtype, device) -> "Stash":
+        s = cls.__new__(cls)
+        s.rows, s.width, s.dtype, s._codes, s._scales = rows, width, dtype, None, None
+        s._memory = torch.empty(rows * -(-width // GROUP) * (GROUP + 1), dtype=torch.uint8, device=device)
+        return s
 
     @property
-    def rows(self) -> int:
-        return self.scales.shape[0]
+    def codes(self) -> torch.Tensor:
+        if self._codes is None:
+            n = self.rows * _groups(self.width) * GROUP
+            self._codes = self._memory[:n].view(torch.int8).view(self.rows, _groups(self.width) * GROUP)
+        return self._codes
+
+    @property
+    def scales(self) -> torch.Tensor:
+        if self._scales is None:
+            n = self.rows * _groups(self.width) * GROUP
+            self._scales = self._memory[n:].view(self.rows, _groups(self.width))
+        return self._scales
 
     @property
     def nbytes(self) -> int:
-        return self.codes.numel() + self.scales.numel()
+        return self.rows * _groups(self.width) * (GROUP + 1)
+
+    @property
+    def device(self) -> torch.device:
+        return (self._codes if self._memory is None else self._memory).device
+
+    def tensors(self):
+        """The memory it holds."""
+        return (self._codes, self._scales) if self._memory is None else (self._memory,)
+
+    def addresses(self):
+        """(codes, scales) of a stash that _stash has looked over."""
+        if self._memory is None:
+            return self._codes.data_ptr(), self._scales.data_ptr()
+        at = self._memory.data_ptr()
+        return at, at + self.rows * _groups(self.width) * GROUP
 
 
 @dataclass
@@ -91,6 +123,10 @@ class ExpertPlan:
     order: torch.Tensor
     position: torch.Tensor
     offsets: torch.Tensor
+
+    def tensors(self):
+        """The memory it holds."""
+        return self.order, self.position, self.offsets
 
 
 def _refuse(where: str):
@@ -109,9 +145,9 @@ def _streamed(f):
         with torch.cuda.stream(stream):
             out = f(*args, **kw)
         for a in (*args, *kw.values()):
-            parts = [a] if isinstance(a, torch.Tensor) else vars(a).values() if isinstance(a, (Stash, ExpertPlan)) else ()
+            parts = (a,) if isinstance(a, torch.Tensor) else a.tensors() if isinstance(a, (Stash, ExpertPlan)) else ()
             for t in parts:
-                if isinstance(t, torch.Tensor) and t.is_cuda:
+                if t.is_cuda:
                     t.record_stream(stream)
         return out
 
@@ -182,17 +218,13 @@ def _groups(width: int) -> int:
     return -(-width // GROUP)
 
 
-def _new_stash(rows: int, width: int, dtype, device) -> Stash:
-    g = _groups(width)
-    return Stash(torch.empty(rows, g * GROUP, dtype=torch.int8, device=device),
-                 torch.empty(rows, g, dtype=torch.uint8, device=device), width, dtype)
-
-
 def _stash(s, where: str, device, rows=None, width=None) -> Stash:
-    if not isinstance(s, Stash) or s.scales.dim() != 2 or (rows is not None and s.scales.shape[0] != rows) or \
-            (width is not None and s.width != width):
-        _refuse(f"{where}: not a Stash of these sizes")
-    n, g = s.scales.shape[0], _groups(s.width)
+    if not isinstance(s, Stash) or (rows is not None and s.rows != rows) or (width is not None and s.width != width) or \
+            s.device != device:
+        _refuse(f"{where}: not a Stash of these sizes on {device}")
+    if s._memory is not None:
+        return s
+    n, g = s.rows, _groups(s.width)
     codes = _whole(s.codes, where, device, torch.int8, (n, g * GROUP))
     scales = _whole(s.scales, where, device, torch.uint8, (n, g))
     return s if codes is s.codes and scales is s.scales else Stash(codes, scales, s.width, s.dtype)
@@ -205,23 +237,23 @@ def poseidon_stash(x) -> Stash:
     """Rows of x [rows, width] kept in 8 bits."""
     x = _rows(x, "poseidon_stash: x")
     n, d = x.shape
-    s = _new_stash(n, d, x.dtype, x.device)
-    _call("poseidon_stash", x.device, x.data_ptr(), _pitch(x), TYPES[x.dtype], n, d, s.codes.data_ptr(),
-          s.scales.data_ptr())
+    s = Stash.empty(n, d, x.dtype, x.device)
+    _call("poseidon_stash", x.device, x.data_ptr(), _pitch(x), TYPES[x.dtype], n, d, *s.addresses())
     return s
 
 
 @_streamed
 def poseidon_restore(stash: Stash, *, dtype=None, out=None) -> torch.Tensor:
     """What was kept, [rows, width], in its own type or in `dtype`."""
+    if not isinstance(stash, Stash) or stash.device.type != "cuda":
+        _refuse("poseidon_restore: stash: not a Stash on the GPU")
     dtype = stash.dtype if dtype is None else dtype
-    if dtype not in TYPES or not stash.codes.is_cuda:
-        _refuse("poseidon_restore: stash on the GPU, and a float32, float16 or bfloat16 result")
-    device = stash.codes.device
+    if dtype not in TYPES:
+        _refuse("poseidon_restore: a float32, float16 or bfloat16 result")
+    device = stash.device
     s = _stash(stash, "poseidon_restore: stash", device)
     out = _out(out, "poseidon_restore: out", device, dtype, (s.rows, s.width))
-    _call("poseidon_restore", device, s.codes.data_ptr(), s.scales.data_ptr(), s.rows, s.width, out.data_ptr(),
-          _pitch(out), TYPES[dtype])
+    _call("poseidon_restore", device, *s.addresses(), s.rows, s.width, out.data_ptr(), _pitch(out), TYPES[dtype])
     return out
 
 
@@ -233,9 +265,9 @@ def poseidon_gated_forward(gate, up, *, keep: bool = True, out=None) -> Tuple[to
     dev, dt = gate.device, gate.dtype
     up = _rows(up, "poseidon_gated_forward: up", dev, dt, (n, d))
     out = _out(out, "poseidon_gated_forward: out", dev, dt, (n, d))
-    sg = _new_stash(n, d, dt, dev) if keep else None
-    su = _new_stash(n, d, dt, dev) if keep else None
-    kept = [t.data_ptr() for s in (sg, su) for t in (s.codes, s.scales)] if keep else [None] * 4
+    sg = Stash.empty(n, d, dt, dev) if keep else None
+    su = Stash.empty(n, d, dt, dev) if keep else None
+    kept = sg.addresses() + su.addresses() if keep else (None,) * 4
     _call("poseidon_gated_forward", dev, gate.data_ptr(), _pitch(gate), up.data_ptr(), _pitch(up), TYPES[dt], n, d,
           out.data_ptr(), _pitch(out), *kept)
     return out, sg, su
@@ -251,9 +283,8 @@ def poseidon_gated_backward(dout, gate: Stash, up: Stash, *, dgate=None, dup=Non
     up = _stash(up, "poseidon_gated_backward: up", dev, n, d)
     dgate = _out(dgate, "poseidon_gated_backward: dgate", dev, dt, (n, d))
     dup = _out(dup, "poseidon_gated_backward: dup", dev, dt, (n, d))
-    _call("poseidon_gated_backward", dev, dout.data_ptr(), _pitch(dout), TYPES[dt], n, d, gate.codes.data_ptr(),
-          gate.scales.data_ptr(), up.codes.data_ptr(), up.scales.data_ptr(), dgate.data_ptr(), _pitch(dgate),
-          dup.data_ptr(), _pitch(dup))
+    _call("poseidon_gated_backward", dev, dout.data_ptr(), _pitch(dout), TYPES[dt], n, d, *gate.addresses(),
+          *up.addresses(), dgate.data_ptr(), _pitch(dgate), dup.data_ptr(), _pitch(dup))
     return dgate, dup
 
 
@@ -282,8 +313,7 @@ def poseidon_weight_gradient(dy, x: Stash, *, offsets=None, dtype=torch.float32,
     if not out.is_contiguous():
         _refuse("poseidon_weight_gradient: out has gaps")
     w, at, size = _workspace("poseidon_weight_gradient", dev, n, o, x.width, ranges)
-    _call("poseidon_weight_gradient", dev, dy.data_ptr(), _pitch(dy), TYPES[dy.dtype], n, o, x.codes.data_ptr(),
-          x.scales.data_ptr(), x.width, None if offsets is None else offsets.data_ptr(), ranges, out.data_ptr(),
+    _call("poseidon_weight_gradient", dev, dy.data_ptr(), _pitch(dy), TYPES[dy.dtype], n, o, *x.addresses(), x.width, None if offsets is None else offsets.data_ptr(), ranges, out.data_ptr(),
           TYPES[dtype], int(accumulate), at, size)
     return out
 
@@ -308,14 +338,14 @@ def poseidon_expert_sort(choice, n_experts: int) -> ExpertPlan:
     return plan
 
 
-def _plan(plan, where: str, device, tokens: int) -> Tuple[torch.Tensor, torch.Tensor, int]:
-    """(position, the number of kept choices as a one-element view, k)"""
+def _plan(plan, where: str, device, tokens: int):
+    """(position, offsets, the address of their last entry, which is the number of kept choices, k)"""
     if not isinstance(plan, ExpertPlan) or plan.position.dim() != 2 or plan.position.shape[0] != tokens or \
-            plan.offsets.dim() != 1 or plan.offsets.numel() < 2:
+            plan.offsets.dim() != 1 or plan.offsets.shape[0] < 2:
         _refuse(f"{where}: not the ExpertPlan of these tokens")
     position = _whole(plan.position, where, device, torch.int32, None)
     offsets = _whole(plan.offsets, where, device, torch.int32, None)
-    return position, offsets[-1:], position.shape[1]
+    return position, offsets, offsets.data_ptr() + 4 * (offsets.shape[0] - 1), position.shape[1]
 
 
 @_streamed
@@ -324,14 +354,13 @@ def poseidon_expert_gather(x, plan: ExpertPlan, *, keep: bool = False, rows: boo
     x = _rows(x, "poseidon_expert_gather: x")
     n, d = x.shape
     dev, dt = x.device, x.dtype
-    position, kept, k = _plan(plan, "poseidon_expert_gather: plan", dev, n)
+    position, offsets, kept, k = _plan(plan, "poseidon_expert_gather: plan", dev, n)
     xs = torch.empty(n * k, d, dtype=dt, device=dev) if rows else None
-    s = _new_stash(n * k, d, dt, dev) if keep else None
+    s = Stash.empty(n * k, d, dt, dev) if keep else None
     if xs is None and s is None:
         _refuse("poseidon_expert_gather: neither rows nor keep")
     _call("poseidon_expert_gather", dev, x.data_ptr(), _pitch(x), TYPES[dt], n, d, position.data_ptr(), k,
-          kept.data_ptr(), xs.data_ptr() if rows else None, s.codes.data_ptr() if keep else None,
-          s.scales.data_ptr() if keep else None)
+          kept, xs.data_ptr() if rows else None, *(s.addresses() if keep else (None, None)))
     return xs, s
 
 
@@ -342,7 +371,7 @@ def poseidon_expert_combine(ys, plan: ExpertPlan, weights=None, *, out=None) -> 
     ys = _rows(ys, "poseidon_expert_combine: ys").contiguous()
     n = plan.position.shape[0] if isinstance(plan, ExpertPlan) else 0
     dev, dt, d = ys.device, ys.dtype, ys.shape[1]
-    position, _, k = _plan(plan, "poseidon_expert_combine: plan", dev, n)
+    position, _, _, k = _plan(plan, "poseidon_expert_combine: plan", dev, n)
     if ys.shape[0] != n * k:
         _refuse("poseidon_expert_combine: ys: not a row for each choice")
     if weights is not None:
@@ -359,12 +388,12 @@ def poseidon_expert_combine_backward(dout, ys, plan: ExpertPlan, weights) -> Tup
     dout = _rows(dout, "poseidon_expert_combine_backward: dout")
     n, d = dout.shape
     dev, dt = dout.device, dout.dtype
-    position, kept, k = _plan(plan, "poseidon_expert_combine_backward: plan", dev, n)
+    position, offsets, kept, k = _plan(plan, "poseidon_expert_combine_backward: plan", dev, n)
     ys = _rows(ys, "poseidon_expert_combine_backward: ys", dev, dt, (n * k, d)).contiguous()
     weights = _whole(weights, "poseidon_expert_combine_backward: weights", dev, torch.float32, (n, k))
     dys, dweights = torch.empty_like(ys), torch.empty_like(weights)
     _call("poseidon_expert_combine_backward", dev, dout.data_ptr(), _pitch(dout), ys.data_ptr(), TYPES[dt], n, d,
-          position.data_ptr(), k, kept.data_ptr(), weights.data_ptr(), dys.data_ptr(), dweights.data_ptr())
+          position.data_ptr(), k, kept, weights.data_ptr(), dys.data_ptr(), dweights.data_ptr())
     return dys, dweights
 
 
