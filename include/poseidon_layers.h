@@ -88,7 +88,7 @@ int poseidon_gated_backward(const void *dout, uint64_t dout_pitch, uint32_t type
  *   grad[r][o][i] = sum over rows t of the range of dy[t][o] * x[t][i],
  * added to what grad holds where `accumulate` is 1 (the micro-batches of a step).  An empty range gives zeros.
  * offsets: DEVICE int32[n_ranges + 1], non-decreasing, range r = rows [offsets[r], offsets[r + 1]) (each cut to
- *   [0, rows]); NULL with n_ranges == 1: all rows.
+ *   [0, rows]; empty if it ends before it begins); NULL with n_ranges == 1: all rows.
  * type: of dy, POSEIDON_F16 or POSEIDON_BF16; x is brought to it (nothing is lost for POSEIDON_BF16, or if x was
  *   kept from POSEIDON_F16; else what leaves the range of POSEIDON_F16 is held to it).  grad: [n_ranges][out_width][in_width] of
  *   grad_type without gaps. */

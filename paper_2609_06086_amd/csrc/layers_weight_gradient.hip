@@ -153,16 +153,15 @@ __global__ __launch_bounds__(kPlanThreads) void weight_plan_kernel(RunPlan p) {
     }
 #pragma unroll
     for (int i = 0; i < 3; ++i) at[i] = sums[i][tid] - need[i];
-    const uint32_t all = sums[0][kPlanThreads - 1], ranked = all <= kRanked;
-
-    // Offsets that do not ascend could ask for more than there is: what does not fit is left out.
+    // Ranges that overlap (offsets that do not ascend) can ask for more than there is room for: then none is split.
+    const uint32_t last_thread = kPlanThreads - 1;
+    const bool fits = sums[0][last_thread] <= p.max_runs && sums[1][last_thread] <= p.max_splits && sums[2][last_thread] <= p.max_slots;
+    const uint32_t all = fits ? sums[0][last_thread] : p.ranges, ranked = all <= kRanked;
     const auto each_run = [&](auto f) {
-        uint32_t n0 = at[0], n1 = at[1], n2 = at[2];
+        uint32_t n0 = fits ? at[0] : first, n1 = at[1], n2 = at[2];
         for (uint32_t r = first; r < last; ++r) {
             const uint32_t begin = bound(r), end = max(begin, bound(r + 1)), steps = steps_of(begin, end);
-            uint32_t n = max(1u, (steps + p.most - 1) / p.most);
-            if (n > 1 && (n1 >= p.max_splits || n2 + n > p.max_slots)) n = 1;
-            const uint32_t part = (steps + n - 1) / n;
+            const uint32_t n = fits ? max(1u, (steps + p.most - 1) / p.most) : 1, part = (steps + n - 1) / n;
             for (uint32_t i = 0; i < n; ++i) {
                 const uint32_t from = min(begin + i * part * kStep, end), to = min(from + part * kStep, end);
                 f(n0++, Run{r, from, to, n > 1 ? n2 + i : kNone});
@@ -173,7 +172,7 @@ __global__ __launch_bounds__(kPlanThreads) void weight_plan_kernel(RunPlan p) {
             }
         }
     };
-    if (tid == 0) *p.table = RunTable{min(all, p.max_runs), min(sums[1][kPlanThreads - 1], p.max_splits)};
+    if (tid == 0) *p.table = RunTable{all, fits ? sums[1][last_thread] : 0};
     if (ranked) {
         each_run([&](uint32_t i, const Run &r) { length[i] = r.end - r.begin; });
         __syncthreads();
@@ -184,7 +183,7 @@ __global__ __launch_bounds__(kPlanThreads) void weight_plan_kernel(RunPlan p) {
             rank = 0;
             for (uint32_t j = 0; j < all; ++j) rank += length[j] > length[i] || (length[j] == length[i] && j < i);
         }
-        if (rank < p.max_runs) p.runs[rank] = r;
+        p.runs[rank] = r;
     });
 }
 

@@ -198,6 +198,35 @@ def test_weight_gradient_of_ranges(dev, kind, offsets, widths):
         assert torch.equal(one[r], got[r])
 
 
+@pytest.mark.parametrize("rows, offsets", [(300, [0, 300, 0, 300]), (300, [-5, 100, 900, 40]), (20000, [0, 20000, 0, 20000]),
+                                           (20000, [0, 64, 19000, 19000, 20000]), (20000, [100, 19900, 19964])])
+def test_weight_gradient_of_odd_offsets(dev, rows, offsets):
+    """Offsets out of range, out of order or overlapping, and long ranges that are split beside short ones."""
+    rng = np.random.default_rng(9)
+    dy, x = _make(rng, (rows, 72), "bf16", dev, spread=0.5), _make(rng, (rows, 200), "bf16", dev, spread=0.5)
+    s = L.poseidon_stash(x)
+    back = L.poseidon_restore(s, dtype=torch.float32).double()
+    got = L.poseidon_weight_gradient(dy, s, offsets=torch.tensor(offsets, dtype=torch.int32, device=dev))
+    for r, (a, b) in enumerate(zip(offsets, offsets[1:])):
+        a, b = min(max(a, 0), rows), min(max(b, 0), rows)
+        want = (dy[a:b].double().t().contiguous() @ back[a:b]).cpu().numpy() if b > a else np.zeros((72, 200))
+        size = (max(b - a, 0) + 2) * V * (dy[a:b].double().abs().t().contiguous() @ back[a:b].abs()).cpu().numpy() if b > a else 0
+        _check(got[r], want, size, "f32")
+
+
+def test_weight_gradient_of_many_ranges(dev):
+    """More ranges than are ordered by length, most of them empty."""
+    rng = np.random.default_rng(10)
+    ranges, rows = 3000, 2500
+    cuts = np.sort(rng.integers(0, rows + 1, size=ranges + 1))
+    cuts[0], cuts[-1] = 0, rows
+    dy, x = _make(rng, (rows, 8), "f16", dev, spread=0.5), _make(rng, (rows, 24), "f16", dev, spread=0.5)
+    got = L.poseidon_weight_gradient(dy, L.poseidon_stash(x), offsets=torch.from_numpy(cuts.astype(np.int32)).to(dev))
+    back = O.restore(*O.stash(_np(x), "f16"), 24)
+    want = O.weight_gradient(_np(dy), back, cuts)
+    _check(got, want, 70 * V * O.weight_gradient(np.abs(_np(dy)), np.abs(back), cuts), "f32")
+
+
 def test_weight_gradient_over_tiles_and_splits(dev):
     """Sizes of each tile and of rows in one or more parts, the sums' bound on each; NaN spreads along its row and column
     alone."""
