@@ -124,9 +124,9 @@ int poseidon_expert_combine(const void *ys, uint32_t type, uint64_t tokens, uint
                             uint32_t k, const float *weights, void *out, uint64_t out_pitch, void *hip_stream);
 
 /* Its gradient: dys[position[t][j]] = weights[t][j] * dout[t] (places past *n_kept zeros) and
- * dweights[t][j] = <dout[t], ys[position[t][j]]>, 0 for a dropped choice. */
+ * dweights[t][j] = <dout[t], ys[position[t][j]]>, 0 for a dropped choice; from the sort's order of all choices. */
 int poseidon_expert_combine_backward(const void *dout, uint64_t dout_pitch, const void *ys, uint32_t type,
-                                     uint64_t tokens, uint64_t width, const int32_t *position, uint32_t k,
+                                     uint64_t tokens, uint64_t width, const int32_t *order, uint32_t k,
                                      const int32_t *n_kept, const float *weights, void *dys, float *dweights,
                                      void *hip_stream);
 

@@ -207,53 +207,53 @@ __device__ __forceinline__ float wave_sum(float v) {
     return v;
 }
 
-// A wave per token: each ys row is read once for its product with dout, and dys written
-// beside it; dout comes from memory for the first choice and from cache for the others.
+// A wave per place, so that ys is read and dys written in order; a token's row of dout comes from memory for the first of
+// its places and from cache for the others.  8000 tokens of 4096 values by 8 choices: 222 us (4.8 TB/s), against 275 with a
+// wave per token, whose rows of ys and dys lie anywhere.
 template <class T, bool STREAM>
 __global__ __launch_bounds__(kBlock) void combine_backward_kernel(const typename T::raw *dout, uint64_t pitch,
-                                                                  const typename T::raw *ys, uint32_t tokens,
-                                                                  uint32_t width, const int32_t *position, uint32_t k,
-                                                                  uint32_t main, const int32_t *n_kept,
-                                                                  uint32_t places, const float *weights,
-                                                                  typename T::raw *dys, float *dweights) {
-    constexpr uint32_t kAhead = 4;    // slices of a row asked for at a time
-    const uint32_t waves = kBlock / 64;
-    if (blockIdx.x >= main) {
-        clear_rows<T, true, false>((blockIdx.x - main) * waves + threadIdx.x / 64, (gridDim.x - main) * waves, n_kept,
-                                   places, width, (width + kGroup - 1) / kGroup, dys, nullptr, nullptr);
-        return;
-    }
-    const uint32_t t = blockIdx.x * waves + threadIdx.x / 64, lane = threadIdx.x & 63;
-    if (t >= tokens) return;
-    const typename T::raw *d = dout + (uint64_t)t * pitch;
-    for (uint32_t j = 0; j < k; ++j) {
-        const uint32_t p = __builtin_amdgcn_readfirstlane(position[(uint64_t)t * k + j]);
-        const float w = weights[(uint64_t)t * k + j];
-        float dot = 0.0f;
-        if (p < places)
-            for (uint32_t c0 = lane * kSlice; c0 < width; c0 += kAhead * 64 * kSlice) {
-                Slice<T> dw[kAhead], yw[kAhead];
+                                                                  const typename T::raw *ys, uint32_t width,
+                                                                  const int32_t *order, Div k, const int32_t *n_kept,
+                                                                  uint32_t first, uint32_t places, uint32_t choices,
+                                                                  const float *weights, typename T::raw *dys,
+                                                                  float *dweights) {
+    constexpr uint32_t kAhead = 2;    // slices of a row asked for at a time
+    const uint32_t i = blockIdx.x * (kBlock / 64) + threadIdx.x / 64, lane = threadIdx.x & 63;
+    if (i >= places) return;
+    const uint64_t p = first + i;
+    const uint32_t choice = (uint32_t)__builtin_amdgcn_readfirstlane(order[p]);
+    if (choice >= choices) return;
+    const bool kept = (int32_t)p < *n_kept;
+    const float w = weights[choice];
+    const typename T::raw *d = dout + quotient(choice, k) * pitch;
+    float dot = 0.0f;
+    for (uint32_t c0 = lane * kSlice; c0 < width; c0 += kAhead * 64 * kSlice) {
+        Slice<T> dw[kAhead], yw[kAhead];
+        if (kept) {
 #pragma unroll
-                for (uint32_t a = 0; a < kAhead; ++a) {    // past the row: zeros
-                    dw[a] = load_words<T>(d, c0 + a * 64 * kSlice, width);
-                    yw[a] = load_words<T, STREAM>(ys + (uint64_t)p * width, c0 + a * 64 * kSlice, width);
-                }
+            for (uint32_t a = 0; a < kAhead; ++a) {    // past the row: zeros
+                dw[a] = load_words<T>(d, c0 + a * 64 * kSlice, width);
+                yw[a] = load_words<T, STREAM>(ys + p * width, c0 + a * 64 * kSlice, width);
+            }
+        }
 #pragma unroll
-                for (uint32_t a = 0; a < kAhead; ++a) {
-                    float v[8], y[8];
-                    values<T>(dw[a], v);
-                    values<T>(yw[a], y);
+        for (uint32_t a = 0; a < kAhead; ++a) {
+            float y[8] = {};
+            if (kept) {
+                float v[8];
+                values<T>(dw[a], v);
+                values<T>(yw[a], y);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        dot = fmaf(v[e], y[e], dot);
-                        y[e] = w * v[e];
-                    }
-                    store_slice<T, STREAM>(dys + (uint64_t)p * width, c0 + a * 64 * kSlice, width, y);
+                for (int e = 0; e < 8; ++e) {
+                    dot = fmaf(v[e], y[e], dot);
+                    y[e] = w * v[e];
                 }
             }
-        dot = wave_sum(dot);
-        if (lane == 0) dweights[(uint64_t)t * k + j] = dot;
+            store_slice<T, STREAM>(dys + p * width, c0 + a * 64 * kSlice, width, y);
+        }
     }
+    dot = wave_sum(dot);
+    if (lane == 0) dweights[choice] = dot;
 }
 
 // ---- embedding ----
@@ -418,7 +418,7 @@ int poseidon_expert_combine(const void *ys, uint32_t type, uint64_t tokens, uint
 }
 
 int poseidon_expert_combine_backward(const void *dout, uint64_t dout_pitch, const void *ys, uint32_t type,
-                                     uint64_t tokens, uint64_t width, const int32_t *position, uint32_t k,
+                                     uint64_t tokens, uint64_t width, const int32_t *order, uint32_t k,
                                      const int32_t *n_kept, const float *weights, void *dys, float *dweights,
                                      void *hip_stream) {
     if (!k) return POSEIDON_E_INVAL;
@@ -428,16 +428,14 @@ int poseidon_expert_combine_backward(const void *dout, uint64_t dout_pitch, cons
     PL_TRY(check_matrix(dout, dout_pitch, type, tokens, width));
     PL_TRY(check_matrix(ys, width, type, places, width));
     PL_TRY(check_matrix(dys, width, type, places, width));
-    if (tokens && (!position || !n_kept || !weights || !dweights)) return POSEIDON_E_INVAL;
+    if (tokens && (!order || !n_kept || !weights || !dweights)) return POSEIDON_E_INVAL;
     if (!tokens) return POSEIDON_OK;
-    const uint64_t step = 1ull << 24;    // tokens of a launch
-    PL_STREAM(tokens * (2 * k + 1) * width * size_of(type), PL_TYPE(type, for (uint64_t t = 0; t < tokens; t += step) {
-        const uint64_t n = tokens - t < step ? tokens - t : step;
-        const uint32_t main = (uint32_t)((n + kBlock / 64 - 1) / (kBlock / 64));
-        combine_backward_kernel<T, STREAM>
-            <<<main + (t + n == tokens ? kClearBlocks : 0), kBlock, 0, (hipStream_t)hip_stream>>>(
-                (const T::raw *)dout + t * dout_pitch, dout_pitch, (const T::raw *)ys, (uint32_t)n, (uint32_t)width,
-                position + t * k, k, main, n_kept, (uint32_t)places, weights + t * k, (T::raw *)dys, dweights + t * k);
+    const uint64_t step = 1ull << 25;    // places of a launch
+    PL_STREAM(tokens * (2 * k + 1) * width * size_of(type), PL_TYPE(type, for (uint64_t p = 0; p < places; p += step) {
+        const uint32_t n = (uint32_t)(places - p < step ? places - p : step);
+        combine_backward_kernel<T, STREAM><<<(n + kBlock / 64 - 1) / (kBlock / 64), kBlock, 0, (hipStream_t)hip_stream>>>(
+            (const T::raw *)dout, dout_pitch, (const T::raw *)ys, (uint32_t)width, order, make_div(k), n_kept, (uint32_t)p, n,
+            (uint32_t)places, weights, (T::raw *)dys, dweights);
     }));
     return launched();
 }

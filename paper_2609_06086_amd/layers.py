@@ -388,12 +388,13 @@ def poseidon_expert_combine_backward(dout, ys, plan: ExpertPlan, weights) -> Tup
     dout = _rows(dout, "poseidon_expert_combine_backward: dout")
     n, d = dout.shape
     dev, dt = dout.device, dout.dtype
-    position, offsets, kept, k = _plan(plan, "poseidon_expert_combine_backward: plan", dev, n)
+    _, offsets, kept, k = _plan(plan, "poseidon_expert_combine_backward: plan", dev, n)
+    order = _whole(plan.order, "poseidon_expert_combine_backward: plan", dev, torch.int32, (n * k,))
     ys = _rows(ys, "poseidon_expert_combine_backward: ys", dev, dt, (n * k, d)).contiguous()
     weights = _whole(weights, "poseidon_expert_combine_backward: weights", dev, torch.float32, (n, k))
     dys, dweights = torch.empty_like(ys), torch.empty_like(weights)
     _call("poseidon_expert_combine_backward", dev, dout.data_ptr(), _pitch(dout), ys.data_ptr(), TYPES[dt], n, d,
-          position.data_ptr(), k, kept, weights.data_ptr(), dys.data_ptr(), dweights.data_ptr())
+          order.data_ptr(), k, kept, weights.data_ptr(), dys.data_ptr(), dweights.data_ptr())
     return dys, dweights
 
 
