@@ -36,20 +36,24 @@ struct Clear {
     uint64_t rows, bytes, pitch;
 };
 
-// Block `block`: a row, or of one row (a table without gaps) a piece of 16 bytes a thread.  Many blocks of one
-// store a thread fill at 6.7 TB/s, blocks that go on through the memory in strides at 4.4 to 5.6.
-__device__ __forceinline__ void clear(const Clear &c, uint32_t block) {
+// Block `block` of `blocks`: a row, or of one row (a table without gaps) a piece of 16 bytes a thread, and what lies
+// whole grids further.  Many blocks of one store a thread fill at 6.7 TB/s, blocks that go on through the memory in
+// strides at 4.4 to 5.6: only above kClearMost blocks (64 GB without gaps) do they go on.
+constexpr uint64_t kClearPiece = (uint64_t)kSortThreads * 16, kClearMost = 1u << 22;
+
+__device__ __forceinline__ void clear(const Clear &c, uint32_t block, uint32_t blocks) {
     const uint4 zero = make_uint4(0, 0, 0, 0);
     const bool flat = c.rows == 1;
-    const uint64_t step = (uint64_t)kSortThreads * 16;
-    char *row = c.to + (flat ? 0 : block * c.pitch);
-    for (uint64_t at = (flat ? block * step : 0) + threadIdx.x * 16u; at < c.bytes; at += step) {
-        if (at + 16 <= c.bytes) {
-            __builtin_memcpy(row + at, &zero, 16);
-        } else {
-            for (uint64_t i = at; i < c.bytes; i += 2) *(uint16_t *)(row + i) = 0;
+    const uint64_t step = flat ? blocks * kClearPiece : kClearPiece;
+    for (uint64_t r = flat ? 0 : block; r < c.rows; r += flat ? 1 : blocks) {
+        char *row = c.to + r * c.pitch;
+        for (uint64_t at = (flat ? block * kClearPiece : 0) + threadIdx.x * 16u; at < c.bytes; at += step) {
+            if (at + 16 <= c.bytes) {
+                __builtin_memcpy(row + at, &zero, 16);
+            } else {
+                for (uint64_t i = at; i < c.bytes; i += 2) *(uint16_t *)(row + i) = 0;
+            }
         }
-        if (flat) break;
     }
 }
 
@@ -60,7 +64,7 @@ __device__ __forceinline__ uint32_t key_at(const SortPass &p, uint32_t i) {
 
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortPass p, Clear c) {
     __shared__ uint32_t count[kMaxBins];
-    if (blockIdx.x >= p.blocks) return clear(c, blockIdx.x - p.blocks);
+    if (blockIdx.x >= p.blocks) return clear(c, blockIdx.x - p.blocks, gridDim.x - p.blocks);
     for (uint32_t b = threadIdx.x; b < p.bins; b += kSortThreads) count[b] = 0;
     __syncthreads();
     const uint32_t first = blockIdx.x * (kSortThreads * p.rounds);
@@ -119,7 +123,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortPass p, Cl
     __shared__ uint32_t count[kSortWaves][kMaxBins];
     __shared__ uint32_t wave_sums[kSortWaves];
     __shared__ uint32_t moved[SOLO ? 2 : 1][SOLO ? kSortTile : 1];
-    if (blockIdx.x >= p.blocks) return clear(c, blockIdx.x - p.blocks);
+    if (blockIdx.x >= p.blocks) return clear(c, blockIdx.x - p.blocks, gridDim.x - p.blocks);
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
     const uint32_t first = (blockIdx.x * kSortWaves + wave) * (64 * p.rounds);
     const uint32_t rounds = first < p.m ? min((p.m - first + 63) / 64, p.rounds) : 0;    // of this wave
@@ -246,8 +250,8 @@ inline uint64_t sort_counts_bytes(uint64_t m) { return round_up(((uint64_t)sort_
 
 // Blocks that clear beside a sort's, and part i of n of a clear.
 inline uint32_t clear_blocks(const Clear &c) {
-    const uint64_t step = (uint64_t)kSortThreads * 16;
-    return (uint32_t)(c.rows == 1 ? (c.bytes + step - 1) / step : c.rows);
+    const uint64_t n = c.rows == 1 ? (c.bytes + kClearPiece - 1) / kClearPiece : c.rows;
+    return (uint32_t)(n < kClearMost ? n : kClearMost);
 }
 inline Clear part_of(const Clear &c, uint64_t i, uint64_t n) {
     Clear p = c;
@@ -269,10 +273,11 @@ struct SortLists {
     int32_t *keys[2], *order[2];
 };
 
-inline void sort(SortPass p, const SortLists &lists, const Clear &c, hipStream_t stream) {
+// A launch that fails ends the sort: the next one would take its counts from memory that nothing wrote.
+inline int sort(SortPass p, const SortLists &lists, const Clear &c, hipStream_t stream) {
     if (p.blocks == 1) {
         sort_place_kernel<true><<<1 + clear_blocks(c), kSortThreads, 0, stream>>>(p, c);
-        return;
+        return launched();
     }
     const bool scan = p.blocks > kSelfScan;
     uint32_t *const totals = p.counts + (uint64_t)p.blocks * p.bins;
@@ -289,13 +294,17 @@ inline void sort(SortPass p, const SortLists &lists, const Clear &c, hipStream_t
         p.shift = i * p.bits;
         const Clear a = part_of(c, 2 * i, 2 * p.passes), b = part_of(c, 2 * i + 1, 2 * p.passes);
         sort_count_kernel<<<p.blocks + clear_blocks(a), kSortThreads, 0, stream>>>(p, a);
+        PL_TRY(launched());
         if (scan) {
             SortPass q = p;
             q.totals = totals;
             sort_scan_kernel<<<p.bins, 256, 0, stream>>>(q);
+            PL_TRY(launched());
         }
         sort_place_kernel<false><<<p.blocks + clear_blocks(b), kSortThreads, 0, stream>>>(p, b);
+        PL_TRY(launched());
     }
+    return POSEIDON_OK;
 }
 
 // ---- gradient of an embedding ----
@@ -488,8 +497,7 @@ int poseidon_expert_sort(const int32_t *choice, uint64_t tokens, uint32_t k, uin
     p.order = order;
     p.position = position;
     p.offsets = offsets;
-    sort(p, {}, {}, (hipStream_t)hip_stream);
-    return launched();
+    return sort(p, {}, {}, (hipStream_t)hip_stream);
 }
 
 uint64_t poseidon_embed_backward_workspace(uint64_t tokens, uint64_t vocab, uint64_t width) {
@@ -540,8 +548,8 @@ int poseidon_embed_backward(const int32_t *ids, uint64_t tokens, const void *dou
     }
     p.keys_out = lists.keys[(p.passes - 1) & 1];
     p.order = lists.order[(p.passes - 1) & 1];
-    sort(p, lists, c, stream);
-    if (!m) return launched();
+    PL_TRY(sort(p, lists, c, stream));
+    if (!m) return POSEIDON_OK;
 
     EmbedGrad e = {};
     e.keys = p.keys_out;

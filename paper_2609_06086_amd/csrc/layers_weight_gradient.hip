@@ -607,6 +607,7 @@ int poseidon_weight_gradient(const void *dy, uint64_t dy_pitch, uint32_t type, u
         g.runs = r.runs;
         g.splits = r.splits;
         weight_plan_kernel<<<1, kPlanThreads, 0, stream>>>(r);
+        PL_TRY(launched());    // the next kernel reads the table
     }
     const uint32_t blocks = (uint32_t)(p.tiles_o * p.tiles_i * p.max_runs);
     const uint64_t joins = (out_width * in_width + kBlock - 1) / kBlock;

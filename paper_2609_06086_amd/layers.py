@@ -52,11 +52,13 @@ def lib():
     """The loaded HIP library, with the layer operators' signatures."""
     L = P.lib()
     if not _functions:
+        made = {}
         for name, args in _ARGS.items():
             f = getattr(L, name)
             f.argtypes = args
             f.restype = _u64 if name.endswith("_workspace") else C.c_int
-            _functions[name] = f
+            made[name] = f
+        _functions.update(made)    # all at once: other threads may be at it too
     return L
 
 
@@ -140,15 +142,16 @@ def _streamed(f):
     def g(*args, stream=None, **kw):
         if stream is None:
             return f(*args, **kw)
+        held = [t for a in (*args, *kw.values())
+                for t in ((a,) if isinstance(a, torch.Tensor) else a.tensors() if isinstance(a, (Stash, ExpertPlan)) else ())
+                if t.is_cuda]
         if not isinstance(stream, torch.cuda.Stream):
-            stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+            device = held[0].device if held else None    # a raw stream is one of the tensors' GPU
+            stream = torch.cuda.ExternalStream(stream, device) if stream else torch.cuda.default_stream(device)
         with torch.cuda.stream(stream):
             out = f(*args, **kw)
-        for a in (*args, *kw.values()):
-            parts = (a,) if isinstance(a, torch.Tensor) else a.tensors() if isinstance(a, (Stash, ExpertPlan)) else ()
-            for t in parts:
-                if t.is_cuda:
-                    t.record_stream(stream)
+        for t in held:
+            t.record_stream(stream)
         return out
 
     return g

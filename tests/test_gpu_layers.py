@@ -370,6 +370,34 @@ def test_embedding_gradient_of_one_token(dev, tokens):
     assert (L.poseidon_embed_backward(ids - 9, dout, 5) == 0).all()
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("vocab", [7, 1000, (1 << 22) + 5, (1 << 23) + 700])
+def test_embedding_gradient_into_rows_with_gaps(dev, kind, vocab):
+    """Rows of no token become zeros, the gaps between the rows stay: also with more rows than blocks that clear them."""
+    wide = torch.full((vocab, 6), 7.0, dtype=KIND[kind], device=dev)
+    out = wide[:, 1:4]
+    ids = torch.tensor([vocab - 1, 2, -1, vocab - 1, vocab], dtype=torch.int32, device=dev)
+    dout = torch.arange(15, device=dev).view(5, 3).to(KIND[kind])
+    L.poseidon_embed_backward(ids, dout, vocab, 2.0, out=out)
+    assert torch.equal(out[-1], 2 * (dout[0] + dout[3])) and torch.equal(out[2], 2 * dout[1])
+    assert out.count_nonzero() == out[-1].count_nonzero() + out[2].count_nonzero()
+    assert (wide[:, 0] == 7).all() and (wide[:, 4:] == 7).all()
+
+
+def test_embedding_gradient_of_a_table_past_32_gib(dev):
+    """A table without gaps that takes more than one store a thread to clear."""
+    vocab, width = 1 << 23, 1200
+    if torch.cuda.mem_get_info(dev)[0] < 60 << 30:
+        pytest.skip("not enough memory")
+    out = torch.full((vocab, width), 7.0, dtype=torch.float32, device=dev)
+    ids = torch.tensor([vocab - 1, 0], dtype=torch.int32, device=dev)
+    dout = torch.ones(2, width, dtype=torch.float32, device=dev)
+    L.poseidon_embed_backward(ids, dout, vocab, out=out)
+    assert (out[-1] == 1).all() and (out[0] == 1).all()
+    for a in range(1, vocab - 1, 1 << 20):
+        assert not out[a:min(a + (1 << 20), vocab - 1)].any()
+
+
 # ---- addresses, streams, graphs ----
 
 def test_offsets_past_32_bits(dev):
