@@ -440,11 +440,13 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedGrad e) {
     write_sum<G>(e, key, col, sum);
 }
 
-// Places a block adds up: few tokens are spread over more blocks.
-// Past 2^25 of them the chunks grow, so that there are at most 2^20.
-inline uint32_t chunk_of(uint64_t tokens) {
-    if (tokens <= 4096) return 8;
-    return tokens <= 1ull << 25 ? 32u : (uint32_t)round_up((tokens + (1u << 20) - 1) >> 20, 8);
+// Places a block adds up: as many as leave 4096 waves, which fill the chip, from 8 to 32 (past 2^25 tokens more, so that there
+// are at most 2^20 chunks).
+inline uint32_t chunk_of(uint64_t tokens, uint64_t width) {
+    const uint64_t columns = (width + 64 * kSlice - 1) / (64 * kSlice);
+    uint32_t chunk = 8;
+    while (chunk < 32 && chunk * 4096ull < tokens * columns) chunk *= 2;
+    return tokens <= 1ull << 25 ? chunk : (uint32_t)round_up((tokens + (1u << 20) - 1) >> 20, 8);
 }
 
 struct EmbedWorkspace {
@@ -454,7 +456,7 @@ struct EmbedWorkspace {
 inline EmbedWorkspace embed_workspace(uint64_t m, uint64_t width) {
     EmbedWorkspace w;
     const uint64_t list = round_up(m * 4, 256), padded = (width + kSlice - 1) / kSlice * kSlice;
-    const uint64_t chunks = (m + chunk_of(m) - 1) / chunk_of(m);
+    const uint64_t chunk = chunk_of(m, width), chunks = (m + chunk - 1) / chunk;
     w.counts = 0;
     w.keys[0] = sort_counts_bytes(m);
     w.keys[1] = w.keys[0] + list;
@@ -557,7 +559,7 @@ int poseidon_embed_backward(const int32_t *ids, uint64_t tokens, const void *dou
     e.m = m;
     e.vocab = (uint32_t)vocab;
     e.width = (uint32_t)width;
-    e.chunk = chunk_of(tokens);
+    e.chunk = chunk_of(tokens, width);
     e.chunks = (m + e.chunk - 1) / e.chunk;
     e.accumulate = accumulate;
     e.scale = scale;

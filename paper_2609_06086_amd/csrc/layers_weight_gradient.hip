@@ -112,6 +112,8 @@ __device__ __forceinline__ Unit unit_of(const WeightGrad &g) {
 // The runs of ragged ranges: a range of more than `most` steps becomes several of about the
 // same length, and of up to kRanked runs the longest come first, so that none is left for the
 // end.  One block.  An empty range is a run too, which writes its zeros.
+// It is one long chain of waits, so few ranges get few waves, and the lengths that a run is compared with come sixteen at a
+// time (64 ranges: 6 us, 8 to 9 one at a time in 16 waves).
 constexpr uint32_t kPlanThreads = 1024, kRanked = 1024;
 
 struct RunPlan {
@@ -125,10 +127,13 @@ struct RunPlan {
 
 __global__ __launch_bounds__(kPlanThreads) void weight_plan_kernel(RunPlan p) {
     __shared__ uint32_t sums[3][kPlanThreads / 64];
-    __shared__ uint32_t length[kRanked];
-    const uint32_t tid = threadIdx.x, each = (p.ranges + kPlanThreads - 1) / kPlanThreads;
+    __shared__ uint4 lengths[kRanked / 4];
+    uint32_t *const length = (uint32_t *)lengths;
+    const uint32_t tid = threadIdx.x, waves = blockDim.x / 64, each = (p.ranges + blockDim.x - 1) / blockDim.x;
     const uint32_t first = min(tid * each, p.ranges), last = min(first + each, p.ranges);
-    const auto bound = [&](uint32_t r) { return (uint32_t)min(max(p.offsets[r], 0), (int32_t)p.rows); };
+    const auto read_bound = [&](uint32_t r) { return (uint32_t)min(max(p.offsets[r], 0), (int32_t)p.rows); };
+    const uint32_t own[2] = {read_bound(first), read_bound(min(first + 1, p.ranges))};    // read once where a thread has one range
+    const auto bound = [&](uint32_t r) { return r - first < 2 ? own[r - first] : read_bound(r); };
     const auto steps_of = [&](uint32_t begin, uint32_t end) { return end > begin ? (end - begin + kStep - 1) / kStep : 0u; };
 
     // how many runs, split ranges and slots the thread's ranges need, and those before it
@@ -156,7 +161,7 @@ __global__ __launch_bounds__(kPlanThreads) void weight_plan_kernel(RunPlan p) {
     for (int i = 0; i < 3; ++i) {
         total[i] = 0;
         uint32_t before = 0;
-        for (uint32_t w = 0; w < kPlanThreads / 64; ++w) {
+        for (uint32_t w = 0; w < waves; ++w) {
             before += w < tid / 64 ? sums[i][w] : 0;
             total[i] += sums[i][w];
         }
@@ -183,6 +188,7 @@ __global__ __launch_bounds__(kPlanThreads) void weight_plan_kernel(RunPlan p) {
     };
     if (tid == 0) *p.table = RunTable{all, fits ? total[1] : 0};
     if (ranked) {
+        if (tid < 16 && all + tid < kRanked) length[all + tid] = 0;
         each_run([&](uint32_t i, const Run &r) { length[i] = r.end - r.begin; });
         __syncthreads();
     }
@@ -190,7 +196,18 @@ __global__ __launch_bounds__(kPlanThreads) void weight_plan_kernel(RunPlan p) {
         uint32_t rank = i;
         if (ranked) {
             rank = 0;
-            for (uint32_t j = 0; j < all; ++j) rank += length[j] > length[i] || (length[j] == length[i] && j < i);
+            const uint32_t mine = r.end - r.begin;
+            for (uint32_t j = 0; j < all; j += 16) {    // past the last run: lengths of 0
+                uint4 u[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) u[q] = lengths[j / 4 + q];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t l[4] = {u[q].x, u[q].y, u[q].z, u[q].w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) rank += l[e] > mine || (l[e] == mine && j + 4 * q + e < i);
+                }
+            }
         }
         p.runs[rank] = r;
     });
@@ -606,7 +623,8 @@ int poseidon_weight_gradient(const void *dy, uint64_t dy_pitch, uint32_t type, u
         g.table = r.table;
         g.runs = r.runs;
         g.splits = r.splits;
-        weight_plan_kernel<<<1, kPlanThreads, 0, stream>>>(r);
+        const uint32_t threads = n_ranges < kPlanThreads ? (n_ranges + 63) / 64 * 64 : kPlanThreads;
+        weight_plan_kernel<<<1, threads, 0, stream>>>(r);
         PL_TRY(launched());    // the next kernel reads the table
     }
     const uint32_t blocks = (uint32_t)(p.tiles_o * p.tiles_i * p.max_runs);

@@ -180,33 +180,33 @@ def _workspace(name: str, device: torch.device, *sizes):
     return w, w.data_ptr(), n
 
 
-def _rows(x, where: str, device=None, dtype=None, shape=None) -> torch.Tensor:
-    """A matrix operand with neighbouring values in a row (copied if it has none)."""
+def _rows(x, where: str, device=None, dtype=None, shape=None):
+    """A matrix operand with neighbouring values in a row (copied if it has none): (x, rows, width, pitch)."""
     if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dim() != 2 or x.dtype not in TYPES:
         _refuse(f"{where}: not a 2-D float32, float16 or bfloat16 tensor on the GPU")
+    n, d = size = x.shape
     if (device is not None and x.device != device) or (dtype is not None and x.dtype != dtype) or \
-            (shape is not None and x.shape != shape):
+            (shape is not None and size != shape):
         _refuse(f"{where}: device, type or shape differs from what the others ask for")
-    return x if _pitched(x) else x.contiguous()
+    pitch, step = x.stride()
+    if n <= 1:
+        pitch = d
+    if (step != 1 and d > 1) or pitch < d:
+        return x.contiguous(), n, d, d
+    return x, n, d, pitch
 
 
-def _pitched(x) -> bool:
-    rows, width = x.shape
-    return (width <= 1 or x.stride(1) == 1) and (rows <= 1 or x.stride(0) >= width)
-
-
-def _pitch(x) -> int:
-    return max(x.stride(0), x.shape[1]) if x.shape[0] > 1 else x.shape[1]
-
-
-def _out(out, where: str, device, dtype, shape) -> torch.Tensor:
-    """An output the caller brought, or a new one."""
+def _out(out, where: str, device, dtype, n: int, d: int):
+    """A matrix that the caller brought for a result, or a new one: (out, pitch)."""
     if out is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    if not isinstance(out, torch.Tensor) or out.device != device or out.dtype != dtype or \
-            out.shape != shape or not (_pitched(out) if out.dim() == 2 else out.is_contiguous()):
-        _refuse(f"{where}: device, type, shape or layout differs from the result's")
-    return out
+        return torch.empty((n, d), dtype=dtype, device=device), d
+    if isinstance(out, torch.Tensor) and out.device == device and out.dtype == dtype and out.shape == (n, d):
+        pitch, step = out.stride()
+        if n <= 1:
+            pitch = d
+        if (step == 1 or d <= 1) and pitch >= d:
+            return out, pitch
+    _refuse(f"{where}: device, type, shape or layout differs from the result's")
 
 
 def _whole(x, where: str, device, dtype, shape) -> torch.Tensor:
@@ -238,10 +238,10 @@ def _stash(s, where: str, device, rows=None, width=None) -> Stash:
 @_streamed
 def poseidon_stash(x) -> Stash:
     """Rows of x [rows, width] kept in 8 bits."""
-    x = _rows(x, "poseidon_stash: x")
-    n, d = x.shape
-    s = Stash.empty(n, d, x.dtype, x.device)
-    _call("poseidon_stash", x.device, x.data_ptr(), _pitch(x), TYPES[x.dtype], n, d, *s.addresses())
+    x, n, d, pitch = _rows(x, "poseidon_stash: x")
+    dev, dt = x.device, x.dtype
+    s = Stash.empty(n, d, dt, dev)
+    _call("poseidon_stash", dev, x.data_ptr(), pitch, TYPES[dt], n, d, *s.addresses())
     return s
 
 
@@ -255,39 +255,37 @@ def poseidon_restore(stash: Stash, *, dtype=None, out=None) -> torch.Tensor:
         _refuse("poseidon_restore: a float32, float16 or bfloat16 result")
     device = stash.device
     s = _stash(stash, "poseidon_restore: stash", device)
-    out = _out(out, "poseidon_restore: out", device, dtype, (s.rows, s.width))
-    _call("poseidon_restore", device, *s.addresses(), s.rows, s.width, out.data_ptr(), _pitch(out), TYPES[dtype])
+    out, pitch = _out(out, "poseidon_restore: out", device, dtype, s.rows, s.width)
+    _call("poseidon_restore", device, *s.addresses(), s.rows, s.width, out.data_ptr(), pitch, TYPES[dtype])
     return out
 
 
 @_streamed
 def poseidon_gated_forward(gate, up, *, keep: bool = True, out=None) -> Tuple[torch.Tensor, Optional[Stash], Optional[Stash]]:
     """(silu(gate) * up, gate kept in 8 bits, up kept in 8 bits); without `keep` the latter are None."""
-    gate = _rows(gate, "poseidon_gated_forward: gate")
-    n, d = gate.shape
+    gate, n, d, gate_pitch = _rows(gate, "poseidon_gated_forward: gate")
     dev, dt = gate.device, gate.dtype
-    up = _rows(up, "poseidon_gated_forward: up", dev, dt, (n, d))
-    out = _out(out, "poseidon_gated_forward: out", dev, dt, (n, d))
+    up, _, _, up_pitch = _rows(up, "poseidon_gated_forward: up", dev, dt, (n, d))
+    out, pitch = _out(out, "poseidon_gated_forward: out", dev, dt, n, d)
     sg = Stash.empty(n, d, dt, dev) if keep else None
     su = Stash.empty(n, d, dt, dev) if keep else None
     kept = sg.addresses() + su.addresses() if keep else (None,) * 4
-    _call("poseidon_gated_forward", dev, gate.data_ptr(), _pitch(gate), up.data_ptr(), _pitch(up), TYPES[dt], n, d,
-          out.data_ptr(), _pitch(out), *kept)
+    _call("poseidon_gated_forward", dev, gate.data_ptr(), gate_pitch, up.data_ptr(), up_pitch, TYPES[dt], n, d,
+          out.data_ptr(), pitch, *kept)
     return out, sg, su
 
 
 @_streamed
 def poseidon_gated_backward(dout, gate: Stash, up: Stash, *, dgate=None, dup=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """(dgate, dup) at the kept gate and up."""
-    dout = _rows(dout, "poseidon_gated_backward: dout")
-    n, d = dout.shape
+    dout, n, d, pitch = _rows(dout, "poseidon_gated_backward: dout")
     dev, dt = dout.device, dout.dtype
     gate = _stash(gate, "poseidon_gated_backward: gate", dev, n, d)
     up = _stash(up, "poseidon_gated_backward: up", dev, n, d)
-    dgate = _out(dgate, "poseidon_gated_backward: dgate", dev, dt, (n, d))
-    dup = _out(dup, "poseidon_gated_backward: dup", dev, dt, (n, d))
-    _call("poseidon_gated_backward", dev, dout.data_ptr(), _pitch(dout), TYPES[dt], n, d, *gate.addresses(),
-          *up.addresses(), dgate.data_ptr(), _pitch(dgate), dup.data_ptr(), _pitch(dup))
+    dgate, dgate_pitch = _out(dgate, "poseidon_gated_backward: dgate", dev, dt, n, d)
+    dup, dup_pitch = _out(dup, "poseidon_gated_backward: dup", dev, dt, n, d)
+    _call("poseidon_gated_backward", dev, dout.data_ptr(), pitch, TYPES[dt], n, d, *gate.addresses(),
+          *up.addresses(), dgate.data_ptr(), dgate_pitch, dup.data_ptr(), dup_pitch)
     return dgate, dup
 
 
@@ -296,8 +294,7 @@ def poseidon_weight_gradient(dy, x: Stash, *, offsets=None, dtype=torch.float32,
                              accumulate: bool = False) -> torch.Tensor:
     """dy^T x from the kept x: [out_width, in_width], or with int32 offsets [ranges + 1] one for each range of rows,
     [ranges, out_width, in_width].  With accumulate it is added to `out`."""
-    dy = _rows(dy, "poseidon_weight_gradient: dy")
-    n, o = dy.shape
+    dy, n, o, pitch = _rows(dy, "poseidon_weight_gradient: dy")
     dev = dy.device
     x = _stash(x, "poseidon_weight_gradient: x", dev, n)
     if accumulate and out is None:
@@ -308,16 +305,17 @@ def poseidon_weight_gradient(dy, x: Stash, *, offsets=None, dtype=torch.float32,
         if offsets.dim() != 1 or offsets.numel() < 2:
             _refuse("poseidon_weight_gradient: offsets: not int32 [ranges + 1]")
         ranges = offsets.numel() - 1
-    dtype = dtype if out is None else out.dtype
+    dtype = dtype if out is None else getattr(out, "dtype", None)
     if dtype not in TYPES:
         _refuse("poseidon_weight_gradient: a float32, float16 or bfloat16 result")
     shape = (o, x.width) if offsets is None else (ranges, o, x.width)
-    out = _out(out, "poseidon_weight_gradient: out", dev, dtype, shape)
-    if not out.is_contiguous():
-        _refuse("poseidon_weight_gradient: out has gaps")
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=dev)
+    elif out.device != dev or out.shape != shape or not out.is_contiguous():
+        _refuse("poseidon_weight_gradient: out: device, shape or layout differs from the result's")
     w, at, size = _workspace("poseidon_weight_gradient", dev, n, o, x.width, ranges)
-    _call("poseidon_weight_gradient", dev, dy.data_ptr(), _pitch(dy), TYPES[dy.dtype], n, o, *x.addresses(), x.width, None if offsets is None else offsets.data_ptr(), ranges, out.data_ptr(),
-          TYPES[dtype], int(accumulate), at, size)
+    _call("poseidon_weight_gradient", dev, dy.data_ptr(), pitch, TYPES[dy.dtype], n, o, *x.addresses(), x.width,
+          None if offsets is None else offsets.data_ptr(), ranges, out.data_ptr(), TYPES[dtype], int(accumulate), at, size)
     return out
 
 
@@ -354,15 +352,14 @@ def _plan(plan, where: str, device, tokens: int):
 @_streamed
 def poseidon_expert_gather(x, plan: ExpertPlan, *, keep: bool = False, rows: bool = True):
     """(x by expert [tokens * k, width], or None without `rows`; the same rows kept in 8 bits, or None without `keep`)."""
-    x = _rows(x, "poseidon_expert_gather: x")
-    n, d = x.shape
+    x, n, d, pitch = _rows(x, "poseidon_expert_gather: x")
     dev, dt = x.device, x.dtype
     position, offsets, kept, k = _plan(plan, "poseidon_expert_gather: plan", dev, n)
     xs = torch.empty(n * k, d, dtype=dt, device=dev) if rows else None
     s = Stash.empty(n * k, d, dt, dev) if keep else None
     if xs is None and s is None:
         _refuse("poseidon_expert_gather: neither rows nor keep")
-    _call("poseidon_expert_gather", dev, x.data_ptr(), _pitch(x), TYPES[dt], n, d, position.data_ptr(), k,
+    _call("poseidon_expert_gather", dev, x.data_ptr(), pitch, TYPES[dt], n, d, position.data_ptr(), k,
           kept, xs.data_ptr() if rows else None, *(s.addresses() if keep else (None, None)))
     return xs, s
 
@@ -371,32 +368,33 @@ def poseidon_expert_gather(x, plan: ExpertPlan, *, keep: bool = False, rows: boo
 def poseidon_expert_combine(ys, plan: ExpertPlan, weights=None, *, out=None) -> torch.Tensor:
     """sum over a token's choices of weight * ys row, [tokens, width]; without weights (float32 [tokens, k]) each
     counts once, which is the gradient of the gather."""
-    ys = _rows(ys, "poseidon_expert_combine: ys").contiguous()
+    ys, places, d, pitch = _rows(ys, "poseidon_expert_combine: ys")
+    ys = ys if pitch == d else ys.contiguous()
     n = plan.position.shape[0] if isinstance(plan, ExpertPlan) else 0
-    dev, dt, d = ys.device, ys.dtype, ys.shape[1]
+    dev, dt = ys.device, ys.dtype
     position, _, _, k = _plan(plan, "poseidon_expert_combine: plan", dev, n)
-    if ys.shape[0] != n * k:
+    if places != n * k:
         _refuse("poseidon_expert_combine: ys: not a row for each choice")
     if weights is not None:
         weights = _whole(weights, "poseidon_expert_combine: weights", dev, torch.float32, (n, k))
-    out = _out(out, "poseidon_expert_combine: out", dev, dt, (n, d))
+    out, pitch = _out(out, "poseidon_expert_combine: out", dev, dt, n, d)
     _call("poseidon_expert_combine", dev, ys.data_ptr(), TYPES[dt], n, d, position.data_ptr(), k,
-          None if weights is None else weights.data_ptr(), out.data_ptr(), _pitch(out))
+          None if weights is None else weights.data_ptr(), out.data_ptr(), pitch)
     return out
 
 
 @_streamed
 def poseidon_expert_combine_backward(dout, ys, plan: ExpertPlan, weights) -> Tuple[torch.Tensor, torch.Tensor]:
     """(dys [tokens * k, width], dweights float32 [tokens, k]) of poseidon_expert_combine."""
-    dout = _rows(dout, "poseidon_expert_combine_backward: dout")
-    n, d = dout.shape
+    dout, n, d, pitch = _rows(dout, "poseidon_expert_combine_backward: dout")
     dev, dt = dout.device, dout.dtype
     _, offsets, kept, k = _plan(plan, "poseidon_expert_combine_backward: plan", dev, n)
     order = _whole(plan.order, "poseidon_expert_combine_backward: plan", dev, torch.int32, (n * k,))
-    ys = _rows(ys, "poseidon_expert_combine_backward: ys", dev, dt, (n * k, d)).contiguous()
+    ys, _, _, ys_pitch = _rows(ys, "poseidon_expert_combine_backward: ys", dev, dt, (n * k, d))
+    ys = ys if ys_pitch == d else ys.contiguous()
     weights = _whole(weights, "poseidon_expert_combine_backward: weights", dev, torch.float32, (n, k))
-    dys, dweights = torch.empty_like(ys), torch.empty_like(weights)
-    _call("poseidon_expert_combine_backward", dev, dout.data_ptr(), _pitch(dout), ys.data_ptr(), TYPES[dt], n, d,
+    dys, dweights = torch.empty((n * k, d), dtype=dt, device=dev), torch.empty_like(weights)
+    _call("poseidon_expert_combine_backward", dev, dout.data_ptr(), pitch, ys.data_ptr(), TYPES[dt], n, d,
           order.data_ptr(), k, kept, weights.data_ptr(), dys.data_ptr(), dweights.data_ptr())
     return dys, dweights
 
@@ -412,14 +410,13 @@ def _ids(ids, where: str, device) -> torch.Tensor:
 @_streamed
 def poseidon_embed(ids, table, scale: float = 1.0, *, out=None) -> torch.Tensor:
     """scale * table[ids], [tokens, width]; ids (int32) outside the table give zeros."""
-    table = _rows(table, "poseidon_embed: table")
-    v, d = table.shape
+    table, v, d, table_pitch = _rows(table, "poseidon_embed: table")
     dev, dt = table.device, table.dtype
     ids = _ids(ids, "poseidon_embed: ids", dev)
     n = ids.numel()
-    out = _out(out, "poseidon_embed: out", dev, dt, (n, d))
-    _call("poseidon_embed", dev, ids.data_ptr(), n, table.data_ptr(), _pitch(table), TYPES[dt], v, d, scale,
-          out.data_ptr(), _pitch(out))
+    out, pitch = _out(out, "poseidon_embed: out", dev, dt, n, d)
+    _call("poseidon_embed", dev, ids.data_ptr(), n, table.data_ptr(), table_pitch, TYPES[dt], v, d, scale,
+          out.data_ptr(), pitch)
     return out
 
 
@@ -428,17 +425,16 @@ def poseidon_embed_backward(ids, dout, vocab: int, scale: float = 1.0, *, dtype=
                             accumulate: bool = False) -> torch.Tensor:
     """Gradient [vocab, width] of the table.  With accumulate the sums are added to `out` and the rows of no token
     are left alone."""
-    dout = _rows(dout, "poseidon_embed_backward: dout")
-    n, d = dout.shape
+    dout, n, d, pitch = _rows(dout, "poseidon_embed_backward: dout")
     dev = dout.device
     ids = _ids(ids, "poseidon_embed_backward: ids", dev)
     if ids.numel() != n or (accumulate and out is None):
         _refuse("poseidon_embed_backward: ids: not one for each row of dout, or accumulate without out")
-    dtype = dtype if out is None else out.dtype
+    dtype = dtype if out is None else getattr(out, "dtype", None)
     if dtype not in TYPES or vocab < 0:
         _refuse("poseidon_embed_backward: a float32, float16 or bfloat16 result")
-    out = _out(out, "poseidon_embed_backward: out", dev, dtype, (vocab, d))
+    out, out_pitch = _out(out, "poseidon_embed_backward: out", dev, dtype, vocab, d)
     w, at, size = _workspace("poseidon_embed_backward", dev, n, vocab, d)
-    _call("poseidon_embed_backward", dev, ids.data_ptr(), n, dout.data_ptr(), _pitch(dout), TYPES[dout.dtype], vocab, d,
-          scale, out.data_ptr(), _pitch(out), TYPES[dtype], int(accumulate), at, size)
+    _call("poseidon_embed_backward", dev, ids.data_ptr(), n, dout.data_ptr(), pitch, TYPES[dout.dtype], vocab, d,
+          scale, out.data_ptr(), out_pitch, TYPES[dtype], int(accumulate), at, size)
     return out
