@@ -161,7 +161,7 @@ __global__ __launch_bounds__(kBlock) void gather_kernel(const typename T::raw *x
 }
 
 // A lane sums its slice over the token's places, in the order of the choices; the
-// rows of eight choices are asked for before the first is added.
+// rows of two choices are asked for before the first is added.
 template <class T, bool STREAM>
 __global__ __launch_bounds__(kBlock) void combine_kernel(const typename T::raw *ys, uint32_t total, Div per_row,
                                                          uint32_t width, const int32_t *position, uint32_t k,
@@ -258,22 +258,39 @@ __global__ __launch_bounds__(kBlock) void combine_backward_kernel(const typename
 
 // ---- embedding ----
 
-template <class T, bool STREAM>
+// A lane's N slices are a grid apart: an id has to be there before its row can be asked for, and with one slice a lane
+// these two waits in a row are most of a long call (65536 x 1024: 41 us with N = 4, 48 with 1).
+template <class T, bool STREAM, uint32_t N>
 __global__ __launch_bounds__(kBlock) void embed_kernel(const int32_t *ids, uint32_t total, Div per_row, uint32_t width,
                                                        const typename T::raw *table, uint64_t table_pitch,
                                                        uint32_t vocab, float scale, typename T::raw *out,
                                                        uint64_t pitch) {
-    const uint32_t i = blockIdx.x * kBlock + threadIdx.x;
-    if (i >= total) return;
-    const uint32_t row = quotient(i, per_row), s = i - row * per_row.d;
-    const uint32_t id = (uint32_t)ids[row];
-    float v[8] = {};
-    if (id < vocab) {
-        load_slice<T>(table + (uint64_t)id * table_pitch, s * kSlice, width, v);
+    const uint32_t first = blockIdx.x * kBlock + threadIdx.x, step = gridDim.x * kBlock;
+    uint32_t row[N], id[N];
+    Slice<T> in[N];
 #pragma unroll
-        for (int c = 0; c < 8; ++c) v[c] *= scale;
+    for (uint32_t j = 0; j < N; ++j) {
+        const uint32_t i = min(first + j * step, total - 1);
+        row[j] = quotient(i, per_row);
+        id[j] = (uint32_t)ids[row[j]];
     }
-    store_slice<T, STREAM>(out + (uint64_t)row * pitch, s * kSlice, width, v);
+#pragma unroll
+    for (uint32_t j = 0; j < N; ++j) {
+        const uint32_t s = min(first + j * step, total - 1) - row[j] * per_row.d;
+        if (id[j] < vocab) in[j] = load_words<T>(table + (uint64_t)id[j] * table_pitch, s * kSlice, width);
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < N; ++j) {
+        const uint32_t i = first + j * step;
+        if (i >= total) return;
+        float v[8] = {};
+        if (id[j] < vocab) {
+            values<T>(in[j], v);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) v[c] *= scale;
+        }
+        store_slice<T, STREAM>(out + (uint64_t)row[j] * pitch, (i - row[j] * per_row.d) * kSlice, width, v);
+    }
 }
 
 inline uint32_t slices_of(uint64_t width) { return (uint32_t)((width + kSlice - 1) / kSlice); }
@@ -449,11 +466,18 @@ int poseidon_embed(const int32_t *ids, uint64_t tokens, const void *table, uint6
     if (tokens && !ids) return POSEIDON_E_INVAL;
     if (!tokens) return POSEIDON_OK;
     const uint32_t per_row = slices_of(width);
-    PL_STREAM(tokens * width * 2 * size_of(type), PL_TYPE(type, over_rows(tokens, per_row, [&](uint64_t r, uint64_t, uint32_t n) {
-        embed_kernel<T, STREAM><<<blocks_for(n), kBlock, 0, (hipStream_t)hip_stream>>>(
-            ids + r, n, make_div(per_row), (uint32_t)width, (const T::raw *)table, table_pitch, (uint32_t)vocab, scale,
-            (T::raw *)out + r * out_pitch, out_pitch);
-    })));
+    const auto run = [&](auto kernel, auto t, uint32_t each) {
+        using T = decltype(t);
+        over_rows(tokens, per_row, [&](uint64_t r, uint64_t, uint32_t n) {
+            kernel<<<blocks_for((n + each - 1) / each), kBlock, 0, (hipStream_t)hip_stream>>>(
+                ids + r, n, make_div(per_row), (uint32_t)width, (const typename T::raw *)table, table_pitch, (uint32_t)vocab,
+                scale, (typename T::raw *)out + r * out_pitch, out_pitch);
+        });
+    };
+    // four slices a lane where that leaves every CU its 2048 lanes
+    const bool four = tokens * per_row >= 4ull * 256 * 2048;
+    PL_STREAM(tokens * width * 2 * size_of(type), PL_TYPE(type, four ? run(embed_kernel<T, STREAM, 4>, T{}, 4)
+                                                                      : run(embed_kernel<T, STREAM, 1>, T{}, 1)));
     return launched();
 }
 

@@ -246,6 +246,34 @@ def test_weight_gradient_over_tiles_and_splits(dev):
     assert torch.equal(torch.isnan(got), bad)
 
 
+@pytest.mark.parametrize("out_kind", KINDS)
+@pytest.mark.parametrize("rows, o, i, ranges", [(6000, 2040, 1365, 0), (700, 8200, 4099, 0), (12000, 1032, 1030, 24),
+                                                (12000, 1024, 1024, 24)])
+def test_weight_gradient_of_many_large_tiles(dev, out_kind, rows, o, i, ranges):
+    """The large tiles at widths that end inside one, with more of them than CUs, alone and added to what is there."""
+    g = torch.Generator(device=dev)
+    g.manual_seed(rows + i)
+    dy = torch.randn(rows, o, generator=g, device=dev).bfloat16()
+    s = L.poseidon_stash(torch.randn(rows, i, generator=g, device=dev).bfloat16())
+    back = L.poseidon_restore(s, dtype=torch.float32).double()
+    cuts = [0, rows]
+    if ranges:
+        cuts = sorted([0, rows, 1, 65] + torch.randint(0, rows, (ranges - 3,), generator=g, device=dev).tolist())
+    at = torch.tensor(cuts, dtype=torch.int32, device=dev) if ranges else None
+    got = L.poseidon_weight_gradient(dy, s, offsets=at, dtype=KIND[out_kind])
+    acc = torch.full_like(got, 3.0)
+    L.poseidon_weight_gradient(dy, s, offsets=at, out=acc, accumulate=True)
+    got, acc = got.view(-1, o, i), acc.view(-1, o, i)
+    assert got.shape[0] == len(cuts) - 1
+    for r, (a, b) in enumerate(zip(cuts, cuts[1:])):
+        left = dy[a:b].double().t().contiguous()
+        want, size = left @ back[a:b], (b - a + 2) * V * (left.abs() @ back[a:b].abs())
+        for have, base in ((got[r], 0.0), (acc[r], 3.0)):
+            exact = want + base
+            slack = size + V * base
+            assert ((have.double() - exact).abs() <= slack + ROUND[out_kind] * (exact.abs() + slack) + STEP[out_kind]).all()
+
+
 # ---- experts ----
 
 BATCHES = [(1, 1, 1), (1, 8, 64), (5, 2, 3), (100, 3, 8), (700, 8, 33), (2100, 2, 511), (33000, 4, 256), (300000, 2, 64)]
