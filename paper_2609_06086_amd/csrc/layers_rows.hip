@@ -7,7 +7,9 @@ namespace pl {
 
 // ---- activations kept in 8 bits ----
 
-// Codes and scale bytes have no gaps, so a lane's slice is slice i of both.
+// e = ceil(log2(max |x| / 127)) over 64 values, code = round(x / 2^e).  Codes and scale bytes have no gaps, so a lane's
+// slice is slice i of both.  Memory bounds both directions: 32768 x 8192 of 16 bits kept in 137 us (5.9 TB/s) and restored in
+// 126 (6.4).
 template <class T, bool STREAM>
 __global__ __launch_bounds__(kBlock) void stash_kernel(const typename T::raw *x, uint64_t pitch, uint32_t total,
                                                        Div per_row, uint32_t width, int8_t *codes, uint8_t *scales) {
@@ -49,6 +51,8 @@ __device__ __forceinline__ float sigmoid(float z) {
         return 1.0f / (1.0f + expf(-z));
 }
 
+// silu(gate) * up and both kept, in one pass over gate and up; the backward pass reads them as they were kept.  Memory bounds
+// both: 16384 x 12288 of 16 bits 258 us forward (6.3 TB/s), 259 backward (6.2).
 template <class T, bool KEEP, bool STREAM>
 __global__ __launch_bounds__(kBlock) void gated_forward_kernel(
     const typename T::raw *gate, uint64_t gate_pitch, const typename T::raw *up, uint64_t up_pitch, uint32_t total,
@@ -126,6 +130,8 @@ __device__ __forceinline__ void clear_rows(uint32_t wave, uint32_t waves, const 
 
 // A lane reads its slice of a token once and writes it to each of the token's
 // places; the rounding to 8 bits is done once too.  Blocks from `main` on clear the places past the last choice.
+// Writes bound it: 16384 tokens of 4096 values to 8 places each, kept too, 333 us (5.3 TB/s).  A lane per place, which
+// writes in order and reads a token's row eight times from cache: 30 us more, with 2 choices 179 instead of 152 us.
 template <class T, bool WRITE, bool KEEP, bool STREAM>
 __global__ __launch_bounds__(kBlock) void gather_kernel(const typename T::raw *x, uint64_t pitch, uint32_t total,
                                                         Div per_row, uint32_t width, const int32_t *position,
@@ -161,7 +167,8 @@ __global__ __launch_bounds__(kBlock) void gather_kernel(const typename T::raw *x
 }
 
 // A lane sums its slice over the token's places, in the order of the choices; the
-// rows of two choices are asked for before the first is added.
+// rows of two choices are asked for before the first is added.  Memory bounds it: 16384 tokens of 4096 values from 8 places
+// 200 us (6.0 TB/s).
 template <class T, bool STREAM>
 __global__ __launch_bounds__(kBlock) void combine_kernel(const typename T::raw *ys, uint32_t total, Div per_row,
                                                          uint32_t width, const int32_t *position, uint32_t k,

@@ -4,7 +4,8 @@
 // low bits first.  A block of eight waves takes up to 4096 neighbouring elements, a wave an eighth
 // of them, 64 at a time in order; lanes with the same digit find each other with one
 // ballot a bit, so an element's rank among the equal ones before it needs no
-// atomics and the order is the same on every call.
+// atomics and the order is the same on every call.  Waits bound it, not bytes: 131072 choices of 64 experts take 5 us to count
+// and 11 to place, up to 4096 elements 3 to 9 us in one block.
 #include "layers_device.h"
 
 namespace pl {
@@ -314,6 +315,8 @@ inline int sort(SortPass p, const SortLists &lists, const Clear &c, hipStream_t 
 // of every token whose places all lie in the chunk.  A token that comes from the chunk
 // before leaves its part in slot 0 of the chunk, one that only goes on into the
 // next chunk in slot 1; embed_join_kernel adds those up in order.
+// Rows lie anywhere, and the waits for them bound it: 32768 tokens of 2048 values 82 us (134 MB read, about 100
+// written); eight rows on their way cost registers and 15 us more, chunks of 16 places 16 us more.
 struct EmbedGrad {
     const int32_t *keys, *order;
     uint32_t m, vocab, width, chunk, chunks, accumulate;
@@ -400,7 +403,7 @@ __global__ __launch_bounds__(64) void embed_sum_kernel(EmbedGrad e) {
 
 // A block of four waves per chunk and 512 columns; it has work where a token
 // begins in the chunk and goes on past it.  The waves take every fourth of the
-// chunks that follow, and the first adds the four sums.
+// chunks that follow, and the first adds the four sums.  A few dependent waits: 9 us for 1024 chunks.
 template <class G>
 __global__ __launch_bounds__(256) void embed_join_kernel(EmbedGrad e) {
     __shared__ float share[3][64][kSlice + 1];

@@ -258,6 +258,12 @@ __device__ __forceinline__ Rsrc buffer(const void *p, uint32_t bytes) {
 // waits for memory took half of the time).
 // C = 4, 128 x 128: 64 sums a lane and half of the LDS, so that two blocks share a CU.
 //
+// Measured: 16384 x 8192 x 4096 in 946 to 961 us (1150 TFLOP/s; the matrix instructions are busy 58% of the cycles, the rest
+// goes to the instructions between them), 64 ragged ranges of 2048 x 2048 over 65536 rows 710 us.  There a unit has 16 steps
+// on average and a start and an end that nothing hides; tried and slower or no faster: the next unit's rows asked for
+// before the stores (705 us), 16 bytes a lane a store (760: pieces of 32 bytes of a line), a range's tiles all on one XCD
+// (756), leaving out the zero step after an odd number (the registers no longer suffice).
+//
 // Rows past the end come back as zeros from the buffers' bounds.  ALIGNED: dy's rows begin on whole words, as
 // buffer loads want, and are a multiple of 8 wide; else they are read with plain loads, which take any address, and
 // masked.
@@ -486,7 +492,7 @@ __global__ __launch_bounds__(256, C == 8 ? 1 : 2) void weight_gradient_kernel(We
         write(G{}, g.grad, run.range, false);
 }
 
-// Adds a split range's slots, in order.
+// Adds a split range's slots, in order: one pass over them, 5 us for 4 of 1024 x 1024.
 template <class G>
 __global__ __launch_bounds__(kBlock) void weight_join_kernel(WeightGrad g) {
     Split s = {0, 0, g.of_one};
