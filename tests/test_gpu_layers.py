@@ -274,6 +274,16 @@ def test_weight_gradient_of_many_large_tiles(dev, out_kind, rows, o, i, ranges):
             assert ((have.double() - exact).abs() <= slack + ROUND[out_kind] * (exact.abs() + slack) + STEP[out_kind]).all()
 
 
+@pytest.mark.parametrize("kind, low, high", [("f16", -24, 10), ("bf16", -133, 100)])
+@pytest.mark.parametrize("o", [1, 7, 64])
+def test_weight_gradient_of_the_least_values(dev, kind, low, high, o):
+    """Gradients below the type's normal range count: every product and sum is exact."""
+    dy = torch.full((16, o), 1.0, dtype=torch.float64, device=dev).mul_(2.0 ** low).to(KIND[kind])
+    x = torch.full((16, 70), 2.0 ** high, dtype=KIND[kind], device=dev)
+    assert (dy != 0).all()
+    assert (L.poseidon_weight_gradient(dy, L.poseidon_stash(x)).double() == 16 * 2.0 ** (low + high)).all()
+
+
 # ---- experts ----
 
 BATCHES = [(1, 1, 1), (1, 8, 64), (5, 2, 3), (100, 3, 8), (700, 8, 33), (2100, 2, 511), (33000, 4, 256), (300000, 2, 64)]
