@@ -112,8 +112,8 @@ __device__ __forceinline__ Unit unit_of(const WeightGrad &g) {
 // The runs of ragged ranges: a range of more than `most` steps becomes several of about the
 // same length, and of up to kRanked runs the longest come first, so that none is left for the
 // end.  One block.  An empty range is a run too, which writes its zeros.
-// It is one long chain of waits, so few ranges get few waves, and the lengths that a run is compared with come sixteen at a
-// time (64 ranges: 6 us, 8 to 9 one at a time in 16 waves).
+// It is one long chain of waits, so a run has a thread of its own, few runs get few waves, and the lengths that a run is
+// compared with come sixteen at a time (64 ranges: 6 us; 25 ranges in about 100 runs 7 us, 54 with a thread per range).
 constexpr uint32_t kPlanThreads = 1024, kRanked = 1024;
 
 struct RunPlan {
@@ -170,47 +170,61 @@ __global__ __launch_bounds__(kPlanThreads) void weight_plan_kernel(RunPlan p) {
 
     // Ranges that overlap (offsets that do not ascend) can ask for more than there is room for: then none is split.
     const bool fits = total[0] <= p.max_runs && total[1] <= p.max_splits && total[2] <= p.max_slots;
-    const uint32_t all = fits ? total[0] : p.ranges, ranked = all <= kRanked;
-    const auto each_run = [&](auto f) {
-        uint32_t n0 = fits ? at[0] : first, n1 = at[1], n2 = at[2];
-        for (uint32_t r = first; r < last; ++r) {
-            const uint32_t begin = bound(r), end = max(begin, bound(r + 1)), steps = steps_of(begin, end);
-            const uint32_t n = fits ? max(1u, (steps + p.most - 1) / p.most) : 1, part = (steps + n - 1) / n;
-            for (uint32_t i = 0; i < n; ++i) {
-                const uint32_t from = min(begin + i * part * kStep, end), to = min(from + part * kStep, end);
-                f(n0++, Run{r, from, to, n > 1 ? n2 + i : kNone});
-            }
-            if (n > 1) {
-                p.splits[n1++] = Split{r, n2, n};
-                n2 += n;
-            }
-        }
-    };
+    const uint32_t all = fits ? total[0] : p.ranges;
     if (tid == 0) *p.table = RunTable{all, fits ? total[1] : 0};
-    if (ranked) {
+    const auto parts_of = [&](uint32_t begin, uint32_t end) { return fits ? max(1u, (steps_of(begin, end) + p.most - 1) / p.most) : 1u; };
+    const auto run_of = [&](uint32_t r, uint32_t begin, uint32_t end, uint32_t n, uint32_t i, uint32_t slot) {
+        const uint32_t part = (steps_of(begin, end) + n - 1) / n, from = min(begin + i * part * kStep, end);
+        const uint32_t to = min(from + part * kStep, end);
+        return Run{r, from, to, n > 1 ? slot + i : kNone};
+    };
+
+    if (all <= kRanked) {    // a thread has a range, then a run: the one that holds its place, and the place that its length takes
+        __shared__ uint32_t run0[kRanked], begins[kRanked], ends[kRanked], slot0[kRanked];
+        if (tid < p.ranges) {
+            run0[tid] = fits ? at[0] : tid;
+            begins[tid] = own[0];
+            ends[tid] = max(own[0], own[1]);
+            slot0[tid] = at[2];
+            if (parts_of(own[0], own[1]) > 1) p.splits[at[1]] = Split{tid, at[2], need[0]};
+        }
         if (tid < 16 && all + tid < kRanked) length[all + tid] = 0;
-        each_run([&](uint32_t i, const Run &r) { length[i] = r.end - r.begin; });
         __syncthreads();
-    }
-    each_run([&](uint32_t i, const Run &r) {
-        uint32_t rank = i;
-        if (ranked) {
-            rank = 0;
-            const uint32_t mine = r.end - r.begin;
-            for (uint32_t j = 0; j < all; j += 16) {    // past the last run: lengths of 0
-                uint4 u[4];
+        Run run = {};
+        uint32_t mine = 0;
+        if (tid < all) {
+            uint32_t r = 0;    // the last range whose first run is not after this one
+            for (uint32_t d = kRanked / 2; d; d >>= 1)
+                if (r + d < p.ranges && run0[r + d] <= tid) r += d;
+            run = run_of(r, begins[r], ends[r], parts_of(begins[r], ends[r]), tid - run0[r], slot0[r]);
+            length[tid] = mine = run.end - run.begin;
+        }
+        __syncthreads();
+        if (tid >= all) return;
+        uint32_t rank = 0;
+        for (uint32_t j = 0; j < all; j += 16) {    // past the last run: lengths of 0
+            uint4 u[4];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) u[q] = lengths[j / 4 + q];
+            for (int q = 0; q < 4; ++q) u[q] = lengths[j / 4 + q];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const uint32_t l[4] = {u[q].x, u[q].y, u[q].z, u[q].w};
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t l[4] = {u[q].x, u[q].y, u[q].z, u[q].w};
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) rank += l[e] > mine || (l[e] == mine && j + 4 * q + e < i);
-                }
+                for (int e = 0; e < 4; ++e) rank += l[e] > mine || (l[e] == mine && j + 4 * q + e < tid);
             }
         }
-        p.runs[rank] = r;
-    });
+        p.runs[rank] = run;
+        return;
+    }
+    uint32_t n0 = fits ? at[0] : first, n1 = at[1], n2 = at[2];
+    for (uint32_t r = first; r < last; ++r) {
+        const uint32_t begin = bound(r), end = max(begin, bound(r + 1)), n = parts_of(begin, end);
+        for (uint32_t i = 0; i < n; ++i) p.runs[n0++] = run_of(r, begin, end, n, i, n2);
+        if (n > 1) {
+            p.splits[n1++] = Split{r, n2, n};
+            n2 += n;
+        }
+    }
 }
 
 template <int N>
@@ -533,13 +547,16 @@ struct WeightPlan {
 
 // Tiles of 256 x 256 where the 256 CUs get 16 steps or more each (1077 TFLOP/s on long sums, 686 with tiles of
 // 128 x 128, which fill the chip with less).  One range: its rows are split until every CU has a block, of
-// 16 (8) steps or more (two of the small tiles a CU take longer: 4096 x 1024 x 1024 31 us instead of 29).  Ragged ranges: runs of at most half of a CU's share.
+// 16 (8) steps or more (two of the small tiles a CU take longer: 4096 x 1024 x 1024 31 us instead of 29).  Ragged ranges: runs
+// of at most half of a CU's share, and the large tiles from 96 steps a CU on, as there are more units to even out: with
+// 128 steps a CU 16 ranges of 2048 x 2048 take 333 us (382 with the small tiles), with 64 8 ranges 204 (182), with 34 34
+// ranges of 520 x 1416 156 (113).
 inline WeightPlan weight_plan(uint64_t rows, uint64_t out_width, uint64_t in_width, uint32_t n_ranges, bool whole) {
     WeightPlan p = {};
     const bool ragged = n_ranges > 1;
     const uint64_t steps = (rows + kStep - 1) / kStep;
     const auto tiles = [&](uint64_t side) { return ((out_width + side - 1) / side) * ((in_width + side - 1) / side); };
-    p.large = whole && steps * tiles(256) >= 256 * 16;
+    p.large = whole && steps * tiles(256) >= 256 * (ragged ? 96 : 16);
     const uint64_t side = p.large ? 256 : 128, each = p.large ? 16 : 8, n = tiles(side);
     p.tiles_o = (uint32_t)((out_width + side - 1) / side);
     p.tiles_i = (uint32_t)((in_width + side - 1) / side);
@@ -629,7 +646,7 @@ int poseidon_weight_gradient(const void *dy, uint64_t dy_pitch, uint32_t type, u
         g.table = r.table;
         g.runs = r.runs;
         g.splits = r.splits;
-        const uint32_t threads = n_ranges < kPlanThreads ? (n_ranges + 63) / 64 * 64 : kPlanThreads;
+        const uint32_t threads = p.max_runs < kPlanThreads ? (uint32_t)(p.max_runs + 63) / 64 * 64 : kPlanThreads;
         weight_plan_kernel<<<1, threads, 0, stream>>>(r);
         PL_TRY(launched());    // the next kernel reads the table
     }

@@ -227,6 +227,25 @@ def test_weight_gradient_of_many_ranges(dev):
     _check(got, want, 70 * V * O.weight_gradient(np.abs(_np(dy)), np.abs(back), cuts), "f32")
 
 
+@pytest.mark.parametrize("ranges", [1, 2, 3, 65, 1023, 1024, 1025])
+def test_weight_gradient_of_ranges_in_many_runs(dev, ranges):
+    """Long ranges in many runs beside short and empty ones, up to and past the number of runs that are put in order."""
+    rng = np.random.default_rng(ranges)
+    rows, o, i = 40000, 64, 72
+    cuts = np.sort(np.concatenate([[0, rows], rng.integers(0, 700, size=ranges - 1)]))
+    g = torch.Generator(device=dev)
+    g.manual_seed(ranges)
+    dy = torch.randn(rows, o, generator=g, device=dev).bfloat16()
+    s = L.poseidon_stash(torch.randn(rows, i, generator=g, device=dev).bfloat16())
+    back = L.poseidon_restore(s, dtype=torch.float32).double()
+    got = L.poseidon_weight_gradient(dy, s, offsets=torch.from_numpy(cuts.astype(np.int32)).to(dev))
+    assert got.shape == (ranges, o, i)
+    for r, (a, b) in enumerate(zip(cuts, cuts[1:])):
+        left = dy[a:b].double().t().contiguous()
+        want, size = left @ back[a:b], (int(b - a) + 2) * V * (left.abs() @ back[a:b].abs())
+        assert ((got[r].double() - want).abs() <= size + ROUND["f32"] * want.abs() + STEP["f32"]).all()
+
+
 def test_weight_gradient_over_tiles_and_splits(dev):
     """Sizes of each tile and of rows in one or more parts, the sums' bound on each; NaN spreads along its row and column
     alone."""
@@ -248,7 +267,7 @@ def test_weight_gradient_over_tiles_and_splits(dev):
 
 @pytest.mark.parametrize("out_kind", KINDS)
 @pytest.mark.parametrize("rows, o, i, ranges", [(6000, 2040, 1365, 0), (700, 8200, 4099, 0), (12000, 1032, 1030, 24),
-                                                (12000, 1024, 1024, 24)])
+                                                (12000, 1024, 1024, 24), (24000, 2040, 2050, 24)])
 def test_weight_gradient_of_many_large_tiles(dev, out_kind, rows, o, i, ranges):
     """The large tiles at widths that end inside one, with more of them than CUs, alone and added to what is there."""
     g = torch.Generator(device=dev)
