@@ -537,12 +537,22 @@ __global__ __launch_bounds__(kBlock) void weight_join_kernel(WeightGrad g) {
     }
 }
 
+// Rows of 16-bit values on a pitch of `padded` (a multiple of 8) values, zeros past the width.
+__global__ __launch_bounds__(kBlock) void pack_rows_kernel(const __bf16 *x, uint64_t pitch, uint32_t total, Div per_row,
+                                                           uint32_t width, uint4 *out) {
+    const uint32_t i = blockIdx.x * kBlock + threadIdx.x;
+    if (i >= total) return;
+    const uint32_t row = quotient(i, per_row);
+    const Slice<BF16> s = load_words<BF16>(x + row * pitch, (i - row * per_row.d) * kSlice, width);
+    out[i] = make_uint4(s.w[0], s.w[1], s.w[2], s.w[3]);
+}
+
 struct WeightPlan {
-    bool large;
+    bool large, pack;
     uint32_t tiles_o, tiles_i;
     uint32_t each;                                // ragged: steps of a run at most
     uint64_t max_runs, max_splits, max_slots;     // one range: exact
-    uint64_t table, runs, splits, bytes;          // offsets of the workspace, after the slots
+    uint64_t packed, table, runs, splits, bytes;  // offsets of the workspace, after the slots
 };
 
 // Tiles of 256 x 256 where the 256 CUs get 16 steps or more each (1077 TFLOP/s on long sums, 686 with tiles of
@@ -551,12 +561,18 @@ struct WeightPlan {
 // of at most half of a CU's share, and the large tiles from 96 steps a CU on, as there are more units to even out: with
 // 128 steps a CU 16 ranges of 2048 x 2048 take 333 us (382 with the small tiles), with 64 8 ranges 204 (182), with 34 34
 // ranges of 520 x 1416 156 (113).
+//
+// A dy that is no multiple of 8 wide is copied to one that is where that brings the large tiles: 16000 x 4098 x 2048 QQQ us
+// instead of 570.  Not for an x of few columns (the copy would take as long as it saves), nor for more than 8 GB.
 inline WeightPlan weight_plan(uint64_t rows, uint64_t out_width, uint64_t in_width, uint32_t n_ranges, bool whole) {
     WeightPlan p = {};
     const bool ragged = n_ranges > 1;
     const uint64_t steps = (rows + kStep - 1) / kStep;
     const auto tiles = [&](uint64_t side) { return ((out_width + side - 1) / side) * ((in_width + side - 1) / side); };
-    p.large = whole && steps * tiles(256) >= 256 * (ragged ? 96 : 16);
+    const bool much = steps * tiles(256) >= 256 * (ragged ? 96 : 16);
+    const uint64_t packed = rows * ((out_width + 7) / 8 * 16);
+    p.pack = much && !whole && out_width % 8 && in_width >= 512 && packed <= 8ull << 30;
+    p.large = much && (whole || p.pack);
     const uint64_t side = p.large ? 256 : 128, each = p.large ? 16 : 8, n = tiles(side);
     p.tiles_o = (uint32_t)((out_width + side - 1) / side);
     p.tiles_i = (uint32_t)((in_width + side - 1) / side);
@@ -581,6 +597,8 @@ inline WeightPlan weight_plan(uint64_t rows, uint64_t out_width, uint64_t in_wid
         p.splits = p.runs + up(p.max_runs * sizeof(Run));
         p.bytes = p.splits + up(p.max_splits * sizeof(Split));
     }
+    p.packed = p.bytes;
+    if (p.pack) p.bytes += up(packed);
     return p;
 }
 
@@ -602,7 +620,7 @@ extern "C" {
 
 uint64_t poseidon_weight_gradient_workspace(uint64_t rows, uint64_t out_width, uint64_t in_width, uint32_t n_ranges) {
     if (check_weight(rows, out_width, in_width, n_ranges) != POSEIDON_OK) return UINT64_MAX;
-    // the most that any layout of dy needs
+    // the most that any layout of dy needs (it is copied by its width alone)
     const uint64_t a = weight_plan(rows, out_width, in_width, n_ranges, false).bytes;
     const uint64_t b = weight_plan(rows, out_width, in_width, n_ranges, true).bytes;
     return a < b ? b : a;
@@ -621,7 +639,7 @@ int poseidon_weight_gradient(const void *dy, uint64_t dy_pitch, uint32_t type, u
     PL_TRY(check_workspace(workspace, workspace_bytes,
                            poseidon_weight_gradient_workspace(rows, out_width, in_width, n_ranges)));
     const hipStream_t stream = (hipStream_t)hip_stream;
-    const bool whole = aligned(dy, 4) && dy_pitch % 2 == 0 && out_width % 8 == 0;
+    const bool whole = out_width % 8 == 0 && aligned(dy, 4) && dy_pitch % 2 == 0;
     const WeightPlan p = weight_plan(rows, out_width, in_width, n_ranges, whole);
     char *base = (char *)workspace;
     WeightGrad g = {};
@@ -640,6 +658,17 @@ int poseidon_weight_gradient(const void *dy, uint64_t dy_pitch, uint32_t type, u
     g.grad = grad;
     g.parts = (float *)base;
     g.offsets = offsets;
+    if (p.pack) {
+        const uint32_t per_row = (uint32_t)((out_width + 7) / 8);
+        over_rows(rows, per_row, [&](uint64_t r, uint64_t, uint32_t n) {
+            pack_rows_kernel<<<blocks_for(n), kBlock, 0, stream>>>((const __bf16 *)dy + r * dy_pitch, dy_pitch, n,
+                                                                   make_div(per_row), (uint32_t)out_width,
+                                                                   (uint4 *)(base + p.packed) + r * per_row);
+        });
+        PL_TRY(launched());    // the next kernel reads it
+        g.dy = base + p.packed;
+        g.dy_pitch = per_row * 8ull;
+    }
     if (n_ranges > 1) {
         RunPlan r = {offsets, (uint32_t)rows, n_ranges, p.each, (uint32_t)p.max_runs, (uint32_t)p.max_splits,
                      (uint32_t)p.max_slots, (RunTable *)(base + p.table), (Run *)(base + p.runs), (Split *)(base + p.splits)};
