@@ -557,13 +557,15 @@ struct WeightPlan {
 
 // Tiles of 256 x 256 where the 256 CUs get 16 steps or more each (1077 TFLOP/s on long sums, 686 with tiles of
 // 128 x 128, which fill the chip with less).  One range: its rows are split until every CU has a block, of
-// 16 (8) steps or more (two of the small tiles a CU take longer: 4096 x 1024 x 1024 31 us instead of 29).  Ragged ranges: runs
+// 16 (8) steps or more, and a little more than 128 or 256 large tiles, which would leave most of the last round of the CUs
+// idle, in two or three parts where that takes less (16000 x 4104 x 2048, 136 tiles: 316 us instead of 376; 8192 x
+// 5120 x 3584, 280 tiles: 373 instead of 415) (two of the small tiles a CU take longer: 4096 x 1024 x 1024 31 us instead of 29).  Ragged ranges: runs
 // of at most half of a CU's share, and the large tiles from 96 steps a CU on, as there are more units to even out: with
 // 128 steps a CU 16 ranges of 2048 x 2048 take 333 us (382 with the small tiles), with 64 8 ranges 204 (182), with 34 34
 // ranges of 520 x 1416 156 (113).
 //
-// A dy that is no multiple of 8 wide is copied to one that is where that brings the large tiles: 16000 x 4098 x 2048 QQQ us
-// instead of 570.  Not for an x of few columns (the copy would take as long as it saves), nor for more than 8 GB.
+// A dy that is no multiple of 8 wide is copied to one that is where that brings the large tiles: 8000 x 2001 x 2048 92 us
+// instead of 133.  Not for an x of few columns (the copy would take as long as it saves), nor for more than 8 GB.
 inline WeightPlan weight_plan(uint64_t rows, uint64_t out_width, uint64_t in_width, uint32_t n_ranges, bool whole) {
     WeightPlan p = {};
     const bool ragged = n_ranges > 1;
@@ -584,6 +586,13 @@ inline WeightPlan weight_plan(uint64_t rows, uint64_t out_width, uint64_t in_wid
         p.max_slots = 2 * p.max_splits;
     } else {
         uint64_t runs = 256 / n, most = steps / each;
+        if (p.large && n > 128) {    // ns: rounds of the CUs, and the parts written and read
+            uint64_t least = ~0ull;
+            for (uint64_t r = 1; r <= 3; ++r) {
+                const uint64_t time = (n * r + 255) / 256 * ((steps + r - 1) / r * 1850 + 14000) + (r > 1 ? r * n * 105 : 0);
+                if (time < least) least = time, runs = r;
+            }
+        }
         runs = runs < most ? runs : most;
         p.max_runs = runs < 2 ? 1 : runs;
         p.max_splits = p.max_runs > 1;

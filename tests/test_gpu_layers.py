@@ -268,7 +268,8 @@ def test_weight_gradient_over_tiles_and_splits(dev):
 @pytest.mark.parametrize("out_kind", KINDS)
 @pytest.mark.parametrize("rows, o, i, ranges", [(6000, 2040, 1365, 0), (700, 8200, 4099, 0), (12000, 1032, 1030, 24),
                                                 (12000, 1024, 1024, 24), (24000, 2040, 2050, 24),
-                                                (6000, 2043, 1365, 0), (5000, 2046, 2100, 0), (24000, 2041, 2050, 24)])
+                                                (6000, 2043, 1365, 0), (5000, 2046, 2100, 0), (24000, 2041, 2050, 24),
+                                                (9000, 3336, 2049, 0)])
 def test_weight_gradient_of_many_large_tiles(dev, out_kind, rows, o, i, ranges):
     """The large tiles at widths that end inside one, with more of them than CUs, alone and added to what is there."""
     g = torch.Generator(device=dev)
