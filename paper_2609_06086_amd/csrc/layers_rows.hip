@@ -41,14 +41,37 @@ __global__ __launch_bounds__(kBlock) void restore_kernel(const int8_t *codes, co
 
 // ---- gated activation ----
 
-// 1 / (1 + exp(-z)).  16-bit outputs take the hardware's exponential and
-// reciprocal (about 1e-7 off); 32-bit ones the exact-to-the-last-bits functions.
+// 1 / (1 + exp(-z)) for z >= kFar.  16-bit outputs take the hardware's exponential and reciprocal (off by (2 + |z|) 2^-24
+// of the value), 32-bit ones the exact-to-the-last-bits functions.  Below kFar exp(-z) soon overflows, at -88.7, and the
+// reciprocal leaves the normal range.
+constexpr float kFar = -80.0f;
+
 template <class T>
 __device__ __forceinline__ float sigmoid(float z) {
     if constexpr (T::kShort)
         return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * z));
     else
         return 1.0f / (1.0f + expf(-z));
+}
+
+// a exp(z) b c for z < kFar, where 1 + exp(z) is 1 in 32 bits, so that the sigmoid is exp(z): what is left of it is still
+// a normal value, or large factors make it one.  exp(z) = 2^n 2^part with a whole n; the factors' fractions are multiplied
+// and the exponents added, so only the product itself can leave the range.  Below -1000 nothing is left of any product.
+__device__ __forceinline__ float times_exp(float a, float z, float b, float c) {
+    const float y = z * 1.44269504f, rest = fmaf(z, 1.44269504f, -y) + z * 1.92596303e-8f;    // z / ln 2 in two parts
+    const bool gone = z < -1000.0f;
+    const float n = gone ? 0.0f : rintf(y), part = gone ? 0.0f : __builtin_amdgcn_exp2f(y - n + rest);
+    float product = part;
+    int e = (int)n;
+    for (const float f : {a, b, c}) {
+        product *= __builtin_amdgcn_frexp_mantf(f);
+        e += __builtin_amdgcn_frexp_expf(f);
+    }
+    return ldexpf(product, e);
+}
+
+__device__ __forceinline__ float least(const float (&v)[8]) {
+    return fminf(fminf(fminf(v[0], v[1]), fminf(v[2], v[3])), fminf(fminf(v[4], v[5]), fminf(v[6], v[7])));
 }
 
 // silu(gate) * up and both kept, in one pass over gate and up; the backward pass reads them as they were kept.  Memory bounds
@@ -66,6 +89,10 @@ __global__ __launch_bounds__(kBlock) void gated_forward_kernel(
     load_slice<T, STREAM>(up + (uint64_t)row * up_pitch, s * kSlice, width, u);
 #pragma unroll
     for (int j = 0; j < 8; ++j) h[j] = g[j] * sigmoid<T>(g[j]) * u[j];
+    if (least(g) < kFar) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) h[j] = g[j] < kFar ? times_exp(g[j], g[j], u[j], 1.0f) : h[j];
+    }
     store_slice<T, STREAM>(out + (uint64_t)row * out_pitch, s * kSlice, width, h);
     if constexpr (KEEP) {
         uint32_t w[2];
@@ -93,19 +120,25 @@ __global__ __launch_bounds__(kBlock) void gated_backward_kernel(
     load_codes<STREAM>(gate_codes, i, wg);
     load_codes<STREAM>(up_codes, i, wu);
     const float sg = scale_of(gate_scales[i >> 3]), su = scale_of(up_scales[i >> 3]);
-    float d[8], g[8], u[8];
+    float d[8], g[8], u[8], a[8], b[8];
     load_slice<T, STREAM>(dout + (uint64_t)row * dout_pitch, s * kSlice, width, d);
     values_of(wg, sg, g);
     values_of(wu, su, u);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const float sig = sigmoid<T>(g[j]), ds = d[j] * sig, slope = 1.0f + g[j] * (1.0f - sig);
-        const float for_up = ds * g[j];
-        g[j] = ds * u[j] * slope;
-        u[j] = for_up;
+        a[j] = ds * u[j] * slope;
+        b[j] = ds * g[j];
     }
-    store_slice<T, STREAM>(dgate + (uint64_t)row * dgate_pitch, s * kSlice, width, g);
-    store_slice<T, STREAM>(dup + (uint64_t)row * dup_pitch, s * kSlice, width, u);
+    if (least(g) < kFar) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            a[j] = g[j] < kFar ? times_exp(1.0f + g[j], g[j], d[j], u[j]) : a[j];
+            b[j] = g[j] < kFar ? times_exp(g[j], g[j], d[j], 1.0f) : b[j];
+        }
+    }
+    store_slice<T, STREAM>(dgate + (uint64_t)row * dgate_pitch, s * kSlice, width, a);
+    store_slice<T, STREAM>(dup + (uint64_t)row * dup_pitch, s * kSlice, width, b);
 }
 
 // ---- experts ----

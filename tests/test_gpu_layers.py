@@ -131,6 +131,56 @@ def test_gated(dev, kind, shape):
     _check(b, du, 8 * V * np.abs(du) * (1 + np.abs(g)), kind)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+def test_gated_far_below_zero(dev, kind):
+    """Gates around -88, where exp(-gate) leaves the range of 32 bits, and far below: silu(gate) is still a normal value there,
+    and a large up brings smaller ones back into range.  The bounds of test_gated."""
+    big = 2.0 ** 15 if kind == "f16" else 2.0 ** 120
+    gates = np.concatenate([np.arange(-70.0, -127.0, -1.0), [-127.0, -60.0, 1.0, 80.0, 127.0]])
+    ups = np.array([1.0, -3.0, big, 2.0 ** -10, 1.75 * big])
+    g, u = (m.reshape(1, -1) for m in np.meshgrid(gates, ups, indexing="ij"))
+    w = np.where(np.arange(g.size) % 2 == 0, 0.75, -big).reshape(1, -1)
+    gate, up, dout = (torch.from_numpy(m).to(KIND[kind]).to(dev) for m in (g, u, w))
+    # a group of its own for each value, so that what is kept of it is exact
+    lone = [torch.zeros(g.size, 64, dtype=KIND[kind], device=dev) for _ in range(3)]
+    for m, v in zip(lone, (gate, up, dout)):
+        m[:, 5] = v[0]
+    top = {"f32": 2.0 ** 128, "f16": 65520.0, "bf16": 2.0 ** 128 * (1 - 2.0 ** -9)}[kind]    # what is rounded to infinity
+
+    def check(got, want, slack):
+        fits = (np.abs(want) + slack < top)[0]
+        here = torch.from_numpy(fits).to(dev)
+        _check(got[:, here], want[:, fits], slack[:, fits], kind)
+        assert torch.isinf(got[:, torch.from_numpy((np.abs(want) - slack >= top)[0]).to(dev)]).all()
+    out = L.poseidon_gated_forward(gate, up)[0]
+    want = O.gated_forward(_np(gate), _np(up))
+    check(out, want, 8 * V * np.abs(want) * (1 + np.abs(_np(gate))))
+    alone, sg, su = L.poseidon_gated_forward(lone[0], lone[1])
+    assert torch.equal(alone[:, 5], out[0]) and alone.count_nonzero() == out.count_nonzero()
+    g, u, w = (_np(m)[:, 5:6].T for m in (L.poseidon_restore(sg), L.poseidon_restore(su), lone[2]))
+    dg, du = O.gated_backward(w, g, u)
+    a, b = L.poseidon_gated_backward(lone[2], sg, su)
+    check(a[:, 5:6].t(), dg, 8 * V * np.abs(w * u * O.sigmoid(g)) * (1 + np.abs(g)) ** 2)
+    check(b[:, 5:6].t(), du, 8 * V * np.abs(du) * (1 + np.abs(g)))
+
+
+def test_gated_of_the_lowest_gates(dev):
+    """Down to the type's lowest value the product is 0 with its sign; minus infinity gives what the formula gives."""
+    x = torch.full((1, 64), 3.0, dtype=torch.float32, device=dev)
+    gate = torch.full((1, 64), -1000.5, dtype=torch.float32, device=dev)
+    gate[0, 1], gate[0, 2], gate[0, 3] = torch.finfo(torch.float32).min, -400.0, -1e20
+    gate[0, 4] = float("-inf")
+    up = torch.full_like(gate, torch.finfo(torch.float32).max)
+    out = L.poseidon_gated_forward(gate, up)[0]
+    assert torch.isnan(out[0, 4]) and out.nan_to_num().count_nonzero() == 0
+    gate[0, 4] = -90.0
+    _, sg, su = L.poseidon_gated_forward(gate, up)
+    a, b = L.poseidon_gated_backward(x, sg, su)
+    dg, du = O.gated_backward(_np(x), _np(L.poseidon_restore(sg)), _np(L.poseidon_restore(su)))
+    for got, want in ((a, dg), (b, du)):    # the scale of the lowest gate makes the others 0
+        assert torch.equal(torch.isinf(got), torch.from_numpy(np.abs(want) > 2.0 ** 128).to(dev)) and not got.isnan().any()
+
+
 def test_gated_with_infinities(dev):
     """An infinity makes its own output what the formula gives, and its group's gradient NaN; the rest is untouched."""
     x = torch.ones(2, 128, dtype=torch.bfloat16, device=dev)
