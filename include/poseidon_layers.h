@@ -96,7 +96,8 @@ int poseidon_weight_gradient(const void *dy, uint64_t dy_pitch, uint32_t type, u
                              const int8_t *codes, const uint8_t *scales, uint64_t in_width, const int32_t *offsets,
                              uint32_t n_ranges, void *grad, uint32_t grad_type, uint32_t accumulate, void *workspace,
                              uint64_t workspace_bytes, void *hip_stream);
-/* Bytes it needs (0: none, workspace may be NULL); UINT64_MAX if the sizes are refused. */
+/* Bytes it needs (0: none, workspace may be NULL); UINT64_MAX if the sizes are refused.  At most 1 GB for 32-bit sums of
+ * parts of the rows, and for an out_width that is no multiple of 8 up to 8 GB for a copy of dy. */
 uint64_t poseidon_weight_gradient_workspace(uint64_t rows, uint64_t out_width, uint64_t in_width, uint32_t n_ranges);
 
 /* ---- tokens by expert ---- */

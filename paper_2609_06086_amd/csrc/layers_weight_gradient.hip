@@ -564,8 +564,14 @@ struct WeightPlan {
 // 128 steps a CU 16 ranges of 2048 x 2048 take 333 us (382 with the small tiles), with 64 8 ranges 204 (182), with 34 34
 // ranges of 520 x 1416 156 (113).
 //
+// Parts take 1 GB at most: without a bound a gradient of 32776 x 32776 asked for 12 GB.  A gradient that would need more is
+// five rounds of the CUs and more, and of the last one there is little to win (131072 x 7424 x 13568 25.9 ms, 25.5 in three
+// parts of 1.2 GB; 65536 x 8448 x 8192, two parts of 0.8 GB, 8.8 instead of 9.7).
+//
 // A dy that is no multiple of 8 wide is copied to one that is where that brings the large tiles: 8000 x 2001 x 2048 92 us
 // instead of 133.  Not for an x of few columns (the copy would take as long as it saves), nor for more than 8 GB.
+constexpr uint64_t kPartsMost = 1ull << 30;
+
 inline WeightPlan weight_plan(uint64_t rows, uint64_t out_width, uint64_t in_width, uint32_t n_ranges, bool whole) {
     WeightPlan p = {};
     const bool ragged = n_ranges > 1;
@@ -588,7 +594,7 @@ inline WeightPlan weight_plan(uint64_t rows, uint64_t out_width, uint64_t in_wid
         uint64_t runs = 256 / n, most = steps / each;
         if (p.large && n > 128) {    // ns: rounds of the CUs, and the parts written and read
             uint64_t least = ~0ull;
-            for (uint64_t r = 1; r <= 3; ++r) {
+            for (uint64_t r = 1; r <= 3 && (r == 1 || r * out_width * in_width * 4 <= kPartsMost); ++r) {
                 const uint64_t time = (n * r + 255) / 256 * ((steps + r - 1) / r * 1850 + 14000) + (r > 1 ? r * n * 105 : 0);
                 if (time < least) least = time, runs = r;
             }

@@ -134,6 +134,20 @@ def test_workspaces():
     assert lib.poseidon_embed_backward_workspace(64, 100, 64) > 0
 
 
+def test_the_workspace_of_a_weight_gradient_is_bounded():
+    """Parts of the rows take at most 1 GB however large the gradient is, and a copy of dy at most 8 GB."""
+    f, rng = L.lib().poseidon_weight_gradient_workspace, np.random.default_rng(0)
+    sizes = [(1 << 20, 32776, 32776, 1), (65536, 8200, 8200, 1), (65536, 16640, 16640, 1), (1 << 20, 2048, 2048, 64)]
+    sizes += [(int(2 ** rng.uniform(0, 21)), 8 * int(2 ** rng.uniform(0, 13)), int(2 ** rng.uniform(0, 16)),
+               int(2 ** rng.uniform(0, 8)) if rng.random() < 0.5 else 1) for _ in range(20000)]
+    for size in sizes:
+        need, tables = f(*size), 32 * (size[3] + 2 * 1024) + 1024
+        assert need == 2 ** 64 - 1 or need <= (1 << 30) + tables, size
+        odd = f(size[0], size[1] + 3, *size[2:])
+        assert odd == 2 ** 64 - 1 or odd <= (1 << 30) + tables + (8 << 30), size
+    assert f(8192, 5120, 3584, 1) == 2 * 5120 * 3584 * 4        # in two parts
+
+
 def test_the_binding_refuses_what_is_not_on_the_gpu():
     x = torch.zeros(4, 64)
     s = L.Stash(torch.zeros(4, 64, dtype=torch.int8), torch.zeros(4, 1, dtype=torch.uint8), 64, torch.float32)
