@@ -5,8 +5,8 @@ and marshals arguments and allocates outputs and workspaces with torch.  All
 tensors live on one GPU.  Matrices are 2-D with neighbouring values in a row;
 any row pitch is taken as it is, any other layout of an input is copied first.
 Work is enqueued on ``stream`` (a ``torch.cuda.Stream`` or a raw ``hipStream_t``
-integer; default: torch's current stream of the tensors' GPU), on which the
-outputs are allocated too.  Nothing synchronises.  What is refused raises
+integer, of the tensors' GPU; default: torch's current stream there), on which
+the outputs are allocated too.  Nothing synchronises.  What is refused raises
 ``PoseidonError`` before anything is enqueued.
 """
 from __future__ import annotations
@@ -148,6 +148,8 @@ def _streamed(f):
         if not isinstance(stream, torch.cuda.Stream):
             device = held[0].device if held else None    # a raw stream is one of the tensors' GPU
             stream = torch.cuda.ExternalStream(stream, device) if stream else torch.cuda.default_stream(device)
+        elif any(t.device != stream.device for t in held):
+            _refuse(f"{f.__name__}: stream: not of the tensors' GPU")
         with torch.cuda.stream(stream):
             out = f(*args, **kw)
         for t in held:

@@ -163,6 +163,33 @@ def test_the_binding_refuses_what_is_not_on_the_gpu():
         assert ei.value.status == BAD
 
 
+def test_the_binding_refuses_a_stream_of_another_gpu(monkeypatch):
+    """Work would be enqueued on the tensors' GPU's current stream, and not on the one that was asked for."""
+    class Tensor:                              # what the binding asks of the memory that a stash holds
+        is_cuda, device, streams = True, torch.device("cuda", 0), []
+
+        def record_stream(self, stream):
+            self.streams.append(stream)
+
+    class Stash(L.Stash):
+        def tensors(self):
+            return (Tensor(),)
+
+    class Stream:
+        def __init__(self, index):
+            self.device = torch.device("cuda", index)
+    monkeypatch.setattr(torch.cuda, "Stream", Stream)
+    s = Stash(torch.zeros(4, 64, dtype=torch.int8), torch.zeros(4, 1, dtype=torch.uint8), 64, torch.float32)
+    calls = []
+    f = L._streamed(lambda stash: calls.append(stash))
+    own = Stream(0)
+    f(s, stream=own)
+    assert calls == [s] and Tensor.streams == [own]
+    with pytest.raises(P.PoseidonError) as ei:
+        f(s, stream=Stream(1))
+    assert ei.value.status == BAD and len(calls) == 1
+
+
 # ---- the oracle against itself ----
 
 def test_the_8_bit_form_holds_its_bounds():
