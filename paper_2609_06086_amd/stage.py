@@ -12,7 +12,7 @@ from __future__ import annotations
 
 import argparse
 import statistics
-from dataclasses import dataclass
+from dataclasses import dataclass, replace
 from typing import List, Optional
 
 import numpy as np
@@ -141,11 +141,17 @@ class ExpertBlock:
 
 @dataclass
 class LayerProfile:
-    """One layer kind: times of a micro-batch, bytes of its weights and their gradients, bytes a micro-batch keeps."""
+    """One layer kind: times of a micro-batch, bytes of its weights and their gradients, bytes a micro-batch keeps, and
+    what it would keep with its activations in their own 16 bits."""
     fwd_us: float
     bwd_us: float
     weight_bytes: int
     kept_bytes: int
+    plain_bytes: int = 0
+
+    def in_16_bits(self) -> "LayerProfile":
+        """The same times with the memory of 16 bits: what a plan gains by the 8 bits' memory alone."""
+        return replace(self, kept_bytes=self.plain_bytes)
 
 
 def _median_us(f, repeats: int) -> float:
@@ -161,7 +167,8 @@ def _median_us(f, repeats: int) -> float:
 
 
 def measure(shape: Shape, device=None, keep_8_bits: bool = True, repeats: int = 5):
-    """(profile of the embedding, profile of an expert block) on this GPU."""
+    """(profile of the embedding, profile of an expert block) on this GPU.  The layers run with their activations kept in 8
+    bits; keep_8_bits False gives those times with the bytes that 16 bits would keep."""
     device = torch.device("cuda", torch.cuda.current_device()) if device is None else device
     g = torch.Generator(device=device)
     g.manual_seed(1)
@@ -172,10 +179,12 @@ def measure(shape: Shape, device=None, keep_8_bits: bool = True, repeats: int = 
     dout = (torch.randn(out.shape, generator=g, device=device) * 0.01).to(out.dtype)
     dx = block.backward(dout, kept)
     first.backward(dx, ids)
-    return (LayerProfile(_median_us(lambda: first.forward(ids), repeats), _median_us(lambda: first.backward(dx, ids), repeats),
-                         first.weight_bytes, ids.numel() * 4),
-            LayerProfile(_median_us(lambda: block.forward(x), repeats), _median_us(lambda: block.backward(dout, kept), repeats),
-                         block.weight_bytes, kept.kept_bytes if keep_8_bits else kept.plain_bytes))
+    profiles = (LayerProfile(_median_us(lambda: first.forward(ids), repeats), _median_us(lambda: first.backward(dx, ids), repeats),
+                             first.weight_bytes, ids.numel() * 4, ids.numel() * 4),
+                LayerProfile(_median_us(lambda: block.forward(x), repeats),
+                             _median_us(lambda: block.backward(dout, kept), repeats), block.weight_bytes, kept.kept_bytes,
+                             kept.plain_bytes))
+    return profiles if keep_8_bits else tuple(p.in_16_bits() for p in profiles)
 
 
 def plan_problem(first: LayerProfile, block: LayerProfile, blocks: int, stages: int, micro_batches: int, *,
@@ -206,11 +215,10 @@ def main() -> None:
     ap.add_argument("--cap-mb", type=int, default=0, help="memory of a device (default: 5% above an even share)")
     a = ap.parse_args()
     shape = Shape(width=a.width, experts=a.experts, chosen=a.chosen, inner=a.inner, tokens=a.tokens)
-    cap = a.cap_mb
-    for kept, eight in (("8 bits", True), ("16 bits", False)):
-        first, block = measure(shape, keep_8_bits=eight)
-        cap = cap or int(1.05 * -(-a.blocks // a.stages) *
-                         (block.weight_bytes + min(a.stages, a.micro_batches) * block.kept_bytes) / 1e6)
+    first, eight = measure(shape)
+    cap = a.cap_mb or int(1.05 * -(-a.blocks // a.stages) *
+                          (eight.weight_bytes + min(a.stages, a.micro_batches) * eight.kept_bytes) / 1e6)
+    for kept, block in (("8 bits", eight), ("16 bits (memory alone, times of 8 bits)", eight.in_16_bits())):
         prob = plan_problem(first, block, a.blocks, a.stages, a.micro_batches, caps_mb=(cap, cap))
         ctx = P.poseidon_load_costs(prob, torch.cuda.current_device())
         best, _ = P.poseidon_search(ctx, rows_per_chunk=64, ramp=True)

@@ -1,4 +1,6 @@
 """The stage's layers: their gradients against a 64-bit model, and a plan from measured layers."""
+import re
+
 import numpy as np
 import pytest
 
@@ -79,3 +81,22 @@ def test_a_plan_from_measured_layers():
     best, _ = P.poseidon_search(ctx, rows_per_chunk=0)
     ctx.close()
     assert (best.index, best.makespan) == coracle.search(prob, 2 ** 31 - 1, rows_per_chunk=0)["best"]
+
+
+@pytest.mark.gpu
+def test_the_command_says_whose_times_it_plans_with(monkeypatch, capsys):
+    """Layers run with activations in 8 bits only: a plan for 16 bits has the same times, and says so."""
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    monkeypatch.setattr("sys.argv", "stage --tokens 200 --width 128 --experts 5 --inner 192 --blocks 7 --stages 3 "
+                                    "--micro-batches 8 --cap-mb 200".split())
+    S.main()
+    eight, sixteen = capsys.readouterr().out.splitlines()
+    assert "in 8 bits" in eight and "in 16 bits" in sixteen and "times of 8 bits" in sixteen
+
+    def times(line):
+        return re.search(r"block (\d+ \+ \d+) us", line).group(1)
+
+    def kept(line):
+        return float(re.search(r"keeps ([\d.]+) MB", line).group(1))
+    assert times(eight) == times(sixteen) and kept(eight) < 0.62 * kept(sixteen)
