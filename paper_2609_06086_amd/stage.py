@@ -212,7 +212,7 @@ def main() -> None:
     ap.add_argument("--blocks", type=int, default=23)
     ap.add_argument("--stages", type=int, default=4)
     ap.add_argument("--micro-batches", type=int, default=32)
-    ap.add_argument("--cap-mb", type=int, default=0, help="memory of a device (default: 5% above an even share)")
+    ap.add_argument("--cap-mb", type=int, default=0, help="memory of a device (default: 5%% above an even share)")
     a = ap.parse_args()
     shape = Shape(width=a.width, experts=a.experts, chosen=a.chosen, inner=a.inner, tokens=a.tokens)
     first, eight = measure(shape)

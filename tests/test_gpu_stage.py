@@ -100,3 +100,10 @@ def test_the_command_says_whose_times_it_plans_with(monkeypatch, capsys):
     def kept(line):
         return float(re.search(r"keeps ([\d.]+) MB", line).group(1))
     assert times(eight) == times(sixteen) and kept(eight) < 0.62 * kept(sixteen)
+
+
+def test_the_command_explains_its_options(monkeypatch, capsys):
+    monkeypatch.setattr("sys.argv", ["stage", "--help"])
+    with pytest.raises(SystemExit) as ei:
+        S.main()
+    assert ei.value.code == 0 and "default: 5% above an even share" in " ".join(capsys.readouterr().out.split())
