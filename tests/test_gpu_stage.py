@@ -106,4 +106,5 @@ def test_the_command_explains_its_options(monkeypatch, capsys):
     monkeypatch.setattr("sys.argv", ["stage", "--help"])
     with pytest.raises(SystemExit) as ei:
         S.main()
-    assert ei.value.code == 0 and "default: 5% above an even share" in " ".join(capsys.readouterr().out.split())
+    text = " ".join(capsys.readouterr().out.split())
+    assert ei.value.code == 0 and "default: 5% above an even share" in text and "argparse" not in text
