@@ -141,13 +141,14 @@ class ExpertBlock:
 
 @dataclass
 class LayerProfile:
-    """One layer kind: times of a micro-batch, bytes of its weights and their gradients, bytes a micro-batch keeps, and
-    what it would keep with its activations in their own 16 bits."""
+    """One layer kind: times of a micro-batch, bytes of its weights and their gradients, bytes a micro-batch keeps, what
+    it would keep with its activations in their own 16 bits, and the most that a pass works with besides."""
     fwd_us: float
     bwd_us: float
     weight_bytes: int
     kept_bytes: int
     plain_bytes: int = 0
+    work_bytes: int = 0
 
     def in_16_bits(self) -> "LayerProfile":
         """The same times with the memory of 16 bits: what a plan gains by the 8 bits' memory alone."""
@@ -166,6 +167,15 @@ def _median_us(f, repeats: int) -> float:
     return statistics.median(times)
 
 
+def _work_bytes(f, device) -> int:
+    """The most that a call of f has allocated at a time, but for what it keeps beside its output."""
+    torch.cuda.reset_peak_memory_stats(device)
+    result = f()
+    out = result[0] if isinstance(result, tuple) else result
+    stays = torch.cuda.memory_allocated(device) - (0 if out is None else out.numel() * out.element_size())
+    return max(0, torch.cuda.max_memory_allocated(device) - stays)
+
+
 def measure(shape: Shape, device=None, keep_8_bits: bool = True, repeats: int = 5):
     """(profile of the embedding, profile of an expert block) on this GPU.  The layers run with their activations kept in 8
     bits; keep_8_bits False gives those times with the bytes that 16 bits would keep."""
@@ -179,11 +189,14 @@ def measure(shape: Shape, device=None, keep_8_bits: bool = True, repeats: int = 
     dout = (torch.randn(out.shape, generator=g, device=device) * 0.01).to(out.dtype)
     dx = block.backward(dout, kept)
     first.backward(dx, ids)
-    profiles = (LayerProfile(_median_us(lambda: first.forward(ids), repeats), _median_us(lambda: first.backward(dx, ids), repeats),
-                             first.weight_bytes, ids.numel() * 4, ids.numel() * 4),
-                LayerProfile(_median_us(lambda: block.forward(x), repeats),
-                             _median_us(lambda: block.backward(dout, kept), repeats), block.weight_bytes, kept.kept_bytes,
-                             kept.plain_bytes))
+
+    def profile(layer, forward, backward, kept_bytes, plain_bytes):
+        work = max(_work_bytes(forward, device), _work_bytes(backward, device))
+        return LayerProfile(_median_us(forward, repeats), _median_us(backward, repeats), layer.weight_bytes, kept_bytes,
+                            plain_bytes, work)
+
+    profiles = (profile(first, lambda: first.forward(ids), lambda: first.backward(dx, ids), ids.numel() * 4, ids.numel() * 4),
+                profile(block, lambda: block.forward(x), lambda: block.backward(dout, kept), kept.kept_bytes, kept.plain_bytes))
     return profiles if keep_8_bits else tuple(p.in_16_bits() for p in profiles)
 
 
@@ -191,15 +204,17 @@ def plan_problem(first: LayerProfile, block: LayerProfile, blocks: int, stages: 
                  slower=(1.0, 1.7), caps_mb=(65536, 65536), link_us: int = 100, assign: Optional[np.ndarray] = None) -> Problem:
     """The planner's tables for an embedding and `blocks` expert blocks: times on each device type (`slower`: times this
     GPU's), memory of a layer = weights, their gradients and what min(stages, micro_batches) micro-batches in flight
-    keep."""
+    keep.  A device runs one pass at a time, so its cap is less what the largest works with."""
     profiles = [first] + [block] * blocks
     flight = min(stages, micro_batches)
     fwd, bwd = (np.array([[max(1, round(getattr(p, name) * s)) for p in profiles] for s in slower], np.uint32)
                 for name in ("fwd_us", "bwd_us"))
     mem = np.array([-(-(p.weight_bytes + flight * p.kept_bytes) // 10 ** 6) for p in profiles], np.uint32)
+    work = -(-max(p.work_bytes for p in profiles) // 10 ** 6)
+    caps = np.array([max(0, cap - work) for cap in caps_mb], np.uint32)
     comm = np.full(stages - 1, link_us, np.uint32)
-    return Problem(len(profiles), stages, micro_batches, len(slower), fwd, bwd, comm, comm, mem,
-                   np.array(caps_mb, np.uint32), assign)
+    return Problem(len(profiles), stages, micro_batches, len(slower), fwd, bwd, comm, comm, mem, caps,
+                   assign)
 
 
 def main() -> None:
@@ -212,12 +227,14 @@ def main() -> None:
     ap.add_argument("--blocks", type=int, default=23)
     ap.add_argument("--stages", type=int, default=4)
     ap.add_argument("--micro-batches", type=int, default=32)
-    ap.add_argument("--cap-mb", type=int, default=0, help="memory of a device (default: 5%% above an even share)")
+    ap.add_argument("--cap-mb", type=int, default=0,
+                    help="memory of a device (default: 5%% above an even share, and what a pass works with)")
     a = ap.parse_args()
     shape = Shape(width=a.width, experts=a.experts, chosen=a.chosen, inner=a.inner, tokens=a.tokens)
     first, eight = measure(shape)
     cap = a.cap_mb or int(1.05 * -(-a.blocks // a.stages) *
-                          (eight.weight_bytes + min(a.stages, a.micro_batches) * eight.kept_bytes) / 1e6)
+                          (eight.weight_bytes + min(a.stages, a.micro_batches) * eight.kept_bytes) / 1e6 +
+                          eight.work_bytes / 1e6)
     for kept, block in (("8 bits", eight), ("16 bits (memory alone, times of 8 bits)", eight.in_16_bits())):
         prob = plan_problem(first, block, a.blocks, a.stages, a.micro_batches, caps_mb=(cap, cap))
         ctx = P.poseidon_load_costs(prob, torch.cuda.current_device())
@@ -225,7 +242,8 @@ def main() -> None:
         ctx.close()
         found = f"best plan {best.index}, {best.makespan} us a step" if best.index is not None else "no plan fits"
         print(f"activations in {kept}: block {block.fwd_us:.0f} + {block.bwd_us:.0f} us, keeps "
-              f"{block.kept_bytes / 1e6:.1f} MB of a micro-batch; devices of {cap} MB: {found}", flush=True)
+              f"{block.kept_bytes / 1e6:.1f} MB of a micro-batch, works with "
+              f"{block.work_bytes / 1e6:.1f} MB; devices of {cap} MB: {found}", flush=True)
 
 
 if __name__ == "__main__":

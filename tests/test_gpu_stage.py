@@ -26,6 +26,27 @@ def test_plan_problem_fills_the_tables():
     assert prob.mem.tolist() == [101] + [260] * 5 and prob.cap.tolist() == [1000, 900]
 
 
+def test_plan_problem_leaves_room_for_a_pass():
+    """What the largest pass works with is free on every device, once; a device that has less holds nothing."""
+    first, block = (S.LayerProfile(p.fwd_us, p.bwd_us, p.weight_bytes, p.kept_bytes, work_bytes=w)
+                    for p, w in zip(_profiles(), (10 ** 6, 150 * 10 ** 6 + 1)))
+    prob = S.plan_problem(first, block, blocks=5, stages=3, micro_batches=2, caps_mb=(1000, 90))
+    assert prob.cap.tolist() == [849, 0] and prob.mem.tolist() == [101] + [260] * 5
+
+
+@pytest.mark.gpu
+def test_the_measured_memory_of_a_pass():
+    """At least what the block's backward pass holds at once: the restored outputs and their gradient, then both
+    gradients of the gated activation, dact and the activation, in 16 bits; at most a few times that, and no weights."""
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    shape = S.Shape(vocab=300, width=256, experts=5, chosen=2, inner=192, tokens=4000)
+    first, block = S.measure(shape, repeats=2)
+    rows, least = shape.tokens * shape.chosen, 2 * shape.tokens * shape.chosen * (2 * shape.width + 4 * shape.inner)
+    assert least <= block.work_bytes <= 3 * least + rows * 200 + (64 << 20)
+    assert shape.tokens * shape.width * 2 <= first.work_bytes <= (64 << 20)
+
+
 @pytest.mark.gpu
 def test_gradients_of_the_block_and_the_embedding():
     """Against a model in 64 bits on the same weights and the same choices.  A kept value is off by 0.011 of its
@@ -99,6 +120,7 @@ def test_the_command_says_whose_times_it_plans_with(monkeypatch, capsys):
 
     def kept(line):
         return float(re.search(r"keeps ([\d.]+) MB", line).group(1))
+    assert times(eight) == times(sixteen) and kept(eight) < 0.62 * kept(sixteen)
     assert times(eight) == times(sixteen) and kept(eight) < 0.62 * kept(sixteen)
 
 
