@@ -89,8 +89,9 @@ int poseidon_gated_backward(const void *dout, uint64_t dout_pitch, uint32_t type
  * added to what grad holds where `accumulate` is 1 (the micro-batches of a step).  An empty range gives zeros.
  * offsets: DEVICE int32[n_ranges + 1], non-decreasing, range r = rows [offsets[r], offsets[r + 1]) (each cut to
  *   [0, rows]; empty if it ends before it begins); NULL with n_ranges == 1: all rows.
- * type: of dy, POSEIDON_F16 or POSEIDON_BF16; x is brought to it (nothing is lost for POSEIDON_BF16, or if x was
- *   kept from POSEIDON_F16; else what leaves the range of POSEIDON_F16 is held to it).  grad: [n_ranges][out_width][in_width] of
+ * type: of dy, POSEIDON_F16 or POSEIDON_BF16; x is brought to it.  Nothing is lost for POSEIDON_BF16, or if x was kept
+ *   from POSEIDON_F16; else what leaves the range of POSEIDON_F16 is held to +-65504, and a value below 2^-14 loses what
+ *   lies below 2^-24 (it is rounded toward zero).  grad: [n_ranges][out_width][in_width] of
  *   grad_type without gaps. */
 int poseidon_weight_gradient(const void *dy, uint64_t dy_pitch, uint32_t type, uint64_t rows, uint64_t out_width,
                              const int8_t *codes, const uint8_t *scales, uint64_t in_width, const int32_t *offsets,

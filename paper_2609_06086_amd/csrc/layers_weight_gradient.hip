@@ -35,7 +35,9 @@ __device__ __forceinline__ Acc mfma<F16>(Words4 a, Words4 b, Acc c) {
                                                   0, 0);
 }
 
-// Two values that the type holds exactly, as a pair.
+// Two values as a pair.  BF16 holds every kept value exactly, and F16 those that were kept from it.  Of the others, this
+// conversion toward zero holds large ones to the type's last finite value in the same instruction, which rounding to nearest
+// would make infinite, and cuts what lies below 2^-24 off small ones: at most 2^-24, where nearest is 2^-25.
 template <class T>
 __device__ __forceinline__ uint32_t pack(float lo, float hi);
 template <>

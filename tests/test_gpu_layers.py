@@ -355,6 +355,31 @@ def test_weight_gradient_of_the_least_values(dev, kind, low, high, o):
     assert (L.poseidon_weight_gradient(dy, L.poseidon_stash(x)).double() == 16 * 2.0 ** (low + high)).all()
 
 
+def _brought(x, kind):
+    """Kept values x (64 bits) as operands of `kind`: f16 holds what leaves its range to its largest value, and drops what lies
+    below its least step."""
+    if kind != "f16":
+        return x
+    x = x.clamp(-65504, 65504)
+    return torch.where(x.abs() < 2.0 ** -14, torch.trunc(x * 2.0 ** 24) * 2.0 ** -24, x)
+
+
+@pytest.mark.parametrize("kind, kept", [("f16", "bf16"), ("f16", "f32"), ("bf16", "f16"), ("bf16", "f32")])
+@pytest.mark.parametrize("o", [72, 67])
+def test_weight_gradient_of_rows_kept_from_another_type(dev, kind, kept, o):
+    """x over all of its own type's range and beyond f16's, both ends; the sums' bound on the operands as they are defined."""
+    rng = np.random.default_rng(11)
+    rows, i = 300, 200
+    dy, x = _make(rng, (rows, o), kind, dev, spread=0.5), _make(rng, (rows, i), kept, dev, spread=1.0)
+    high = 40 if kept != "f16" else 0
+    x.mul_(torch.exp2(torch.linspace(-40 if kept != "f16" else -14, high, rows, device=dev)).to(x.dtype).unsqueeze(1))
+    s = L.poseidon_stash(x)
+    back = _brought(L.poseidon_restore(s, dtype=torch.float32).double(), kind)
+    left = dy.double().t().contiguous()
+    want, size = (left @ back).cpu().numpy(), (rows + 2) * V * (left.abs() @ back.abs()).cpu().numpy()
+    _check(L.poseidon_weight_gradient(dy, s), want, size, "f32")
+
+
 # ---- experts ----
 
 BATCHES = [(1, 1, 1), (1, 8, 64), (5, 2, 3), (100, 3, 8), (700, 8, 33), (2100, 2, 511), (33000, 4, 256), (300000, 2, 64)]
