@@ -5,6 +5,8 @@ place at the lower end of a binade), STEP half of the least step below the norma
 A sum of n products in 32 bits is off by at most (n + 2) V times the sum of their absolute values, whatever its
 order.
 """
+from concurrent.futures import ThreadPoolExecutor
+
 import numpy as np
 import pytest
 
@@ -380,6 +382,26 @@ def test_weight_gradient_of_rows_kept_from_another_type(dev, kind, kept, o):
     _check(L.poseidon_weight_gradient(dy, s), want, size, "f32")
 
 
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("rows, o, i, ranges, pad", [(6000, 2040, 1365, 0, 0), (6000, 2043, 1365, 0, 0), (24000, 2041, 2050, 24, 0),
+                                                     (24000, 2040, 2050, 24, 0), (2048, 1408, 1536, 0, 0),
+                                                     (2048, 1024, 2048, 0, 0), (6000, 2040, 1365, 0, 1), (2048, 1413, 1536, 0, 1)])
+def test_weight_gradient_of_large_calls_by_type(dev, kind, rows, o, i, ranges, pad):
+    """Every tile and split in both types, whole and copied dy, and dy on an odd pitch, which no large tile takes."""
+    g = torch.Generator(device=dev)
+    g.manual_seed(rows + o)
+    dy = torch.randn(rows, o + pad, generator=g, device=dev).to(KIND[kind])[:, pad:]
+    s = L.poseidon_stash(torch.randn(rows, i, generator=g, device=dev).to(KIND[kind]))
+    back = L.poseidon_restore(s, dtype=torch.float32).double()
+    cuts = sorted([0, rows, 1, 65] + torch.randint(0, rows, (ranges - 3,), generator=g, device=dev).tolist()) if ranges else [0, rows]
+    at = torch.tensor(cuts, dtype=torch.int32, device=dev) if ranges else None
+    got = L.poseidon_weight_gradient(dy, s, offsets=at).view(-1, o, i)
+    for r, (a, b) in enumerate(zip(cuts, cuts[1:])):
+        left = dy[a:b].double().t().contiguous()
+        want, size = left @ back[a:b], (b - a + 2) * V * (left.abs() @ back[a:b].abs())
+        assert ((got[r].double() - want).abs() <= size + ROUND["f32"] * want.abs() + STEP["f32"]).all()
+
+
 # ---- experts ----
 
 BATCHES = [(1, 1, 1), (1, 8, 64), (5, 2, 3), (100, 3, 8), (700, 8, 33), (2100, 2, 511), (33000, 4, 256), (300000, 2, 64)]
@@ -532,6 +554,110 @@ def test_embedding_gradient_of_a_table_past_32_gib(dev):
         assert not out[a:min(a + (1 << 20), vocab - 1)].any()
 
 
+def test_calls_of_no_rows(dev):
+    """Every operator takes no rows, and writes what depends on none."""
+    x, ids = torch.zeros(0, 70, dtype=torch.bfloat16, device=dev), torch.zeros(0, dtype=torch.int32, device=dev)
+    s = L.poseidon_stash(x)
+    assert L.poseidon_restore(s).shape == (0, 70)
+    out, gate, up = L.poseidon_gated_forward(x, x)
+    assert out.shape == (0, 70) and all(t.shape == (0, 70) for t in L.poseidon_gated_backward(x, gate, up))
+    plan = L.poseidon_expert_sort(ids.view(0, 2), 3)
+    w = torch.zeros(0, 2, device=dev)
+    xs, kept = L.poseidon_expert_gather(x, plan, keep=True)
+    assert xs.shape == (0, 70) and kept.codes.shape == (0, 128) and L.poseidon_expert_combine(xs, plan, w).shape == (0, 70)
+    dys, dw = L.poseidon_expert_combine_backward(x, xs, plan, w)
+    assert dys.shape == (0, 70) and dw.shape == (0, 2) and L.poseidon_embed(ids, torch.ones(5, 70, device=dev)).shape == (0, 70)
+    for offsets, shape in ((None, (70, 70)), (plan.offsets, (3, 70, 70))):
+        for value, out in ((0, torch.full(shape, 7.0, device=dev)), (7, torch.full(shape, 7.0, device=dev))):
+            L.poseidon_weight_gradient(x, s, offsets=offsets, out=out, accumulate=bool(value))
+            assert (out == value).all()
+
+
+# ---- long calls: the variants that stream, or take several slices a lane or several launches ----
+
+@pytest.mark.parametrize("kind, tokens, width", [("f32", 16301, 1025), ("f32", 40001, 1025), ("bf16", 16301, 1027),
+                                                 ("bf16", 70001, 1025), ("f16", 2100003, 3)])
+def test_long_lookups(dev, kind, tokens, width):
+    """A product of two 32-bit values, rounded to the type, is the same in any order."""
+    g = torch.Generator(device=dev)
+    g.manual_seed(tokens)
+    table = torch.randn(3001, width, generator=g, device=dev).to(KIND[kind])
+    ids = torch.randint(-1, 3002, (tokens,), generator=g, device=dev, dtype=torch.int32)
+    there = ((ids >= 0) & (ids < 3001)).unsqueeze(1)
+    want = torch.where(there, table[ids.clamp(0, 3000).long()].float() * 1.7, torch.zeros((), device=dev)).to(KIND[kind])
+    assert torch.equal(L.poseidon_embed(ids, table, 1.7), want)
+
+
+@pytest.mark.parametrize("kind, width", [("f32", 2501), ("f16", 5003), ("bf16", 5003)])
+def test_long_batches_of_experts(dev, kind, width):
+    g = torch.Generator(device=dev)
+    g.manual_seed(width)
+    n, k, e = 9001, 3, 40
+    choice = torch.randint(-1, e, (n, k), generator=g, device=dev, dtype=torch.int32)
+    plan = L.poseidon_expert_sort(choice, e)
+    kept_places, position = int(plan.offsets[-1]), plan.position.long()
+    x, dout = (torch.randn(n, width, generator=g, device=dev).to(KIND[kind]) for _ in range(2))
+    xs, kept = L.poseidon_expert_gather(x, plan, keep=True)
+    want = x[plan.order.long() // k]
+    want[kept_places:] = 0
+    assert torch.equal(xs, want) and torch.equal(L.poseidon_expert_gather(x, plan)[0], want)
+    s = L.poseidon_stash(want)
+    assert torch.equal(kept.codes, s.codes) and torch.equal(kept.scales, s.scales)
+    ys = torch.randn(n * k, width, generator=g, device=dev).to(KIND[kind])
+    ys[kept_places:] = float("nan")
+    w = torch.rand(n, k, generator=g, device=dev)
+    out, plain = L.poseidon_expert_combine(ys, plan, w), L.poseidon_expert_combine(ys, plan)
+    dys, dw = L.poseidon_expert_combine_backward(dout, ys, plan, w)
+    rows = torch.where((position >= 0).unsqueeze(2), ys[position.clamp(min=0)], ys.new_zeros(())).double()
+
+    def near(got, want, slack, kind):
+        return ((got.double() - want).abs() <= slack + ROUND[kind] * (want.abs() + slack) + STEP[kind]).all()
+    for got, by in ((out, w.double()), (plain, torch.ones(n, k, dtype=torch.float64, device=dev))):
+        by = by.unsqueeze(2)
+        assert near(got, (rows * by).sum(1), (k + 2) * V * (rows * by).abs().sum(1), kind)
+    d = dout.double().unsqueeze(1)
+    assert near(dw, (rows * d).sum(2), (width + 2) * V * (rows * d).abs().sum(2), "f32")
+    flat = plan.order.long()
+    want = (w.view(-1)[flat].unsqueeze(1) * dout.float()[flat // k]).to(KIND[kind])    # one product, rounded to the type
+    want[kept_places:] = 0
+    assert torch.equal(dys, want)
+
+
+def test_combination_gradient_of_many_places(dev):
+    """More places than a launch takes, of one value each: every result is one product."""
+    n = (1 << 25) + 3
+    g = torch.Generator(device=dev)
+    g.manual_seed(1)
+    choice = torch.randint(-1, 2, (n, 1), generator=g, device=dev, dtype=torch.int32)
+    plan = L.poseidon_expert_sort(choice, 2)
+    ys, dout, w = (torch.randn(n, 1, generator=g, device=dev) for _ in range(3))
+    dys, dw = L.poseidon_expert_combine_backward(dout, ys, plan, w)
+    here, flat = int(plan.offsets[-1]), plan.order.long()
+    assert torch.equal(dys[:here], (w * dout)[flat[:here]]) and dys[here:].count_nonzero() == 0
+    assert torch.equal(dw, torch.where(plan.position >= 0, dout * ys[plan.position.clamp(min=0).long().view(-1)], torch.zeros((), device=dev)))
+
+
+@pytest.mark.parametrize("kind, vocab, width", [("bf16", 1000, 230), ("f32", 70000, 120)])
+def test_embedding_gradient_of_many_tokens(dev, kind, vocab, width):
+    """Two passes of the sort over more blocks than add up the counts before them, beside a clear in parts."""
+    tokens = 600001
+    g = torch.Generator(device=dev)
+    g.manual_seed(vocab)
+    ids = torch.randint(-1, vocab + 1, (tokens,), generator=g, device=dev, dtype=torch.int32)
+    ids[torch.rand(tokens, generator=g, device=dev) < 0.3] = vocab - 7      # a frequent one
+    dout = torch.randn(tokens, width, generator=g, device=dev).to(KIND[kind])
+    got = L.poseidon_embed_backward(ids, dout, vocab, 1.25, out=torch.full((vocab, width), 7.0, device=dev))
+    assert torch.equal(got, L.poseidon_embed_backward(ids, dout, vocab, 1.25))
+    fine = (ids >= 0) & (ids < vocab)
+    at = ids[fine].long()
+
+    def sums(rows):
+        return torch.zeros(vocab, width, dtype=torch.float64, device=dev).index_add_(0, at, rows)
+    d = dout[fine].double() * 1.25
+    want, size = sums(d), (torch.bincount(at, minlength=vocab).unsqueeze(1) + 2) * V * sums(d.abs())
+    assert ((got.double() - want).abs() <= size + ROUND["f32"] * want.abs()).all()
+
+
 # ---- addresses, streams, graphs ----
 
 def test_offsets_past_32_bits(dev):
@@ -604,6 +730,55 @@ def test_other_streams(dev):
         back = L.poseidon_restore(s, stream=stream)
         torch.cuda.synchronize()
         assert torch.equal(back, L.poseidon_restore(L.poseidon_stash(args[0])))
+
+
+def _with_workspaces(x, ids, choice, e, **kw):
+    """The operators that bring a workspace of their own."""
+    plan = L.poseidon_expert_sort(choice, e, **kw)
+    kept = L.poseidon_stash(x, **kw)
+    half = torch.tensor([0, x.shape[0] // 3, x.shape[0]], dtype=torch.int32, device=x.device)
+    return [plan.order, plan.position, plan.offsets, L.poseidon_weight_gradient(x, kept, **kw),
+            L.poseidon_weight_gradient(x, kept, offsets=half, **kw), L.poseidon_embed_backward(ids, x, 50, 2.0, **kw)]
+
+
+def _long_inputs(dev, seed):
+    g = torch.Generator(device=dev)
+    g.manual_seed(seed)
+    n = 9000
+    return (torch.randn(n, 136, generator=g, device=dev).bfloat16(),
+            torch.randint(-1, 50, (n,), generator=g, device=dev, dtype=torch.int32),
+            torch.randint(-1, 6, (n, 2), generator=g, device=dev, dtype=torch.int32), 6)
+
+
+def test_workspaces_on_named_streams(dev):
+    """Two streams at once, each call with a workspace that belongs to its stream."""
+    batches = [_long_inputs(dev, seed) for seed in (1, 2)]
+    want = [_with_workspaces(*b) for b in batches]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in batches]
+    for _ in range(3):
+        got = [_with_workspaces(*b, stream=s) for b, s in zip(batches, streams)]
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_threads(dev):
+    """Calls from several threads, each with a stream of its own, give what they give alone."""
+    batches = [_long_inputs(dev, seed) for seed in range(4)]
+    want = [_with_workspaces(*b) for b in batches]
+    torch.cuda.synchronize()
+
+    def work(batch):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            got = [_with_workspaces(*batch) for _ in range(5)]
+        stream.synchronize()
+        return got
+    with ThreadPoolExecutor(max_workers=4) as pool:
+        results = list(pool.map(work, batches))
+    for got, w in zip(results, want):
+        assert all(torch.equal(x, y) for one in got for x, y in zip(one, w))
 
 
 def test_capture_and_replay(dev):
