@@ -39,7 +39,7 @@ struct Clear {
 
 // Block `block` of `blocks`: a row, or of one row (a table without gaps) a piece of 16 bytes a thread, and what lies
 // whole grids further.  Many blocks of one store a thread fill at 6.7 TB/s, blocks that go on through the memory in
-// strides at 4.4 to 5.6: only above kClearMost blocks (64 GB without gaps) do they go on.
+// strides at 4.4 to 5.6: only above kClearMost blocks (32 GiB without gaps in a launch) do they go on.
 constexpr uint64_t kClearPiece = (uint64_t)kSortThreads * 16, kClearMost = 1u << 22;
 
 __device__ __forceinline__ void clear(const Clear &c, uint32_t block, uint32_t blocks) {

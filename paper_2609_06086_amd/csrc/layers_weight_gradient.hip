@@ -9,8 +9,8 @@
 // instruction wants eight neighbouring rows of one column in a lane, so a
 // thread loads an 8 x 8 block (eight rows of eight columns: coalesced), turns
 // it in registers with byte permutes, and writes each column's eight rows as 16
-// bytes to LDS, where a column's 64 rows of a step lie together.  Half of the
-// waves bring dy, the other half the codes, which they also unpack and scale.
+// bytes to LDS, where a column's 64 rows of a step lie together.  Every thread
+// brings a block of dy and one of the codes, which it also unpacks and scales.
 #include "layers_device.h"
 
 namespace pl {
@@ -267,16 +267,17 @@ __device__ __forceinline__ Rsrc buffer(const void *p, uint32_t bytes) {
 // A thread brings 8 rows of C columns of each operand.
 //
 // C = 8, 256 x 256: a wave reads 8 KB of LDS for 16 matrix instructions of 32 cycles, half of what LDS
-// delivers (8 waves of 128 x 64 would ask for three quarters, and the writes come on top).  With 256
+// delivers, and a quarter more is written (by count, 8 waves of 128 x 64 would read three quarters; not measured).  With 256
 // sums a lane there is one wave a SIMD, so nothing hides behind another wave: LDS holds two
 // steps, and while the matrix instructions work on one, the rows of the next are turned and
 // unpacked between them; those of the two after are on their way in registers (with only one of them the
 // waits for memory took half of the time).
 // C = 4, 128 x 128: 64 sums a lane and half of the LDS, so that two blocks share a CU.
 //
-// Measured: 16384 x 8192 x 4096 in 946 to 961 us (1150 TFLOP/s; the matrix instructions are busy 58% of the cycles, the rest
-// goes to the instructions between them), 64 ragged ranges of 2048 x 2048 over 65536 rows 710 us.  There a unit has 16 steps
-// on average and a start and an end that nothing hides; tried and slower or no faster: the next unit's rows asked for
+// Measured: 16384 x 8192 x 4096 in 946 to 961 us (1150 TFLOP/s).  The matrix instructions are busy 58% of the cycles; beside
+// each of them lie 22 cycles of issue of its 32, and LDS moves data in three quarters of the time that they would take
+// alone: which of the two holds it is not shown.  64 ragged ranges of 2048 x 2048 over 65536 rows take 710 us.  There a unit
+// has 16 steps on average and a start and an end that nothing hides; tried and slower or no faster: the next unit's rows asked for
 // before the stores (705 us), 16 bytes a lane a store (760: pieces of 32 bytes of a line), a range's tiles all on one XCD
 // (756), leaving out the zero step after an odd number (the registers no longer suffice).
 //
@@ -559,7 +560,8 @@ struct WeightPlan {
 
 // Tiles of 256 x 256 where the 256 CUs get 16 steps or more each (1077 TFLOP/s on long sums, 686 with tiles of
 // 128 x 128, which fill the chip with less).  One range: its rows are split until every CU has a block, of
-// 16 (8) steps or more, and a little more than 128 or 256 large tiles, which would leave most of the last round of the CUs
+// 16 (8) steps or more (small tiles with 4: 512 x 1024 x 1024 15 us, 11 with 8 or 16; with 16: 2048 x 512 x 512 19, 15 with 4 or 8;
+// large tiles have 16 wherever they are taken), and a little more than 128 or 256 large tiles, which would leave most of the last round of the CUs
 // idle, in two or three parts where that takes less (16000 x 4104 x 2048, 136 tiles: 316 us instead of 376; 8192 x
 // 5120 x 3584, 280 tiles: 373 instead of 415) (two of the small tiles a CU take longer: 4096 x 1024 x 1024 31 us instead of 29).  Ragged ranges: runs
 // of at most half of a CU's share, and the large tiles from 96 steps a CU on, as there are more units to even out: with
@@ -571,7 +573,9 @@ struct WeightPlan {
 // parts of 1.2 GB; 65536 x 8448 x 8192, two parts of 0.8 GB, 8.8 instead of 9.7).
 //
 // A dy that is no multiple of 8 wide is copied to one that is where that brings the large tiles: 8000 x 2001 x 2048 92 us
-// instead of 133.  Not for an x of few columns (the copy would take as long as it saves), nor for more than 8 GB.
+// instead of 133.  Not for an x of few columns (with 256 the copy loses, 65536 x 2001 180 us against 157; with 384 and 448 it would gain a
+// tenth, 32768 x 2001 x 448 127 against 140; with 512 both take 126 for 16384 x 4001), nor for more than 8 GB, as that
+// memory is the caller's.
 constexpr uint64_t kPartsMost = 1ull << 30;
 
 inline WeightPlan weight_plan(uint64_t rows, uint64_t out_width, uint64_t in_width, uint32_t n_ranges, bool whole) {

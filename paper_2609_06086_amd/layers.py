@@ -3,7 +3,10 @@
 Every operator runs in the HIP library ``libposeidon.so``; this module checks
 and marshals arguments and allocates outputs and workspaces with torch.  All
 tensors live on one GPU.  Matrices are 2-D with neighbouring values in a row;
-any row pitch is taken as it is, any other layout of an input is copied first.
+any row pitch is taken as it is, any other layout of an input is copied first,
+and so are the experts' rows (``ys``) on a pitch.  Results are new tensors without
+a history: autograd does not see these calls, and the backward operators are called
+by name.
 Work is enqueued on ``stream`` (a ``torch.cuda.Stream`` or a raw ``hipStream_t``
 integer, of the tensors' GPU; default: torch's current stream there), on which
 the outputs are allocated too.  Nothing synchronises.  What is refused raises
