@@ -72,8 +72,8 @@ def _function(name: str):
 
 
 class Stash:
-    """Rows kept in 8 bits: int8 codes [rows, groups * 64], uint8 scale bytes [rows, groups], the rows' width and the
-    type they came from.  The operators make theirs in one piece of memory, of which codes and scales are views."""
+    """Rows kept in 8 bits: int8 codes [rows, groups * 64] on a 16-byte boundary, uint8 scale bytes [rows, groups], the
+    rows' width and the type they came from.  The operators make theirs in one piece of memory, of which codes and scales are views."""
     __slots__ = ("rows", "width", "dtype", "_codes", "_scales", "_memory")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, width: int, dtype: torch.dtype):
