@@ -55,10 +55,13 @@ extern "C" {
 #define POSEIDON_WIDTH_MAX (1u << 20)      /* values in a row */
 #define POSEIDON_PITCH_MAX (1u << 24)      /* values from row to row */
 #define POSEIDON_ROWS_MAX 0x7fffffffu      /* rows; for experts: tokens * k */
-#define POSEIDON_EXPERTS_MAX 511u          /* experts of poseidon_expert_sort */
+#define POSEIDON_EXPERTS_MAX 511u          /* experts of poseidon_expert_sort and poseidon_expert_product */
 #define POSEIDON_RANGES_MAX 65535u         /* row ranges of poseidon_weight_gradient */
 #define POSEIDON_TILES_MAX 0x400000u       /* 128 x 128 tiles of all its gradients together */
 #define POSEIDON_VOCAB_MAX 0x3ffffffu      /* rows of an embedding table */
+#define POSEIDON_NORM_WIDTH_MAX 16384u     /* values in a row of the norm */
+#define POSEIDON_HEAD_MAX 128u             /* values of an attention head, a multiple of 8 */
+#define POSEIDON_HEADS_MAX 1024u           /* heads of an attention */
 
 enum { POSEIDON_F32 = 0, POSEIDON_F16 = 1, POSEIDON_BF16 = 2 };   /* value types */
 
@@ -145,6 +148,38 @@ int poseidon_embed_backward(const int32_t *ids, uint64_t tokens, const void *dou
                             uint32_t dtable_type, uint32_t accumulate, void *workspace, uint64_t workspace_bytes,
                             void *hip_stream);
 uint64_t poseidon_embed_backward_workspace(uint64_t tokens, uint64_t vocab, uint64_t width);
+
+/* Rows times the weights of their range: out[t] = W[r] x[t] for the rows t of range r, or with `transposed` 1 W[r]^T x[t],
+ * the gradient of the rows.  weights: [n_ranges][out_width][in_width] of `type` without gaps; x has in_width values a row
+ * (transposed: out_width), out the other.  type: POSEIDON_F16 or POSEIDON_BF16; out_type: the same, or POSEIDON_F32.
+ * offsets: DEVICE int32[n_ranges + 1], non-decreasing, range r = rows [offsets[r], offsets[r + 1]), each cut to
+ * [0, rows]; rows before the first and after the last range get zeros.  Offsets that descend leave it open which rows are written.
+ * NULL with n_ranges == 1: all rows. */
+int poseidon_expert_product(const void *x, uint64_t pitch, uint32_t type, uint64_t rows, const void *weights,
+                            uint64_t out_width, uint64_t in_width, uint32_t transposed, const int32_t *offsets,
+                            uint32_t n_ranges, void *out, uint64_t out_pitch, uint32_t out_type, void *hip_stream);
+
+/* ---- norm ---- */
+
+/* h = x + residual (residual NULL: x), rstd[t] = 1 / sqrt(mean over the row of h^2 + eps),
+ * out[t] = h[t] * rstd[t] * weight; sum[t] = h[t].  sum and rstd may be NULL, and so may out where it is kept in 8 bits.
+ * With out_codes and out_scales (both or none) the rows of out are kept in 8 bits, with sum_codes and sum_scales those of
+ * h, as they are in `type`.  width <= POSEIDON_NORM_WIDTH_MAX; weight: `width` values of weight_type; eps >= 0. */
+int poseidon_norm_forward(const void *x, uint64_t x_pitch, const void *residual, uint64_t residual_pitch, uint32_t type,
+                          uint64_t rows, uint64_t width, const void *weight, uint32_t weight_type, float eps, void *out,
+                          uint64_t out_pitch, void *sum, uint64_t sum_pitch, float *rstd, int8_t *out_codes,
+                          uint8_t *out_scales, int8_t *sum_codes, uint8_t *sum_scales, void *hip_stream);
+
+/* Its gradient at h, from `sum` or from what was kept of it (codes and scales; one of the two): with n = h rstd,
+ * g = weight dout: dx = dsum + rstd (g - n mean over the row of n g), which is the gradient of x and of the residual
+ * alike, and dweight = sum over the rows of dout n, in a fixed order, added to what dweight holds where `accumulate` is
+ * 1.  dsum: the gradient that arrives at `sum`, or NULL.  dweight may be NULL; then it needs no workspace. */
+int poseidon_norm_backward(const void *dout, uint64_t dout_pitch, uint32_t type, uint64_t rows, uint64_t width,
+                           const void *sum, uint64_t sum_pitch, const int8_t *codes, const uint8_t *scales,
+                           const float *rstd, const void *weight, uint32_t weight_type, const void *dsum,
+                           uint64_t dsum_pitch, void *dx, uint64_t dx_pitch, float *dweight, uint32_t accumulate,
+                           void *workspace, uint64_t workspace_bytes, void *hip_stream);
+uint64_t poseidon_norm_backward_workspace(uint64_t rows, uint64_t width);
 
 #ifdef __cplusplus
 }

@@ -11,29 +11,11 @@
 // it in registers with byte permutes, and writes each column's eight rows as 16
 // bytes to LDS, where a column's 64 rows of a step lie together.  Every thread
 // brings a block of dy and one of the codes, which it also unpacks and scales.
-#include "layers_device.h"
+#include "layers_mfma.h"
 
 namespace pl {
 
-using Acc = float __attribute__((ext_vector_type(16)));
-using HalfVec = _Float16 __attribute__((ext_vector_type(8)));
-using BrainVec = __bf16 __attribute__((ext_vector_type(8)));
-using Words4 = uint32_t __attribute__((ext_vector_type(4)));
-
 constexpr uint32_t kStep = 64;    // rows of a step
-
-template <class T>
-__device__ __forceinline__ Acc mfma(Words4 a, Words4 b, Acc c);
-template <>
-__device__ __forceinline__ Acc mfma<BF16>(Words4 a, Words4 b, Acc c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(BrainVec, a), __builtin_bit_cast(BrainVec, b), c,
-                                                   0, 0, 0);
-}
-template <>
-__device__ __forceinline__ Acc mfma<F16>(Words4 a, Words4 b, Acc c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(HalfVec, a), __builtin_bit_cast(HalfVec, b), c, 0,
-                                                  0, 0);
-}
 
 // Two values as a pair.  BF16 holds every kept value exactly, and F16 those that were kept from it.  Of the others, this
 // conversion toward zero holds large ones to the type's last finite value in the same instruction, which rounding to nearest
@@ -255,12 +237,6 @@ __device__ __forceinline__ float signed_byte(uint32_t w) {
     else
         asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(v) : "v"(w));
     return v;
-}
-
-using Rsrc = __amdgpu_buffer_rsrc_t;
-
-__device__ __forceinline__ Rsrc buffer(const void *p, uint32_t bytes) {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, bytes, 0x00027000);
 }
 
 // Four waves on a tile of 32 C x 32 C, 16 C x 16 C a wave, in steps of 64 rows.

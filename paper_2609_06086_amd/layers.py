@@ -27,6 +27,7 @@ from .poseidon import PoseidonError
 GROUP = 64
 WIDTH_MAX, PITCH_MAX, ROWS_MAX = 1 << 20, 1 << 24, 2 ** 31 - 1
 EXPERTS_MAX, RANGES_MAX, VOCAB_MAX, TILES_MAX = 511, 65535, 2 ** 26 - 1, 1 << 22
+NORM_WIDTH_MAX, HEAD_MAX, HEADS_MAX = 16384, 128, 1024
 TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 _p, _u64, _u32 = C.c_void_p, C.c_uint64, C.c_uint32
@@ -45,6 +46,12 @@ _ARGS = {
     "poseidon_embed": [_p, _u64, _p, _u64, _u32, _u64, _u64, C.c_float, _p, _u64, _p],
     "poseidon_embed_backward": [_p, _u64, _p, _u64, _u32, _u64, _u64, C.c_float, _p, _u64, _u32, _u32, _p, _u64, _p],
     "poseidon_embed_backward_workspace": [_u64, _u64, _u64],
+    "poseidon_expert_product": [_p, _u64, _u32, _u64, _p, _u64, _u64, _u32, _p, _u32, _p, _u64, _u32, _p],
+    "poseidon_norm_forward": [_p, _u64, _p, _u64, _u32, _u64, _u64, _p, _u32, C.c_float, _p, _u64, _p, _u64, _p, _p, _p, _p,
+                              _p, _p],
+    "poseidon_norm_backward": [_p, _u64, _u32, _u64, _u64, _p, _u64, _p, _p, _p, _p, _u32, _p, _u64, _p, _u64, _p, _u32, _p,
+                               _u64, _p],
+    "poseidon_norm_backward_workspace": [_u64, _u64],
 }
 EXPORTS = tuple(_ARGS)
 
@@ -132,6 +139,17 @@ class ExpertPlan:
     def tensors(self):
         """The memory it holds."""
         return self.order, self.position, self.offsets
+
+
+@dataclass
+class Norm:
+    """What poseidon_norm_forward gives: the normalised rows, the sum that it normalised (None without a residual), 1 over the
+    root of each row's mean square (float32 [rows]), and the rows of both kept in 8 bits (None where not asked for)."""
+    out: torch.Tensor
+    sum: Optional[torch.Tensor]
+    rstd: torch.Tensor
+    kept_out: Optional[Stash]
+    kept_sum: Optional[Stash]
 
 
 def _refuse(where: str):
@@ -404,6 +422,35 @@ def poseidon_expert_combine_backward(dout, ys, plan: ExpertPlan, weights) -> Tup
     return dys, dweights
 
 
+@_streamed
+def poseidon_expert_product(x, weights, offsets=None, *, transposed: bool = False, dtype=None, out=None) -> torch.Tensor:
+    """Rows of x times the weights of their range: weights [ranges, out_width, in_width], int32 offsets [ranges + 1] (an
+    ExpertPlan's, for one); [rows, in_width] gives [rows, out_width], or with transposed the reverse, which is the gradient of the
+    rows.  Rows of no range get zeros.  Without offsets weights are [out_width, in_width], for all rows.  float16 or bfloat16; the
+    result is of the same type or float32."""
+    x, n, d, pitch = _rows(x, "poseidon_expert_product: x")
+    dev, dt = x.device, x.dtype
+    if not isinstance(weights, torch.Tensor) or weights.dim() != (2 if offsets is None else 3):
+        _refuse("poseidon_expert_product: weights: not [out_width, in_width], or with offsets one for each range")
+    weights = _whole(weights, "poseidon_expert_product: weights", dev, dt, None)
+    o, i = weights.shape[-2:]
+    ranges = 1
+    if offsets is not None:
+        offsets = _whole(offsets, "poseidon_expert_product: offsets", dev, torch.int32, None)
+        ranges = weights.shape[0]
+        if offsets.shape != (ranges + 1,):
+            _refuse("poseidon_expert_product: offsets: not int32 [ranges + 1]")
+    if d != (o if transposed else i):
+        _refuse("poseidon_expert_product: x: width differs from the weights'")
+    dtype = (dt if dtype is None else dtype) if out is None else getattr(out, "dtype", None)
+    if dtype not in (dt, torch.float32):
+        _refuse("poseidon_expert_product: a result of the rows' type or float32")
+    out, out_pitch = _out(out, "poseidon_expert_product: out", dev, dtype, n, i if transposed else o)
+    _call("poseidon_expert_product", dev, x.data_ptr(), pitch, TYPES[dt], n, weights.data_ptr(), o, i, int(transposed),
+          None if offsets is None else offsets.data_ptr(), ranges, out.data_ptr(), out_pitch, TYPES[dtype])
+    return out
+
+
 # ---- embedding ----
 
 def _ids(ids, where: str, device) -> torch.Tensor:
@@ -443,3 +490,72 @@ def poseidon_embed_backward(ids, dout, vocab: int, scale: float = 1.0, *, dtype=
     _call("poseidon_embed_backward", dev, ids.data_ptr(), n, dout.data_ptr(), pitch, TYPES[dout.dtype], vocab, d,
           scale, out.data_ptr(), out_pitch, TYPES[dtype], int(accumulate), at, size)
     return out
+
+
+# ---- norm ----
+
+def _weight(w, where: str, device, width: int) -> torch.Tensor:
+    if not isinstance(w, torch.Tensor) or w.dtype not in TYPES:
+        _refuse(f"{where}: not a float32, float16 or bfloat16 tensor")
+    return _whole(w, where, device, w.dtype, (width,))
+
+
+@_streamed
+def poseidon_norm_forward(x, weight, residual=None, *, eps: float = 1e-6, keep_out: bool = False, keep_sum: bool = False,
+                          out=None) -> Norm:
+    """The root-mean-square norm of h = x + residual (without one: of x): rows h / sqrt(mean h^2 + eps) * weight.
+    keep_out and keep_sum: those rows and h are kept in 8 bits too."""
+    x, n, d, pitch = _rows(x, "poseidon_norm_forward: x")
+    dev, dt = x.device, x.dtype
+    h, residual_pitch = None, 0
+    if residual is not None:
+        residual, _, _, residual_pitch = _rows(residual, "poseidon_norm_forward: residual", dev, dt, (n, d))
+        h = torch.empty((n, d), dtype=dt, device=dev)
+    weight = _weight(weight, "poseidon_norm_forward: weight", dev, d)
+    out, out_pitch = _out(out, "poseidon_norm_forward: out", dev, dt, n, d)
+    rstd = torch.empty(n, dtype=torch.float32, device=dev)
+    so = Stash.empty(n, d, dt, dev) if keep_out else None
+    sh = Stash.empty(n, d, dt, dev) if keep_sum else None
+    _call("poseidon_norm_forward", dev, x.data_ptr(), pitch, None if residual is None else residual.data_ptr(), residual_pitch,
+          TYPES[dt], n, d, weight.data_ptr(), TYPES[weight.dtype], eps, out.data_ptr(), out_pitch,
+          None if h is None else h.data_ptr(), d, rstd.data_ptr(), *(so.addresses() if keep_out else (None, None)),
+          *(sh.addresses() if keep_sum else (None, None)))
+    return Norm(out, h, rstd, so, sh)
+
+
+@_streamed
+def poseidon_norm_backward(dout, h, rstd, weight, dsum=None, *, dx=None, dweight=None, accumulate: bool = False,
+                           weight_gradient: bool = True) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """(gradient of x, which is the residual's too, float32 gradient of the weight) at h, the sum as it is or as it was
+    kept in 8 bits; dsum: the gradient that arrives at the sum.  With accumulate the weight's gradient is added to `dweight`;
+    without weight_gradient it is None."""
+    dout, n, d, pitch = _rows(dout, "poseidon_norm_backward: dout")
+    dev, dt = dout.device, dout.dtype
+    if isinstance(h, Stash):
+        h = _stash(h, "poseidon_norm_backward: h", dev, n, d)
+        at = (None, 0, *h.addresses())
+    else:
+        h, _, _, h_pitch = _rows(h, "poseidon_norm_backward: h", dev, dt, (n, d))
+        at = (h.data_ptr(), h_pitch, None, None)
+    rstd = _whole(rstd, "poseidon_norm_backward: rstd", dev, torch.float32, (n,))
+    weight = _weight(weight, "poseidon_norm_backward: weight", dev, d)
+    dsum_pitch = 0
+    if dsum is not None:
+        dsum, _, _, dsum_pitch = _rows(dsum, "poseidon_norm_backward: dsum", dev, dt, (n, d))
+    dx, dx_pitch = _out(dx, "poseidon_norm_backward: dx", dev, dt, n, d)
+    w, place, size = None, None, 0
+    if weight_gradient:
+        if accumulate and dweight is None:
+            _refuse("poseidon_norm_backward: accumulate without dweight")
+        if dweight is None:
+            dweight = torch.empty(d, dtype=torch.float32, device=dev)
+        elif not isinstance(dweight, torch.Tensor) or dweight.device != dev or dweight.dtype != torch.float32 or \
+                dweight.shape != (d,) or not dweight.is_contiguous():
+            _refuse("poseidon_norm_backward: dweight: not float32 [width] without gaps")
+        w, place, size = _workspace("poseidon_norm_backward", dev, n, d)
+    elif dweight is not None or accumulate:
+        _refuse("poseidon_norm_backward: dweight or accumulate without weight_gradient")
+    _call("poseidon_norm_backward", dev, dout.data_ptr(), pitch, TYPES[dt], n, d, *at, rstd.data_ptr(), weight.data_ptr(),
+          TYPES[weight.dtype], None if dsum is None else dsum.data_ptr(), dsum_pitch, dx.data_ptr(), dx_pitch,
+          None if dweight is None else dweight.data_ptr(), int(accumulate), place, size)
+    return dx, dweight
