@@ -181,6 +181,38 @@ int poseidon_norm_backward(const void *dout, uint64_t dout_pitch, uint32_t type,
                            void *workspace, uint64_t workspace_bytes, void *hip_stream);
 uint64_t poseidon_norm_backward_workspace(uint64_t rows, uint64_t width);
 
+/* ---- attention ---- */
+
+/* Causal attention of `heads` heads of `dim` values over packed sequences; query head h reads key and value head
+ * h / (heads / kv_heads).  For token i of a sequence, over its tokens j up to i:
+ *   s[j] = scale <q[i], k[j]>, lse[i] = log sum exp s[j], out[i] = sum of exp(s[j] - lse[i]) v[j].
+ * q, k, v, out: token t's head h begins at t * token pitch + h * head pitch; both are multiples of 8 and at least dim, the
+ * addresses on a 16-byte boundary.  type: POSEIDON_F16 or POSEIDON_BF16 (exp(s - ...) is rounded to it for the product with v).
+ * dim: a multiple of 8 up to POSEIDON_HEAD_MAX; kv_heads divides heads.  lse: float[heads][tokens].
+ * offsets: DEVICE int32[sequences + 1], non-decreasing, sequence r = tokens [offsets[r], offsets[r + 1]), each cut to
+ * [0, tokens]; tokens before the first and after the last sequence get zeros, their lse -infinity.  Offsets that descend leave
+ * it open which tokens are written.  NULL with sequences == 1: all tokens.
+ * An infinity or a NaN may reach every result of its own sequence, and none of another. */
+int poseidon_attention_forward(const void *q, uint64_t q_token, uint64_t q_head, const void *k, uint64_t k_token,
+                               uint64_t k_head, const void *v, uint64_t v_token, uint64_t v_head, uint32_t type,
+                               uint64_t tokens, uint32_t heads, uint32_t kv_heads, uint32_t dim, float scale,
+                               const int32_t *offsets, uint32_t sequences, void *out, uint64_t out_token,
+                               uint64_t out_head, float *lse, void *hip_stream);
+
+/* Its gradients from dout and what the forward pass gave: with p[i][j] = exp(s[i][j] - lse[i]) and
+ * ds[i][j] = p[i][j] (<dout[i], v[j]> - <dout[i], out[i]>): dq[i] = scale * sum over j of ds[i][j] k[j],
+ * dk[j] = scale * sum over i of ds[i][j] q[i], dv[j] = sum over i of p[i][j] dout[i], those two over the query heads that share
+ * the key, all in a fixed order.  p and ds are rounded to `type` for these products. */
+int poseidon_attention_backward(const void *dout, uint64_t dout_token, uint64_t dout_head, const void *q,
+                                uint64_t q_token, uint64_t q_head, const void *k, uint64_t k_token, uint64_t k_head,
+                                const void *v, uint64_t v_token, uint64_t v_head, const void *out, uint64_t out_token,
+                                uint64_t out_head, const float *lse, uint32_t type, uint64_t tokens, uint32_t heads,
+                                uint32_t kv_heads, uint32_t dim, float scale, const int32_t *offsets,
+                                uint32_t sequences, void *dq, uint64_t dq_token, uint64_t dq_head, void *dk,
+                                uint64_t dk_token, uint64_t dk_head, void *dv, uint64_t dv_token, uint64_t dv_head,
+                                void *workspace, uint64_t workspace_bytes, void *hip_stream);
+uint64_t poseidon_attention_backward_workspace(uint64_t tokens, uint32_t heads);
+
 #ifdef __cplusplus
 }
 #endif

@@ -52,6 +52,10 @@ _ARGS = {
     "poseidon_norm_backward": [_p, _u64, _u32, _u64, _u64, _p, _u64, _p, _p, _p, _p, _u32, _p, _u64, _p, _u64, _p, _u32, _p,
                                _u64, _p],
     "poseidon_norm_backward_workspace": [_u64, _u64],
+    "poseidon_attention_forward": [_p, _u64, _u64] * 3 + [_u32, _u64, _u32, _u32, _u32, C.c_float, _p, _u32, _p, _u64, _u64, _p, _p],
+    "poseidon_attention_backward": [_p, _u64, _u64] * 5 + [_p, _u32, _u64, _u32, _u32, _u32, C.c_float, _p, _u32] +
+                                   [_p, _u64, _u64] * 3 + [_p, _u64, _p],
+    "poseidon_attention_backward_workspace": [_u64, _u32],
 }
 EXPORTS = tuple(_ARGS)
 
@@ -559,3 +563,104 @@ def poseidon_norm_backward(dout, h, rstd, weight, dsum=None, *, dx=None, dweight
           TYPES[weight.dtype], None if dsum is None else dsum.data_ptr(), dsum_pitch, dx.data_ptr(), dx_pitch,
           None if dweight is None else dweight.data_ptr(), int(accumulate), place, size)
     return dx, dweight
+
+
+# ---- attention ----
+
+def _heads(x, where: str, device=None, dtype=None, shape=None):
+    """Rows [tokens, heads, dim] with neighbouring values in a head (copied if the library can't take them as they are):
+    (x, token pitch, head pitch)."""
+    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dim() != 3 or x.dtype not in (torch.float16, torch.bfloat16):
+        _refuse(f"{where}: not a 3-D float16 or bfloat16 tensor on the GPU")
+    if (device is not None and x.device != device) or (dtype is not None and x.dtype != dtype) or \
+            (shape is not None and x.shape != shape):
+        _refuse(f"{where}: device, type or shape differs from what the others ask for")
+    pitches = _pitches(x)
+    if pitches is None:
+        x = x.contiguous()
+        pitches = _pitches(x)
+        if pitches is None:    # at an odd address: a copy is on an even one
+            x = x.clone()
+            pitches = _pitches(x)
+            if pitches is None:
+                _refuse(f"{where}: heads that are no multiple of 8 wide")
+    return (x, *pitches)
+
+
+def _pitches(x):
+    """(token pitch, head pitch) of rows that the library takes as they are, or None."""
+    (n, h, d), (token, head, step) = x.shape, x.stride()
+    token, head = (h * d if n <= 1 else token), (d if h <= 1 else head)
+    if (step == 1 or d <= 1) and token >= d and head >= d and not (token % 8 or head % 8 or x.data_ptr() % 16) and \
+            token <= PITCH_MAX:
+        return token, head
+    return None
+
+
+def _heads_out(x, where: str, device, dtype, shape):
+    """Rows that the caller brought for a result, or new ones: (x, token pitch, head pitch)."""
+    if x is None:
+        x = torch.empty(shape, dtype=dtype, device=device)
+    elif not isinstance(x, torch.Tensor) or x.device != device or x.dtype != dtype or x.shape != shape:
+        _refuse(f"{where}: device, type or shape differs from the result's")
+    pitches = _pitches(x)
+    if pitches is None:
+        _refuse(f"{where}: layout: heads of neighbouring values on pitches that are multiples of 8, on a 16-byte boundary")
+    return (x, *pitches)
+
+
+def _attended(name: str, q, k, v, offsets, scale):
+    """The operands of an attention, looked over: ((q, pitches), (k, ...), (v, ...), offsets, sequences, scale)."""
+    q = _heads(q, f"{name}: q")
+    dev, dt, (n, h, d) = q[0].device, q[0].dtype, q[0].shape
+    kv_heads = k.shape[1] if isinstance(k, torch.Tensor) and k.dim() == 3 else 0
+    if not kv_heads or not d or h % kv_heads:
+        _refuse(f"{name}: k: heads that do not divide the queries'")
+    if d > HEAD_MAX or h > HEADS_MAX:
+        raise PoseidonError(P.POSEIDON_E_RANGE, name)
+    k, v = (_heads(x, f"{name}: {w}", dev, dt, (n, kv_heads, d)) for x, w in ((k, "k"), (v, "v")))
+    sequences = 1
+    if offsets is not None:
+        offsets = _whole(offsets, f"{name}: offsets", dev, torch.int32, None)
+        if offsets.dim() != 1 or offsets.numel() < 2:
+            _refuse(f"{name}: offsets: not int32 [sequences + 1]")
+        sequences = offsets.numel() - 1
+    return q, k, v, offsets, sequences, d ** -0.5 if scale is None else scale
+
+
+def _places(*heads):
+    """(address, token pitch, head pitch) of each, in a row."""
+    return [y for x, token, head in heads for y in (x.data_ptr(), token, head)]
+
+
+@_streamed
+def poseidon_attention_forward(q, k, v, offsets=None, *, scale=None, out=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(out [tokens, heads, dim], log of the sum of the exponentials, float32 [heads, tokens]) of causal attention: q [tokens,
+    heads, dim], k and v [tokens, key heads, dim], each key head shared by heads / key heads neighbouring query heads;
+    int32 offsets [sequences + 1] of packed sequences, without them one sequence.  scale: dim ** -0.5 if not given.
+    Views of one product's rows are taken as they are."""
+    q, k, v, offsets, sequences, scale = _attended("poseidon_attention_forward", q, k, v, offsets, scale)
+    dev, dt, (n, h, d) = q[0].device, q[0].dtype, q[0].shape
+    out = _heads_out(out, "poseidon_attention_forward: out", dev, dt, (n, h, d))
+    lse = torch.empty((h, n), dtype=torch.float32, device=dev)
+    _call("poseidon_attention_forward", dev, *_places(q, k, v), TYPES[dt], n, h, k[0].shape[1], d, scale,
+          None if offsets is None else offsets.data_ptr(), sequences, *_places(out), lse.data_ptr())
+    return out[0], lse
+
+
+@_streamed
+def poseidon_attention_backward(dout, q, k, v, out, lse, offsets=None, *, scale=None, dq=None, dk=None,
+                                dv=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """(dq, dk, dv) of poseidon_attention_forward, from its arguments and its results."""
+    name = "poseidon_attention_backward"
+    q, k, v, offsets, sequences, scale = _attended(name, q, k, v, offsets, scale)
+    dev, dt, shape, kv_shape = q[0].device, q[0].dtype, q[0].shape, k[0].shape
+    n, h, d = shape
+    dout, out = (_heads(x, f"{name}: {w}", dev, dt, shape) for x, w in ((dout, "dout"), (out, "out")))
+    lse = _whole(lse, f"{name}: lse", dev, torch.float32, (h, n))
+    dq = _heads_out(dq, f"{name}: dq", dev, dt, shape)
+    dk, dv = (_heads_out(x, f"{name}: {w}", dev, dt, kv_shape) for x, w in ((dk, "dk"), (dv, "dv")))
+    w, at, size = _workspace(name, dev, n, h)
+    _call(name, dev, *_places(dout, q, k, v, out), lse.data_ptr(), TYPES[dt], n, h, kv_shape[1], d, scale,
+          None if offsets is None else offsets.data_ptr(), sequences, *_places(dq, dk, dv), at, size)
+    return dq[0], dk[0], dv[0]
