@@ -211,7 +211,9 @@ int poseidon_attention_backward(const void *dout, uint64_t dout_token, uint64_t 
                                 uint32_t sequences, void *dq, uint64_t dq_token, uint64_t dq_head, void *dk,
                                 uint64_t dk_token, uint64_t dk_head, void *dv, uint64_t dv_token, uint64_t dv_head,
                                 void *workspace, uint64_t workspace_bytes, void *hip_stream);
-uint64_t poseidon_attention_backward_workspace(uint64_t tokens, uint32_t heads);
+/* Bytes it needs: 8 for each token and head, and up to 1 GB for 32-bit sums of parts of the heads that share a key. */
+uint64_t poseidon_attention_backward_workspace(uint64_t tokens, uint32_t heads, uint32_t kv_heads, uint32_t dim,
+                                               uint32_t sequences);
 
 #ifdef __cplusplus
 }

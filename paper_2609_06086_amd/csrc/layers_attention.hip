@@ -13,8 +13,9 @@
 namespace pl {
 
 constexpr uint32_t kTile = 64;               // keys (backward for dk and dv: queries) in LDS at a time
+constexpr int kWaves = 4;                    // of a block
 constexpr uint32_t kClearBlocks = 64;        // blocks that look for rows outside of all sequences
-constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
+constexpr float kLog2e = 1.44269504f;
 
 // Rows [tokens][heads][dim] of a 16-bit type: where a token's and a head's values begin.
 struct Heads {
@@ -24,9 +25,10 @@ struct Heads {
 
 struct Attention {
     Heads q, k, v, dout, out, dq, dk, dv;    // written: out forward, dq, dk, dv backward
-    float *lse, *delta;                      // [heads][tokens]
+    float *lse, *delta, *base;               // [heads][tokens]; base: -lse / ln 2
     const int32_t *offsets;                  // null: one sequence of all tokens
-    uint32_t tokens, sequences, heads, kv_heads, dim, tiles;
+    float *parts;                            // [split][dk, dv][tokens][kv heads][dim] sums, where split > 1
+    uint32_t tokens, sequences, heads, kv_heads, dim, tiles, split;
     float scale;
 };
 
@@ -35,55 +37,96 @@ __device__ __forceinline__ const typename T::raw *row_of(const Heads &x, uint64_
     return (const typename T::raw *)x.at + token * x.token + head * x.head;
 }
 
-// Rows of D values lie in LDS in pieces of 16 bytes; piece p of row r at p ^ mixed(r).  Eight rows' pieces p and four rows'
-// pieces [p, p + 4) are so in banks of their own.
+// Rows of D values lie in LDS in pieces of 16 bytes; piece p of row r at p ^ mixed(r).  The pieces p of sixteen rows, which
+// LDS reads at a time, and the pieces [4 p, 4 p + 4) of four rows, which a turned read takes, are so in banks of their own.
 template <int D>
 __device__ __forceinline__ uint32_t mixed(uint32_t r) {
+    const uint32_t high = (r >> 2 & 1) | (r >> 2 & 2);
     if constexpr (D == 128)
-        return (r >> 2 & 1) | (r & 2) | (r & 1) << 2 | (r & 2) << 2;
+        return (r & 3) << 2 | high;
     else
-        return (r >> 2 & 1) | (r & 1) << 1 | (r & 2) << 1;
+        return (r & 2) << 1 | high;    // two rows to all banks
 }
 
-// A tile of rows on its way to LDS, by `threads` threads; rows from `rows` on and values from `dim` on come as zeros.
+// A tile of rows on its way to LDS, by THREADS threads, some rows in each of a few copies; rows from `rows` on and values from
+// `dim` on come as zeros.  A copy's rows are a multiple of 16, so a lane's piece lies at the same place in all of them.
 template <int D, uint32_t THREADS>
 struct Loader {
-    static constexpr uint32_t kPieces = kTile * D / 8 / THREADS;
-    uint32_t row[kPieces], piece[kPieces];
-    __device__ __forceinline__ void aim(uint32_t dim) {
-#pragma unroll
-        for (uint32_t i = 0; i < kPieces; ++i) {
-            const uint32_t p = i * THREADS + threadIdx.x;
-            row[i] = p / (D / 8);
-            const uint32_t c = (p % (D / 8)) ^ mixed<D>(row[i]);
-            piece[i] = c * 8 < dim ? c * 16 : kNowhere;
-        }
+    static constexpr uint32_t kRows = THREADS / (D / 8);
+    static_assert(kRows % 16 == 0 && kTile % kRows == 0);
+    uint32_t row, piece;
+    __device__ __forceinline__ explicit Loader(uint32_t dim) {
+        row = threadIdx.x / (D / 8);
+        const uint32_t c = (threadIdx.x % (D / 8)) ^ mixed<D>(row);
+        piece = c * 8 < dim ? c * 16 : kNowhere;
     }
+    __device__ __forceinline__ uint32_t place(uint64_t pitch) const { return row * ((uint32_t)pitch * 2) + piece; }
     template <class T>
-    __device__ __forceinline__ void load(const typename T::raw *from, uint64_t pitch, uint32_t rows, uint16_t *to) const {
-        const uint64_t bytes = rows * pitch * 2;
-        const Rsrc r = buffer(from, (uint32_t)min(bytes, (uint64_t)kBufferBytes));
+    __device__ __forceinline__ void load(const typename T::raw *from, uint64_t pitch, uint32_t place, uint32_t rows, uint16_t *to) const {
 #pragma unroll
-        for (uint32_t i = 0; i < kPieces; ++i)
-            copy_to_lds(r, row[i] * ((uint32_t)pitch * 2) + piece[i], to + (i * THREADS + threadIdx.x / 64 * 64) * 8);
+        for (uint32_t i = 0; i < kTile / kRows; ++i) {
+            const uint32_t left = rows > i * kRows ? min(rows - i * kRows, kRows) : 0;
+            copy_to_lds(buffer(from + i * kRows * pitch, __builtin_amdgcn_readfirstlane(left * ((uint32_t)pitch * 2))), place,
+                        to + (i * THREADS + __builtin_amdgcn_readfirstlane(threadIdx.x & ~63u)) * 8);
+        }
     }
 };
 
-// Operands from LDS: 16 values from 16 s on of rows 32 t + lane % 32, and the turned rows (lane: value 32 d + lane % 32) that
-// go with the scores of rows [16 s, 16 s + 16) in a lane's registers: 4 half + {0..3}, then 8 + 4 half + {0..3}.
+// Operands from a tile in LDS that begins OFFSET values into it: 16 values from 16 s on of rows 32 t + lane % 32, and the
+// turned rows (lane: value 32 d + lane % 32) that go with the scores of rows [16 s, 16 s + 16) in a lane's registers:
+// 4 half + {0..3}, then 8 + 4 half + {0..3}.  A lane's places are found once; tiles and rows are offsets in the instructions.
 template <int D>
-__device__ __forceinline__ Words4 rows_at(const uint16_t *lds, int t, int s, uint32_t lane) {
-    const uint32_t r = lane % 32;
-    return *(const Words4 *)(lds + (32 * t + r) * D + ((2 * s + lane / 32) ^ mixed<D>(r)) * 8);
-}
+struct Reader {
+    using Bytes = __attribute__((address_space(3))) const char *;
+    uint32_t rows[D / 16], lo[D / 32], hi[D / 32];
+    __device__ __forceinline__ Reader(const uint16_t *lds, uint32_t lane) {
+        const uint32_t base = (uint32_t)(uintptr_t)(Bytes)(const char *)lds;
+        const uint32_t r = lane % 32, u = 4 * (lane / 32) + lane % 16 / 4, c = 2 * (lane / 16 % 2) + lane % 4 / 2;
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) rows[s] = base + r * (2 * D) + ((2 * s + lane / 32) ^ mixed<D>(r)) * 16;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) {
+            lo[d] = base + u * (2 * D) + ((4 * d + c) ^ mixed<D>(u)) * 16 + lane % 2 * 8;
+            hi[d] = base + (u + 8) * (2 * D) + ((4 * d + c) ^ mixed<D>(u + 8)) * 16 + lane % 2 * 8;
+        }
+    }
+    template <uint32_t OFFSET>
+    __device__ __forceinline__ Words4 row(int t, int s) const {
+        return *(__attribute__((address_space(3))) const Words4 *)((Bytes)(uintptr_t)rows[s] + 2 * OFFSET + 64 * D * t);
+    }
+    template <uint32_t OFFSET>
+    __device__ __forceinline__ Words4 turn(int s, int d) const {
+        const uint2 a = read_turned((Bytes)(uintptr_t)lo[d] + 2 * OFFSET + 32 * D * s);
+        const uint2 b = read_turned((Bytes)(uintptr_t)hi[d] + 2 * OFFSET + 32 * D * s);
+        return Words4{a.x, a.y, b.x, b.y};
+    }
+};
+
+// The same with three places, from which the others are an exclusive or away: for a kernel that needs its registers.
 template <int D>
-__device__ __forceinline__ Words4 turned_at(const uint16_t *lds, int s, int d, uint32_t lane) {
-    const uint32_t r = 4 * (lane / 32) + lane % 16 / 4;
-    const uint32_t piece = (4 * d + 2 * (lane / 16 % 2) + lane % 4 / 2) ^ mixed<D>(r);
-    const uint16_t *from = lds + (16 * s + r) * D + piece * 8 + lane % 2 * 4;
-    const uint2 lo = read_turned(from), hi = read_turned(from + 8 * D);
-    return Words4{lo.x, lo.y, hi.x, hi.y};
-}
+struct SmallReader {
+    using Bytes = __attribute__((address_space(3))) const char *;
+    uint32_t rows, lo, hi;
+    __device__ __forceinline__ SmallReader(const uint16_t *lds, uint32_t lane) {
+        const Reader<D> all(lds, lane);
+        rows = all.rows[0];
+        lo = all.lo[0];
+        hi = all.hi[0];
+    }
+    template <uint32_t OFFSET>
+    __device__ __forceinline__ Words4 row(int t, int s) const {
+        return *(__attribute__((address_space(3))) const Words4 *)((Bytes)(uintptr_t)(rows ^ 32 * s) + 2 * OFFSET + 64 * D * t);
+    }
+    template <uint32_t OFFSET>
+    __device__ __forceinline__ Words4 turn(int s, int d) const {
+        const uint2 a = read_turned((Bytes)(uintptr_t)(lo ^ 64 * d) + 2 * OFFSET + 32 * D * s);
+        const uint2 b = read_turned((Bytes)(uintptr_t)(hi ^ 64 * d) + 2 * OFFSET + 32 * D * s);
+        return Words4{a.x, a.y, b.x, b.y};
+    }
+};
+
+template <uint32_t N>
+using At = std::integral_constant<uint32_t, N>;
 
 // Eight values [16 s + 8 (lane / 32), ...) of a row in memory, zeros from `dim` on.
 template <class T>
@@ -109,8 +152,8 @@ __device__ __forceinline__ float sum_half(float v) {
 }
 
 // Sums whose column is the lane's row, times f, to that row in memory.
-template <class T, int D>
-__device__ __forceinline__ void store_turned(const Acc (&sum)[D / 32], float f, typename T::raw *row, uint32_t dim, uint32_t lane) {
+template <class O, int D>
+__device__ __forceinline__ void store_turned(const Acc (&sum)[D / 32], float f, typename O::raw *row, uint32_t dim, uint32_t lane) {
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
@@ -124,7 +167,7 @@ __device__ __forceinline__ void store_turned(const Acc (&sum)[D / 32], float f, 
                 v[4 + i] = __uint_as_float(r[1]);
             }
             const uint32_t c = 32 * d + 16 * h + 8 * (lane / 32);
-            if (row && c < dim) store_slice<T>(row, c, dim, v);
+            if (row && c < dim) store_slice<O>(row, c, dim, v);
         }
 }
 
@@ -191,31 +234,39 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_forward_kernel(Attent
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) query[s] = piece_of<T>(row, s, lane, a.dim);
     }
-    Loader<D, 64 * WAVES> loader;
-    loader.aim(a.dim);
+    const Loader<D, 64 * WAVES> loader(a.dim);
+    const Reader<D> reader(lds, lane);
+    const uint32_t k_place = loader.place(a.k.token), v_place = loader.place(a.v.token);
     const auto fetch = [&](uint32_t i) {
         const uint32_t t = begin + i * kTile, rows = at.end - t;
         uint16_t *to = lds + (i & 1) * kStage;
-        loader.template load<T>(row_of<T>(a.k, t, w.kv), a.k.token, rows, to);
-        loader.template load<T>(row_of<T>(a.v, t, w.kv), a.v.token, rows, to + kTile * D);
+        loader.template load<T>(row_of<T>(a.k, t, w.kv), a.k.token, k_place, rows, to);
+        loader.template load<T>(row_of<T>(a.v, t, w.kv), a.v.token, v_place, rows, to + kTile * D);
     };
 
     const float c = a.scale * kLog2e;
     float m = -__builtin_inff(), total = 0.0f;
     Acc sum[D / 32] = {};
     fetch(0);
-    for (uint32_t i = 0; i < tiles; ++i) {
+    const auto step = [&](auto stage, uint32_t i) {
+        constexpr uint32_t kKeys = decltype(stage)::value, kValues = kKeys + kTile * D;
         __builtin_amdgcn_s_waitcnt(0x0f70);    // vmcnt(0): this wave's part of the tile is in LDS
         __syncthreads();
         if (i + 1 < tiles) fetch(i + 1);
         const uint32_t t0 = begin + i * kTile;
-        if (t0 > q0 + 31) continue;            // all of it after the wave's queries
-        const uint16_t *keys = lds + (i & 1) * kStage, *vals = keys + kTile * D;
+        if (t0 > q0 + 31) return;            // all of it after the wave's queries
         Acc s[2] = {};
 #pragma unroll
         for (int j = 0; j < D / 16; ++j)
 #pragma unroll
-            for (int t = 0; t < 2; ++t) s[t] = mfma<T>(rows_at<D>(keys, t, j, lane), query[j], s[t]);
+            for (int t = 0; t < 2; ++t) s[t] = mfma<T>(reader.template row<kKeys>(t, j), query[j], s[t]);
+        then<kReadLds, 6>();
+#pragma unroll
+        for (int j = 0; j < D / 8 - 6; ++j) {
+            then<kMatrix, 1>();
+            then<kReadLds, 1>();
+        }
+        then<kMatrix, 6>();
         float p[2][16];
         float most = -__builtin_inff();
 #pragma unroll
@@ -223,11 +274,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_forward_kernel(Attent
 #pragma unroll
             for (int r = 0; r < 16; ++r) p[t][r] = s[t][r];
         if (t0 + kTile - 1 > q0) {
+            const int last_key = (int)(q - t0) - (int)(4 * (lane / 32));
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    if (t0 + 32 * t + (r & 3) + 8 * (r >> 2) + 4 * (lane / 32) > q) p[t][r] = -__builtin_inff();
+                    if (32 * t + (r & 3) + 8 * (r >> 2) > last_key) p[t][r] = -__builtin_inff();
         }
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -253,8 +305,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_forward_kernel(Attent
         for (int j = 0; j < 4; ++j) {
             const Words4 w = packed<T>(p[j / 2], j % 2);
 #pragma unroll
-            for (int d = 0; d < D / 32; ++d) sum[d] = mfma<T>(turned_at<D>(vals, j, d, lane), w, sum[d]);
+            for (int d = 0; d < D / 32; ++d) sum[d] = mfma<T>(reader.template turn<kValues>(j, d), w, sum[d]);
         }
+    };
+    for (uint32_t i = 0; i < tiles; i += 2) {
+        step(At<0>{}, i);
+        if (i + 1 < tiles) step(At<kStage>{}, i + 1);
     }
     total = sum_half(total);
     const bool there = q < at.end;
@@ -300,25 +356,29 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_queries_kernel(Attent
             for (int i = 0; i < 8; ++i) delta = fmaf(T::up(x[i]), T::up(y[i]), delta);
         }
         delta = sum_half(delta);
-        if (there && lane < 32) a.delta[(uint64_t)w.head * a.tokens + q] = delta;
     }
-    Loader<D, 64 * WAVES> loader;
-    loader.aim(a.dim);
+    const Loader<D, 64 * WAVES> loader(a.dim);
+    const Reader<D> reader(lds, lane);
+    const uint32_t k_place = loader.place(a.k.token), v_place = loader.place(a.v.token);
     const auto fetch = [&](uint32_t i) {
         const uint32_t t = begin + i * kTile, rows = at.end - t;
         uint16_t *to = lds + (i & 1) * kStage;
-        loader.template load<T>(row_of<T>(a.k, t, w.kv), a.k.token, rows, to);
-        loader.template load<T>(row_of<T>(a.v, t, w.kv), a.v.token, rows, to + kTile * D);
+        loader.template load<T>(row_of<T>(a.k, t, w.kv), a.k.token, k_place, rows, to);
+        loader.template load<T>(row_of<T>(a.v, t, w.kv), a.v.token, v_place, rows, to + kTile * D);
     };
 
     const float c = a.scale * kLog2e, lse = a.lse[(uint64_t)w.head * a.tokens + mine] * kLog2e;
+    if (there && lane < 32) {
+        a.delta[(uint64_t)w.head * a.tokens + q] = delta;
+        a.base[(uint64_t)w.head * a.tokens + q] = -lse;
+    }
     Acc sum[D / 32] = {};
     fetch(0);
-    for (uint32_t i = 0; i < tiles; ++i) {
+    const auto step = [&](auto stage, uint32_t i) {
+        constexpr uint32_t kKeys = decltype(stage)::value, kValues = kKeys + kTile * D;
         __builtin_amdgcn_s_waitcnt(0x0f70);
         __syncthreads();
         if (i + 1 < tiles) fetch(i + 1);
-        const uint16_t *keys = lds + (i & 1) * kStage, *vals = keys + kTile * D;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const uint32_t t0 = begin + i * kTile + 32 * t;
@@ -326,36 +386,52 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_queries_kernel(Attent
             Acc s = {}, dp = {};
 #pragma unroll
             for (int j = 0; j < D / 16; ++j) {
-                s = mfma<T>(rows_at<D>(keys, t, j, lane), query[j], s);
-                dp = mfma<T>(rows_at<D>(vals, t, j, lane), dout[j], dp);
+                s = mfma<T>(reader.template row<kKeys>(t, j), query[j], s);
+                dp = mfma<T>(reader.template row<kValues>(t, j), dout[j], dp);
             }
+            then<kReadLds, 6>();
+#pragma unroll
+            for (int j = 0; j < D / 8 - 6; ++j) {
+                then<kMatrix, 1>();
+                then<kReadLds, 1>();
+            }
+            then<kMatrix, 6>();
             float ds[16];
 #pragma unroll
             for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -lse)) * (dp[r] - delta);
             if (t0 + 31 > q0) {
+                const int last_key = (int)(q - t0) - (int)(4 * (lane / 32));
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    if (t0 + (r & 3) + 8 * (r >> 2) + 4 * (lane / 32) > q) ds[r] = 0.0f;
+                    if ((r & 3) + 8 * (r >> 2) > last_key) ds[r] = 0.0f;
             }
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const Words4 w = packed<T>(ds, j);
 #pragma unroll
-                for (int d = 0; d < D / 32; ++d) sum[d] = mfma<T>(turned_at<D>(keys, 2 * t + j, d, lane), w, sum[d]);
+                for (int d = 0; d < D / 32; ++d) sum[d] = mfma<T>(reader.template turn<kKeys>(2 * t + j, d), w, sum[d]);
             }
         }
+    };
+    for (uint32_t i = 0; i < tiles; i += 2) {
+        step(At<0>{}, i);
+        if (i + 1 < tiles) step(At<kStage>{}, i + 1);
     }
     store_turned<T, D>(sum, a.scale, there ? (raw *)row_of<T>(a.dq, q, w.head) : nullptr, a.dim, lane);
 }
 
-// dk and dv: WAVES waves of 32 keys each go through the queries of every head that shares them, in one order.
+// dk and dv: WAVES waves of 32 keys each go through the queries of every head that shares them, in one order.  With 128
+// values a head the keys, the values and both sums would leave no registers for what is read ahead, so some of the
+// values lie in LDS.
 template <class T, int D, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void attention_keys_kernel(Attention a) {
     constexpr uint32_t kKeys = 32 * WAVES, kStage = 2 * kTile * D;
     __shared__ __attribute__((aligned(16))) uint16_t lds[2 * kStage];
-    __shared__ __attribute__((aligned(16))) float rows[2][2][kTile];    // lse and delta
+    __shared__ __attribute__((aligned(16))) float rows[2][2][kTile];    // base and delta
+    constexpr int kHeld = D == 128 ? 5 : D / 16, kSpare = D / 16 - kHeld;
+    __shared__ Words4 spare[kSpare ? WAVES * kSpare * 64 : 1];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const uint32_t blocks = a.tiles * a.kv_heads;
+    const uint32_t blocks = a.tiles * a.split * a.kv_heads;
     if (blockIdx.x >= blocks) {
         outside(a, blockIdx.x - blocks, gridDim.x - blocks, [&](uint64_t t) {
             clear_token<T>(a.dk, t, a.kv_heads, a.dim);
@@ -363,93 +439,173 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_keys_kernel(Attention
         });
         return;
     }
-    const uint32_t kv = blockIdx.x % a.kv_heads, group = a.heads / a.kv_heads;
+    const uint32_t kv = blockIdx.x % a.kv_heads, group = a.heads / a.kv_heads / a.split;
+    const uint32_t tile = blockIdx.x / a.kv_heads / a.split, part = blockIdx.x / a.kv_heads % a.split;
+    const uint32_t head0 = (kv * a.split + part) * group;    // the first of the block's query heads
     uint32_t begin;    // keys early in a sequence have the most queries: these first
-    const Place at = sequence_of(a, blockIdx.x / a.kv_heads, kKeys, begin);
+    const Place at = sequence_of(a, tile, kKeys, begin);
     if (!at.there) return;
     const uint32_t k0 = at.begin + 32 * wave, key = k0 + lane % 32;
     const bool there = key < at.end;
     const uint32_t tiles = (at.end - at.begin + kTile - 1) / kTile;    // of queries, from the block's first key on
 
     using raw = typename T::raw;
-    Words4 keys[D / 16], vals[D / 16];
+    Words4 keys[D / 16], vals[kHeld];
+    Words4 *const rest = spare + wave * (kSpare * 64) + lane;
     {
         const uint32_t mine = min(key, at.end - 1);
         const raw *kr = row_of<T>(a.k, mine, kv), *vr = row_of<T>(a.v, mine, kv);
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) {
             keys[s] = piece_of<T>(kr, s, lane, a.dim);
-            vals[s] = piece_of<T>(vr, s, lane, a.dim);
+            const Words4 v = piece_of<T>(vr, s, lane, a.dim);
+            if (s < kHeld)
+                vals[s] = v;
+            else
+                rest[(s - kHeld) * 64] = v;
         }
     }
-    Loader<D, 64 * WAVES> loader;
-    loader.aim(a.dim);
-    const auto fetch = [&](uint32_t set, uint32_t head, uint32_t i) {
-        const uint32_t t = at.begin + i * kTile, n = at.end - t;
+    const Loader<D, 64 * WAVES> loader(a.dim);
+    const SmallReader<D> all(lds, lane);
+    const uint32_t q_place = loader.place(a.q.token), dout_place = loader.place(a.dout.token);
+    // From the last queries down, all heads at each: blocks that run together then ask for the same rows.
+    uint32_t asked = tiles - 1, g = 0;
+    bool more = true;
+    const auto fetch = [&](uint32_t set) {    // the next tile
+        if (!more) return;
+        const uint32_t t = at.begin + asked * kTile, n = at.end - t, head = head0 + g;
         uint16_t *to = lds + set * kStage;
-        loader.template load<T>(row_of<T>(a.q, t, head), a.q.token, n, to);
-        loader.template load<T>(row_of<T>(a.dout, t, head), a.dout.token, n, to + kTile * D);
+        loader.template load<T>(row_of<T>(a.q, t, head), a.q.token, q_place, n, to);
+        loader.template load<T>(row_of<T>(a.dout, t, head), a.dout.token, dout_place, n, to + kTile * D);
         if (wave < 2) {    // rows past the end: zeros, as q and dout have there
-            const float *from = (wave ? a.delta : a.lse) + (uint64_t)head * a.tokens + t;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer(from, min(n, kTile) * 4),
+            const float *from = (wave ? a.delta : a.base) + (uint64_t)head * a.tokens + t;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer(from, __builtin_amdgcn_readfirstlane(min(n, kTile) * 4)),
                                                      (__attribute__((address_space(3))) void *)rows[set][wave], 4, lane * 4, 0, 0, 0);
+        }
+        if (++g == group) {
+            g = 0;
+            more = asked-- != 0;
         }
     };
 
     const float c = a.scale * kLog2e;
     Acc dk[D / 32] = {}, dv[D / 32] = {};
-    uint32_t set = 0;
-    fetch(0, kv * group, 0);
-    for (uint32_t g = 0; g < group; ++g)
-        for (uint32_t i = 0; i < tiles; ++i, set ^= 1) {
-            __builtin_amdgcn_s_waitcnt(0x0f70);
-            __syncthreads();
-            if (i + 1 < tiles)
-                fetch(set ^ 1, kv * group + g, i + 1);
-            else if (g + 1 < group)
-                fetch(set ^ 1, kv * group + g + 1, 0);
-            const uint16_t *queries = lds + set * kStage, *douts = queries + kTile * D;
+    const auto use = [&](auto stage, int t, uint32_t t0) {    // 32 queries
+        constexpr uint32_t kSet = decltype(stage)::value, kQueries = kSet * kStage, kDout = kQueries + kTile * D;
+        if (t0 + 31 < k0) return;    // all of them before the wave's keys
+        SmallReader<D> reader = all;
+        uint32_t half = lane / 32;
+        asm("" : "+v"(reader.rows), "+v"(reader.lo), "+v"(reader.hi), "+v"(half));    // places are found where they are used, not kept
+        // What LDS gives is asked for two products of a kind before its use, and no earlier: there are no registers for more.
+        Words4 x[2], y[2], z[2];
+        const auto ask_x = [&](int j) { x[j & 1] = reader.template row<kQueries>(t, j); };
+        const auto ask_y = [&](int j) {
+            y[j & 1] = reader.template row<kDout>(t, j);
+            if (j >= kHeld) z[j & 1] = rest[(j - kHeld) * 64];
+        };
+        Acc s = {}, dp = {};
+        ask_x(0);
+        ask_y(0);
+        ask_x(1);
+        ask_y(1);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const uint32_t t0 = at.begin + i * kTile + 32 * t;
-                if (t0 + 31 < k0) continue;    // all of them before the wave's keys
-                Acc s = {}, dp = {};
+        for (int j = 0; j < D / 16; ++j) {
+            s = mfma<T>(x[j & 1], keys[j], s);
+            if (j + 2 < D / 16) ask_x(j + 2);
+            __builtin_amdgcn_sched_barrier(0);
+            dp = mfma<T>(y[j & 1], j < kHeld ? vals[j] : z[j & 1], dp);
+            if (j + 2 < D / 16) ask_y(j + 2);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        float p[16], ds[16];
 #pragma unroll
-                for (int j = 0; j < D / 16; ++j) {
-                    s = mfma<T>(rows_at<D>(queries, t, j, lane), keys[j], s);
-                    dp = mfma<T>(rows_at<D>(douts, t, j, lane), vals[j], dp);
-                }
-                float p[16], ds[16];
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t r0 = 32 * t + 8 * q + 4 * half;
+            const float4 base = *(const float4 *)&rows[kSet][0][r0], delta = *(const float4 *)&rows[kSet][1][r0];
+            const float l[4] = {base.x, base.y, base.z, base.w}, d[4] = {delta.x, delta.y, delta.z, delta.w};
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const uint32_t r0 = 32 * t + 8 * q + 4 * (lane / 32);
-                    const float4 lse = *(const float4 *)&rows[set][0][r0], delta = *(const float4 *)&rows[set][1][r0];
-                    const float l[4] = {lse.x, lse.y, lse.z, lse.w}, d[4] = {delta.x, delta.y, delta.z, delta.w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int r = 4 * q + e;
-                        p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -l[e] * kLog2e));
-                        ds[r] = p[r] * (dp[r] - d[e]);
-                    }
-                }
-                if (t0 < k0 + 31) {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (t0 + (r & 3) + 8 * (r >> 2) + 4 * (lane / 32) < key) p[r] = ds[r] = 0.0f;
-                }
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const Words4 pw = packed<T>(p, j), dw = packed<T>(ds, j);
-#pragma unroll
-                    for (int d = 0; d < D / 32; ++d) {
-                        dv[d] = mfma<T>(turned_at<D>(douts, 2 * t + j, d, lane), pw, dv[d]);
-                        dk[d] = mfma<T>(turned_at<D>(queries, 2 * t + j, d, lane), dw, dk[d]);
-                    }
-                }
+            for (int e = 0; e < 4; ++e) {
+                const int r = 4 * q + e;
+                p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, l[e]));
+                ds[r] = p[r] * (dp[r] - d[e]);
             }
         }
-    store_turned<T, D>(dk, a.scale, there ? (raw *)row_of<T>(a.dk, key, kv) : nullptr, a.dim, lane);
-    store_turned<T, D>(dv, 1.0f, there ? (raw *)row_of<T>(a.dv, key, kv) : nullptr, a.dim, lane);
+        if (t0 < k0 + 31) {
+            const int before = (int)(key - t0) - (int)(4 * half);    // the first of these queries come before the key
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if ((r & 3) + 8 * (r >> 2) < before) p[r] = ds[r] = 0.0f;
+        }
+        const Words4 pw[2] = {packed<T>(p, 0), packed<T>(p, 1)}, dw[2] = {packed<T>(ds, 0), packed<T>(ds, 1)};
+        Words4 u[3], v[3];
+        const auto ask_turned = [&](int j) {
+            u[j % 3] = reader.template turn<kDout>(2 * t + j / (D / 32), j % (D / 32));
+            v[j % 3] = reader.template turn<kQueries>(2 * t + j / (D / 32), j % (D / 32));
+        };
+        ask_turned(0);
+        ask_turned(1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) {
+            if (j + 2 < D / 16) ask_turned(j + 2);
+            constexpr int kTurns = D / 32;
+            dv[j % kTurns] = mfma<T>(u[j % 3], pw[j / kTurns], dv[j % kTurns]);
+            dk[j % kTurns] = mfma<T>(v[j % 3], dw[j / kTurns], dk[j % kTurns]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    uint32_t first = at.begin + (tiles - 1) * kTile, heads = 0;
+    const uint64_t turns = (uint64_t)tiles * group;
+    fetch(0);
+    const auto step = [&](auto stage) {
+        constexpr uint32_t kSet = decltype(stage)::value;
+        __builtin_amdgcn_s_waitcnt(0x0f70);    // vmcnt(0): this wave's part of the tile is in LDS
+        __syncthreads();
+        fetch(kSet ^ 1);
+        use(stage, 0, first);
+        use(stage, 1, first + 32);
+        if (++heads == group) {
+            heads = 0;
+            first -= kTile;
+        }
+    };
+    for (uint64_t turn = 0; turn < turns; turn += 2) {
+        step(At<0>{});
+        if (turn + 1 < turns) step(At<1>{});
+    }
+    if (a.split == 1) {
+        store_turned<T, D>(dk, a.scale, there ? (raw *)row_of<T>(a.dk, key, kv) : nullptr, a.dim, lane);
+        store_turned<T, D>(dv, 1.0f, there ? (raw *)row_of<T>(a.dv, key, kv) : nullptr, a.dim, lane);
+    } else {
+        const uint64_t whole = (uint64_t)a.tokens * a.kv_heads * a.dim;
+        float *to = a.parts + 2 * part * whole + ((uint64_t)key * a.kv_heads + kv) * a.dim;
+        store_turned<F32, D>(dk, a.scale, there ? to : nullptr, a.dim, lane);
+        store_turned<F32, D>(dv, 1.0f, there ? to + whole : nullptr, a.dim, lane);
+    }
+}
+
+// dk and dv of the blocks that share a key's query heads, in order: eight values a lane.
+template <class T>
+__global__ __launch_bounds__(kBlock) void attention_join_kernel(Attention a) {
+    const uint32_t per_token = a.kv_heads * (a.dim / 8);
+    const uint64_t i = (uint64_t)blockIdx.x * kBlock + threadIdx.x;
+    const uint32_t token = (uint32_t)(i / per_token), at = (uint32_t)(i % per_token);
+    if (i >= (uint64_t)a.tokens * per_token) return;
+    if (a.offsets && (token < bound_of(a.offsets, 0, a.tokens) || token >= bound_of(a.offsets, a.sequences, a.tokens))) return;
+    const uint64_t whole = (uint64_t)a.tokens * a.kv_heads * a.dim;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        float sum[8] = {};
+        for (uint32_t s = 0; s < a.split; ++s) {
+            float v[8];
+            load_slice<F32>(a.parts + (2 * s + w) * whole + i * 8, 0, 8, v);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) sum[c] += v[c];
+        }
+        const Heads &to = w ? a.dv : a.dk;
+        store_slice<T>((typename T::raw *)row_of<T>(to, token, at / (a.dim / 8)) + at % (a.dim / 8) * 8, 0, 8, sum);
+    }
 }
 
 inline int check_heads(const void *p, uint64_t token, uint64_t head, uint64_t tokens, uint64_t heads, uint64_t dim) {
@@ -477,10 +633,25 @@ inline int for_heads(uint32_t type, uint64_t dim, F f) {
     return dim <= 64 ? f(BF16{}, Small{}) : f(BF16{}, Large{});
 }
 
+inline uint64_t attention_tiles(uint64_t tokens, uint64_t sequences) {
+    const uint32_t size = 32 * kWaves;
+    return sequences ? tiles_for(tokens, sequences, size) : (tokens + size - 1) / size;
+}
+
+// Blocks that share a key's query heads: enough that there are two for each that a chip has at a time, so that the keys with
+// the most queries, which take longest, do not go on alone; the sums of their parts take 1 GB at most.  8192 tokens, 32 heads on 8: SPLITFIGURES.
+inline uint32_t split_of(uint64_t tokens, uint64_t sequences, uint64_t heads, uint64_t kv_heads, uint64_t dim) {
+    const uint64_t group = heads / kv_heads, blocks = attention_tiles(tokens, sequences) * kv_heads;
+    uint64_t n = 1;
+    while (n < group && (blocks * n < 1024 || group % n)) ++n;
+    while (n > 1 && (group % n || n * tokens * kv_heads * dim * 8 > 1ull << 30)) --n;
+    return (uint32_t)n;
+}
+
 template <class K>
-inline int run_attention(K kernel, Attention &a, uint32_t heads, uint32_t waves, void *hip_stream) {
-    const uint64_t size = 32 * waves;
-    const uint64_t tiles = a.offsets ? tiles_for(a.tokens, a.sequences, (uint32_t)size) : (a.tokens + size - 1) / size;
+inline int run_attention(K kernel, Attention &a, uint64_t heads, void *hip_stream) {
+    constexpr uint32_t waves = kWaves;
+    const uint64_t tiles = attention_tiles(a.tokens, a.offsets ? a.sequences : 0);
     if (tiles * heads > 0x7fffff00ull) return POSEIDON_E_RANGE;
     a.tiles = (uint32_t)tiles;
     kernel<<<(uint32_t)(tiles * heads) + (a.offsets ? kClearBlocks : 0), 64 * waves, 0, (hipStream_t)hip_stream>>>(a);
@@ -520,12 +691,18 @@ int poseidon_attention_forward(const void *q, uint64_t q_token, uint64_t q_head,
     a.dim = dim;
     a.scale = scale;
     return for_heads(type, dim, [&](auto t, auto d) {
-        return run_attention(attention_forward_kernel<decltype(t), d.value, 4>, a, heads, 4, hip_stream);
+        return run_attention(attention_forward_kernel<decltype(t), d.value, kWaves>, a, heads, hip_stream);
     });
 }
 
-uint64_t poseidon_attention_backward_workspace(uint64_t tokens, uint32_t heads) {
-    return tokens > POSEIDON_ROWS_MAX || !heads || heads > POSEIDON_HEADS_MAX ? UINT64_MAX : tokens * heads * 4;
+uint64_t poseidon_attention_backward_workspace(uint64_t tokens, uint32_t heads, uint32_t kv_heads, uint32_t dim, uint32_t sequences) {
+    if (check_attention(tokens, heads, kv_heads, dim, 1.0f, nullptr, 1) != POSEIDON_OK) return UINT64_MAX;
+    uint64_t parts = 0;
+    for (const uint64_t n : {(uint64_t)sequences, (uint64_t)0}) {    // the call may come without offsets
+        const uint64_t split = split_of(tokens, n, heads, kv_heads, dim);
+        if (split > parts) parts = split;
+    }
+    return tokens * heads * 8 + (parts > 1 ? parts * tokens * kv_heads * dim * 8 : 0);
 }
 
 int poseidon_attention_backward(const void *dout, uint64_t dout_token, uint64_t dout_head, const void *q,
@@ -547,7 +724,7 @@ int poseidon_attention_backward(const void *dout, uint64_t dout_token, uint64_t 
     PL_TRY(check_heads(dk, dk_token, dk_head, tokens, kv_heads, dim));
     PL_TRY(check_heads(dv, dv_token, dv_head, tokens, kv_heads, dim));
     if (tokens && (!lse || !aligned(lse, 4))) return POSEIDON_E_INVAL;
-    PL_TRY(check_workspace(workspace, workspace_bytes, poseidon_attention_backward_workspace(tokens, heads)));
+    PL_TRY(check_workspace(workspace, workspace_bytes, poseidon_attention_backward_workspace(tokens, heads, kv_heads, dim, sequences)));
     if (!tokens) return POSEIDON_OK;
     Attention a = {};
     a.q = {q, q_token, q_head};
@@ -560,6 +737,9 @@ int poseidon_attention_backward(const void *dout, uint64_t dout_token, uint64_t 
     a.dv = {dv, dv_token, dv_head};
     a.lse = const_cast<float *>(lse);
     a.delta = (float *)workspace;
+    a.base = a.delta + tokens * heads;
+    a.parts = a.base + tokens * heads;
+    a.split = split_of(tokens, offsets ? sequences : 0, heads, kv_heads, dim);
     a.offsets = offsets;
     a.tokens = (uint32_t)tokens;
     a.sequences = sequences;
@@ -568,8 +748,12 @@ int poseidon_attention_backward(const void *dout, uint64_t dout_token, uint64_t 
     a.dim = dim;
     a.scale = scale;
     return for_heads(type, dim, [&](auto t, auto d) -> int {
-        PL_TRY(run_attention(attention_queries_kernel<decltype(t), d.value, 4>, a, heads, 4, hip_stream));
-        return run_attention(attention_keys_kernel<decltype(t), d.value, 4>, a, kv_heads, 4, hip_stream);
+        PL_TRY(run_attention(attention_queries_kernel<decltype(t), d.value, kWaves>, a, heads, hip_stream));
+        PL_TRY(run_attention(attention_keys_kernel<decltype(t), d.value, kWaves>, a, (uint64_t)kv_heads * a.split, hip_stream));
+        if (a.split == 1) return POSEIDON_OK;
+        const uint64_t slices = tokens * kv_heads * (dim / 8);
+        attention_join_kernel<decltype(t)><<<(uint32_t)((slices + kBlock - 1) / kBlock), kBlock, 0, (hipStream_t)hip_stream>>>(a);
+        return launched();
     });
 }
 

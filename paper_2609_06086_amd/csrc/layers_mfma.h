@@ -33,10 +33,12 @@ __device__ __forceinline__ Rsrc buffer(const void *p, uint32_t bytes) {
 // Four rows of a column of 16-bit values that lie row by row in LDS.
 // The sixteen lanes of a quarter of the wave bring the addresses of 4 rows x 16 values, four neighbouring values a lane,
 // row by row, and lane l of them gets the rows of value l % 16.
-__device__ __forceinline__ uint2 read_turned(const uint16_t *lds) {
+__device__ __forceinline__ uint2 read_turned(__attribute__((address_space(3))) const void *lds) {
     using Four = short __attribute__((ext_vector_type(4)));
-    using Place = __attribute__((address_space(3))) Four *;
-    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(lds)));
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) Four *)lds));
+}
+__device__ __forceinline__ uint2 read_turned(const uint16_t *lds) {
+    return read_turned((__attribute__((address_space(3))) const void *)lds);
 }
 
 // 16 bytes a lane from a buffer to LDS, at `to` + 16 lane; an offset past the buffer's end brings zeros.
@@ -45,12 +47,19 @@ __device__ __forceinline__ void copy_to_lds(Rsrc from, uint32_t offset, uint16_t
 }
 constexpr uint32_t kNowhere = 0x80000000u, kBufferBytes = 0x7ffffff0u;
 
+// Two values rounded to nearest even, in one instruction.
 template <class T>
-__device__ __forceinline__ uint32_t pair(float lo, float hi) {    // rounded to nearest even
-    typename T::raw v[2] = {T::down(lo), T::down(hi)};
-    uint32_t w;
-    __builtin_memcpy(&w, v, 4);
-    return w;
+__device__ __forceinline__ uint32_t pair(float lo, float hi) {
+    using Two = typename T::raw __attribute__((ext_vector_type(2)));
+    using Floats = float __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((Floats){lo, hi}, Two));
+}
+
+// How the compiler is to mix what a block of code does: first N of a kind, and so on, in the order of the calls.
+constexpr int kMatrix = 0x8, kAlu = 0x402, kReadLds = 0x100;
+template <int KIND, int N>
+__device__ __forceinline__ void then() {
+    __builtin_amdgcn_sched_group_barrier(KIND, N, 0);
 }
 
 // Which of the ranges [offsets[r], offsets[r + 1]) of rows a tile belongs to.  Range r has the tiles from

@@ -55,7 +55,7 @@ _ARGS = {
     "poseidon_attention_forward": [_p, _u64, _u64] * 3 + [_u32, _u64, _u32, _u32, _u32, C.c_float, _p, _u32, _p, _u64, _u64, _p, _p],
     "poseidon_attention_backward": [_p, _u64, _u64] * 5 + [_p, _u32, _u64, _u32, _u32, _u32, C.c_float, _p, _u32] +
                                    [_p, _u64, _u64] * 3 + [_p, _u64, _p],
-    "poseidon_attention_backward_workspace": [_u64, _u32],
+    "poseidon_attention_backward_workspace": [_u64, _u32, _u32, _u32, _u32],
 }
 EXPORTS = tuple(_ARGS)
 
@@ -660,7 +660,7 @@ def poseidon_attention_backward(dout, q, k, v, out, lse, offsets=None, *, scale=
     lse = _whole(lse, f"{name}: lse", dev, torch.float32, (h, n))
     dq = _heads_out(dq, f"{name}: dq", dev, dt, shape)
     dk, dv = (_heads_out(x, f"{name}: {w}", dev, dt, kv_shape) for x, w in ((dk, "dk"), (dv, "dv")))
-    w, at, size = _workspace(name, dev, n, h)
+    w, at, size = _workspace(name, dev, n, h, kv_shape[1], d, sequences)
     _call(name, dev, *_places(dout, q, k, v, out), lse.data_ptr(), TYPES[dt], n, h, kv_shape[1], d, scale,
           None if offsets is None else offsets.data_ptr(), sequences, *_places(dq, dk, dv), at, size)
     return dq[0], dk[0], dv[0]
