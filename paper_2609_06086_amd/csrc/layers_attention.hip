@@ -638,12 +638,15 @@ inline uint64_t attention_tiles(uint64_t tokens, uint64_t sequences) {
     return sequences ? tiles_for(tokens, sequences, size) : (tokens + size - 1) / size;
 }
 
-// Blocks that share a key's query heads: enough that there are two for each that a chip has at a time, so that the keys with
-// the most queries, which take longest, do not go on alone; the sums of their parts take 1 GB at most.  8192 tokens, 32 heads on 8: SPLITFIGURES.
+// Blocks that share a key's query heads, each with some of them: the keys with the most queries take longest and would go on
+// alone.  1024 blocks, two for each that the chip has at a time, are enough for one sequence (8192 tokens, 32 heads on 8: 1444 us
+// in 512 blocks, 1100 in 1024, 1111 in 2048, the sum of parts counted), 2048 for several, whose longest may
+// come late (16384 tokens in 24 sequences, 16 heads on 8: 446 us in 1216 blocks, 413 in 2432).  The sums of parts take 1 GB at most.
 inline uint32_t split_of(uint64_t tokens, uint64_t sequences, uint64_t heads, uint64_t kv_heads, uint64_t dim) {
     const uint64_t group = heads / kv_heads, blocks = attention_tiles(tokens, sequences) * kv_heads;
+    const uint64_t least = sequences > 1 ? 2048 : 1024;
     uint64_t n = 1;
-    while (n < group && (blocks * n < 1024 || group % n)) ++n;
+    while (n < group && (blocks * n < least || group % n)) ++n;
     while (n > 1 && (group % n || n * tokens * kv_heads * dim * 8 > 1ull << 30)) --n;
     return (uint32_t)n;
 }

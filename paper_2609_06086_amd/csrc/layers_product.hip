@@ -6,7 +6,7 @@
 
 namespace pl {
 
-constexpr uint32_t kDeep = 64;           // values along the sum in a step
+constexpr uint32_t kDeep = 64;           // values along the sum in a stage
 constexpr uint32_t kClearing = 64;       // blocks that look for rows outside of all ranges
 
 struct Product {
@@ -50,13 +50,19 @@ __device__ __forceinline__ void clear_outside(const Product &g, uint32_t block, 
 }
 
 // R x C waves on a tile of 32 R M rows by 32 C N columns, 32 M x 32 N a wave.
-// TURNED: W^T, whose values along the sum are a row apart.
+// TURNED: W^T, whose values along the sum are a row apart.  ALIGNED: rows begin on 16 bytes and are whole pieces of 16 bytes, which
+// go to LDS without a register between; else they are read with plain loads, which take any address, and masked.
+//
+// LDS holds two stages of 64 values along the sum, 128 bytes of a row.  The last of a stage's operands are in registers when
+// a quarter of its products is still to come: there the waves meet, the stage's place is given to the one after the
+// next, and the next one's first operands are read beside the last products, so that no wave waits for LDS at a stage's start.
 template <class T, bool TURNED, bool ALIGNED, int R, int C, int M, int N>
 __global__ __launch_bounds__(64 * R * C, 2) void product_kernel(Product g) {
     constexpr uint32_t kRows = 32 * R * M, kCols = 32 * C * N, kThreads = 64 * R * C;
-    constexpr uint32_t kX = kRows * kDeep, kW = kCols * kDeep;    // values of a step
+    constexpr uint32_t kX = kRows * kDeep, kW = kCols * kDeep, kStage = kX + kW;    // values of a stage
     constexpr uint32_t kLoadsX = kX / 8 / kThreads, kLoadsW = kW / 8 / kThreads;
-    __shared__ __attribute__((aligned(16))) uint16_t lds[2 * (kX + kW)];
+    constexpr uint32_t kPieces = kDeep / 8;                                         // of a row
+    __shared__ __attribute__((aligned(16))) uint16_t lds[2 * kStage];
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const uint32_t tiles = g.tiles_r * g.tiles_c;
     if (blockIdx.x >= tiles) {
@@ -71,73 +77,71 @@ __global__ __launch_bounds__(64 * R * C, 2) void product_kernel(Product g) {
     using raw = typename T::raw;
     const raw *x = (const raw *)g.x + row0 * g.pitch;
     const raw *w = (const raw *)g.weights + (uint64_t)at.range * g.deep * g.wide + (TURNED ? col0 : (uint64_t)col0 * g.deep);
-    const uint32_t steps = (g.deep + kDeep - 1) / kDeep;
+    const uint32_t stages = (g.deep + kDeep - 1) / kDeep;
 
-    // Rows of LDS hold 64 values along the sum in eight pieces of 16 bytes; piece p lies at p ^ (row & 7), so that
-    // neighbouring lanes' rows, 128 bytes apart, are read from all banks.  TURNED: rows of kCols values of W, piece p
-    // at p ^ 4 (row & 3), so that four rows are read from all banks.
-    uint32_t x_at[kLoadsX], x_col[kLoadsX], w_at[kLoadsW], w_col[kLoadsW];
-    uint64_t x_row[kLoadsX], w_row[kLoadsW];
-#pragma unroll
-    for (uint32_t i = 0; i < kLoadsX; ++i) {
-        const uint32_t piece = i * kThreads + tid, row = piece / 8;
-        x_col[i] = ((piece ^ row) & 7) * 8;
-        x_row[i] = (uint64_t)min(row, here - 1) * g.pitch;
-        x_at[i] = (uint32_t)(x_row[i] + x_col[i]) * 2;
-    }
-#pragma unroll
-    for (uint32_t i = 0; i < kLoadsW; ++i) {
-        const uint32_t piece = i * kThreads + tid;
-        if constexpr (TURNED) {
-            const uint32_t k = piece / (kCols / 8);
-            w_col[i] = (piece % (kCols / 8) ^ 4 * (k & 3)) * 8;
-            w_row[i] = k;
-            w_at[i] = col0 + w_col[i] < g.wide ? (k * g.wide + w_col[i]) * 2 : kNowhere;
-        } else {
-            const uint32_t row = piece / 8;
-            w_col[i] = ((piece ^ row) & 7) * 8;
-            w_row[i] = (uint64_t)min(row, g.wide - 1 - col0) * g.deep;
-            w_at[i] = (uint32_t)(w_row[i] + w_col[i]) * 2;
-        }
-    }
+    // Rows of LDS are eight pieces of 16 bytes; piece p lies at p ^ (row / 2 & 7), so that sixteen rows' are read from banks
+    // of their own.  TURNED: rows of kCols values of W, piece p at p ^ 4 (row & 3), for four rows' next four pieces.
+    // A lane's pieces of a stage lie at the same place of rows a multiple of 16 (4) apart.
+    const uint32_t x_row = tid / kPieces, x_col = ((tid ^ x_row / 2) & 7) * 8;
+    const uint32_t w_row = TURNED ? tid / (kCols / 8) : x_row, w_col = TURNED ? (tid % (kCols / 8) ^ 4 * (w_row & 3)) * 8 : x_col;
+    constexpr uint32_t kStepX = kThreads / kPieces, kStepW = TURNED ? kThreads / (kCols / 8) : kStepX;    // rows from piece to piece
+    static_assert(kStepX % 16 == 0 && kStepW % 4 == 0);
+    const uint32_t x_at = (x_row * (uint32_t)g.pitch + x_col) * 2;
+    const uint32_t w_at = TURNED ? (col0 + w_col < g.wide ? (w_row * g.wide + w_col) * 2 : kNowhere) : (w_row * g.deep + w_col) * 2;
+    const uint32_t w_here = min(g.wide - col0, kCols);
     Words4 held_x[ALIGNED ? 1 : kLoadsX], held_w[ALIGNED ? 1 : kLoadsW];
-    const auto fetch = [&](uint32_t step) {    // asks for a step's values; ALIGNED: right into LDS
-        const uint32_t k0 = step * kDeep;
+    // Asks for a stage's values; ALIGNED: right into LDS.  Past the rows, the columns and the sum come zeros.
+    const auto fetch = [&](uint32_t stage) __attribute__((always_inline)) {
+        const uint32_t k0 = stage * kDeep;
         if constexpr (ALIGNED) {
-            uint16_t *to = lds + (step & 1) * (kX + kW) + wave * 512;
-            const Rsrc from_x = buffer(x + k0, kBufferBytes);
-            const Rsrc from_w = buffer(TURNED ? w + (uint64_t)k0 * g.wide : w + k0, kBufferBytes);
+            uint16_t *to = lds + (stage & 1) * kStage + wave * 512;
+            const uint32_t xo = k0 + x_col < g.deep ? x_at : kNowhere;
+            const uint32_t wo = TURNED || k0 + w_col < g.deep ? w_at : kNowhere;
 #pragma unroll
-            for (uint32_t i = 0; i < kLoadsX; ++i)
-                copy_to_lds(from_x, k0 + x_col[i] < g.deep ? x_at[i] : kNowhere, to + i * kThreads * 8);
+            for (uint32_t i = 0; i < kLoadsX; ++i) {
+                const uint32_t left = here > i * kStepX ? min(here - i * kStepX, kStepX) : 0;
+                copy_to_lds(buffer(x + i * kStepX * g.pitch + k0, __builtin_amdgcn_readfirstlane(left * (uint32_t)g.pitch * 2)), xo,
+                            to + i * kThreads * 8);
+            }
 #pragma unroll
-            for (uint32_t i = 0; i < kLoadsW; ++i)
-                copy_to_lds(from_w, k0 + (TURNED ? (uint32_t)w_row[i] : w_col[i]) < g.deep ? w_at[i] : kNowhere,
-                            to + kX + i * kThreads * 8);
+            for (uint32_t i = 0; i < kLoadsW; ++i) {
+                uint32_t bytes;
+                const raw *from;
+                if constexpr (TURNED) {
+                    const uint32_t k = k0 + i * kStepW, left = g.deep > k ? min(g.deep - k, kStepW) : 0;
+                    from = w + (uint64_t)k * g.wide;
+                    bytes = left * g.wide * 2;
+                } else {
+                    const uint32_t left = w_here > i * kStepW ? min(w_here - i * kStepW, kStepW) : 0;
+                    from = w + (uint64_t)(i * kStepW) * g.deep + k0;
+                    bytes = left * g.deep * 2;
+                }
+                copy_to_lds(buffer(from, __builtin_amdgcn_readfirstlane(bytes)), wo, to + kX + i * kThreads * 8);
+            }
         } else {
 #pragma unroll
             for (uint32_t i = 0; i < kLoadsX; ++i) {
-                const Slice<T> s = load_words<T>(x + x_row[i], k0 + x_col[i], g.deep);
+                const Slice<T> s = load_words<T>(x + min(x_row + i * kStepX, here - 1) * g.pitch, k0 + x_col, g.deep);
                 held_x[i] = Words4{s.w[0], s.w[1], s.w[2], s.w[3]};
             }
 #pragma unroll
             for (uint32_t i = 0; i < kLoadsW; ++i) {
                 Slice<T> s;
                 if constexpr (TURNED) {
-                    const uint32_t k = k0 + (uint32_t)w_row[i];
-                    s = load_words<T>(w - col0 + (uint64_t)min(k, g.deep - 1) * g.wide, col0 + w_col[i], g.wide);
+                    const uint32_t k = k0 + w_row + i * kStepW;
+                    s = load_words<T>(w - col0 + (uint64_t)min(k, g.deep - 1) * g.wide, col0 + w_col, g.wide);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) s.w[j] = k < g.deep ? s.w[j] : 0u;
                 } else {
-                    s = load_words<T>(w + w_row[i], k0 + w_col[i], g.deep);
+                    s = load_words<T>(w + (uint64_t)min(w_row + i * kStepW, w_here - 1) * g.deep, k0 + w_col, g.deep);
                 }
                 held_w[i] = Words4{s.w[0], s.w[1], s.w[2], s.w[3]};
             }
         }
     };
-    const auto deposit = [&](uint32_t step) {
+    const auto deposit = [&](uint32_t stage) __attribute__((always_inline)) {
         if constexpr (!ALIGNED) {
-            Words4 *to = (Words4 *)(lds + (step & 1) * (kX + kW)) + tid;
+            Words4 *to = (Words4 *)(lds + (stage & 1) * kStage) + tid;
 #pragma unroll
             for (uint32_t i = 0; i < kLoadsX; ++i) to[i * kThreads] = held_x[i];
 #pragma unroll
@@ -145,48 +149,102 @@ __global__ __launch_bounds__(64 * R * C, 2) void product_kernel(Product g) {
         }
     };
 
+    // A wave's operands: values [16 s + 8 (lane / 32), ...) of its rows and columns.
     const uint32_t r0 = wave / C * 32 * M, c0 = wave % C * 32 * N, l32 = lane % 32, half = lane / 32;
-    const auto read_x = [&](uint32_t step, int s, int m) {
-        return *(const Words4 *)(lds + (step & 1) * (kX + kW) + (r0 + 32 * m + l32) * kDeep + ((2 * s + half) ^ (l32 & 7)) * 8);
-    };
-    const auto read_w = [&](uint32_t step, int s, int n) {
-        const uint16_t *from = lds + (step & 1) * (kX + kW) + kX;
-        if constexpr (TURNED) {
-            const uint32_t k = 8 * half + lane % 16 / 4, piece = (c0 / 8 + 4 * n) ^ 4 * (k & 3);
-            from += (16 * s + k) * kCols + (piece + 2 * (lane / 16 % 2) + lane % 4 / 2) * 8 + lane % 2 * 4;
-            const uint2 lo = read_turned(from), hi = read_turned(from + 4 * kCols);
-            return Words4{lo.x, lo.y, hi.x, hi.y};
-        } else {
-            return *(const Words4 *)(from + (c0 + 32 * n + l32) * kDeep + ((2 * s + half) ^ (l32 & 7)) * 8);
+    using Bytes = __attribute__((address_space(3))) const char *;
+    const uint32_t base = (uint32_t)(uintptr_t)(Bytes)(const char *)lds;
+    uint32_t x_from[4], w_from[TURNED ? N : 4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+        const uint32_t piece = ((2 * s + half) ^ l32 / 2) & 7;
+        x_from[s] = base + ((r0 + l32) * kDeep + piece * 8) * 2;
+        if constexpr (!TURNED) w_from[s] = base + (kX + (c0 + l32) * kDeep + piece * 8) * 2;
+    }
+    if constexpr (TURNED) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const uint32_t k = 8 * half + lane % 16 / 4, piece = ((c0 / 8 + 4 * n) ^ 4 * (k & 3)) + 2 * (lane / 16 % 2) + lane % 4 / 2;
+            w_from[n] = base + (kX + k * kCols + piece * 8 + lane % 2 * 4) * 2;
         }
+    }
+    Words4 a[2][M], b[2][N];
+    const auto read = [&](auto stage, int s) {    // stage: its place in LDS
+        constexpr uint32_t kAt = decltype(stage)::value * kStage * 2;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            if constexpr (TURNED) {
+                const uint2 lo = read_turned((Bytes)(uintptr_t)w_from[n] + kAt + 32 * s * kCols);
+                const uint2 hi = read_turned((Bytes)(uintptr_t)w_from[n] + kAt + (32 * s + 8) * kCols);
+                b[s & 1][n] = Words4{lo.x, lo.y, hi.x, hi.y};
+            } else {
+                b[s & 1][n] = *(__attribute__((address_space(3))) const Words4 *)((Bytes)(uintptr_t)w_from[s] + kAt + 64 * n * kDeep);
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < M; ++m)
+            a[s & 1][m] = *(__attribute__((address_space(3))) const Words4 *)((Bytes)(uintptr_t)x_from[s] + kAt + 64 * m * kDeep);
     };
-
+    constexpr int kReads = M + (TURNED ? 2 * N : N), kProducts = M * N;
     Acc acc[M][N] = {};
+    const auto multiply = [&](int s) {
+#pragma unroll
+        for (int m = 0; m < M; ++m)
+#pragma unroll
+            for (int n = 0; n < N; ++n) acc[m][n] = mfma<T>(b[s & 1][n], a[s & 1][m], acc[m][n]);
+        // one or two reads after a product
+        constexpr int kTwo = kReads > kProducts ? kReads - kProducts : 0, kOne = (kReads < kProducts ? kReads : kProducts) - kTwo;
+#pragma unroll
+        for (int i = 0; i < kTwo; ++i) {
+            then<kMatrix, 1>();
+            then<kReadLds, 2>();
+        }
+#pragma unroll
+        for (int i = 0; i < kOne; ++i) {
+            then<kMatrix, 1>();
+            then<kReadLds, 1>();
+        }
+        if constexpr (kProducts > kTwo + kOne) then<kMatrix, kProducts - kTwo - kOne>();
+    };
+    // Until every wave of the block has what it read, and what it asked for is in LDS.
+    const auto meet = [&] {
+        __builtin_amdgcn_s_waitcnt(ALIGNED ? 0x0070 : 0xc07f);    // vmcnt(0) lgkmcnt(0); not ALIGNED: lgkmcnt(0)
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    using First = std::integral_constant<int, 0>;
+    using Second = std::integral_constant<int, 1>;
     fetch(0);
     deposit(0);
-    for (uint32_t step = 0; step < steps; ++step) {
-        if constexpr (ALIGNED) __builtin_amdgcn_s_waitcnt(0x0f70);    // vmcnt(0): this wave's part of the step is in LDS
-        __syncthreads();
-        if (step + 1 < steps) fetch(step + 1);
-        Words4 a[2][M], b[2][N];
-#pragma unroll
-        for (int m = 0; m < M; ++m) a[0][m] = read_x(step, 0, m);
-#pragma unroll
-        for (int n = 0; n < N; ++n) b[0][n] = read_w(step, 0, n);
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            if (s < 3) {
-#pragma unroll
-                for (int m = 0; m < M; ++m) a[(s + 1) & 1][m] = read_x(step, s + 1, m);
-#pragma unroll
-                for (int n = 0; n < N; ++n) b[(s + 1) & 1][n] = read_w(step, s + 1, n);
-            }
-#pragma unroll
-            for (int m = 0; m < M; ++m)
-#pragma unroll
-                for (int n = 0; n < N; ++n) acc[m][n] = mfma<T>(b[s & 1][n], a[s & 1][m], acc[m][n]);
+    meet();
+    if (stages > 1) {
+        fetch(1);
+        deposit(1);
+    }
+    read(First{}, 0);
+    const auto step = [&](auto place, auto other, uint32_t i) __attribute__((always_inline)) {
+        if constexpr (!ALIGNED) {
+            if (i + 2 < stages) fetch(i + 2);
         }
-        if (step + 1 < steps) deposit(step + 1);
+        read(place, 1);
+        multiply(0);
+        read(place, 2);
+        multiply(1);
+        read(place, 3);
+        multiply(2);
+        meet();
+        if (i + 2 < stages) {
+            if constexpr (ALIGNED)
+                fetch(i + 2);
+            else
+                deposit(i + 2);
+        }
+        read(other, 0);    // after the last stage: of what lies there, to no use
+        multiply(3);
+    };
+    for (uint32_t i = 0; i < stages; i += 2) {
+        step(First{}, Second{}, i);
+        if (i + 1 < stages) step(Second{}, First{}, i + 1);
     }
 
     // A lane has a row, and of each 32 columns 4 of every 8: the two halves of the wave trade theirs, so that a lane
@@ -201,10 +259,10 @@ __global__ __launch_bounds__(64 * R * C, 2) void product_kernel(Product g) {
                 float v[8];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float lo = acc[m][n][8 * q + i], hi = acc[m][n][8 * q + 4 + i];
-                    const float other = __shfl_xor(half ? lo : hi, 32, 64);
-                    v[i] = half ? other : lo;
-                    v[4 + i] = half ? hi : other;
+                    const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[m][n][8 * q + i]),
+                                                                    __float_as_uint(acc[m][n][8 * q + 4 + i]), false, false);
+                    v[i] = __uint_as_float(w[0]);
+                    v[4 + i] = __uint_as_float(w[1]);
                 }
                 const uint32_t col = col0 + c0 + 32 * n + 16 * q + 8 * half;
                 if (r >= here || col >= g.wide) continue;
