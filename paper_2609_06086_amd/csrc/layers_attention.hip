@@ -66,7 +66,7 @@ struct Loader {
 #pragma unroll
         for (uint32_t i = 0; i < kTile / kRows; ++i) {
             const uint32_t left = rows > i * kRows ? min(rows - i * kRows, kRows) : 0;
-            copy_to_lds(buffer(from + i * kRows * pitch, __builtin_amdgcn_readfirstlane(left * ((uint32_t)pitch * 2))), place,
+            copy_to_lds<false>(buffer(from + i * kRows * pitch, __builtin_amdgcn_readfirstlane(left * ((uint32_t)pitch * 2))), place,
                         to + (i * THREADS + __builtin_amdgcn_readfirstlane(threadIdx.x & ~63u)) * 8);
         }
     }
@@ -479,8 +479,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_keys_kernel(Attention
         loader.template load<T>(row_of<T>(a.dout, t, head), a.dout.token, dout_place, n, to + kTile * D);
         if (wave < 2) {    // rows past the end: zeros, as q and dout have there
             const float *from = (wave ? a.delta : a.base) + (uint64_t)head * a.tokens + t;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer(from, __builtin_amdgcn_readfirstlane(min(n, kTile) * 4)),
-                                                     (__attribute__((address_space(3))) void *)rows[set][wave], 4, lane * 4, 0, 0, 0);
+            const auto to = (__attribute__((address_space(3))) void *)rows[set][wave];
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer(from, __builtin_amdgcn_readfirstlane(min(n, kTile) * 4)), to, 4, lane * 4, 0, 0, 0);
         }
         if (++g == group) {
             g = 0;

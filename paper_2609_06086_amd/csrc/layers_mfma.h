@@ -41,9 +41,18 @@ __device__ __forceinline__ uint2 read_turned(const uint16_t *lds) {
     return read_turned((__attribute__((address_space(3))) const void *)lds);
 }
 
-// 16 bytes a lane from a buffer to LDS, at `to` + 16 lane; an offset past the buffer's end brings zeros.
+// 16 bytes a lane from a buffer to LDS, at `to` + 16 lane; an offset past the buffer's end brings zeros.  Before a turned read
+// the compiler waits for every such load that it knows of, though it may be meant for another stage.  OWN loads are instructions that it
+// does not know: nothing but the caller's own wait for vmcnt says that they are done.  Their s_nop stands for the waits that
+// the compiler puts between what writes m0 or the descriptor's registers and such a load.
+template <bool OWN>
 __device__ __forceinline__ void copy_to_lds(Rsrc from, uint32_t offset, uint16_t *to) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)to, 16, offset, 0, 0, 0);
+    using Place = __attribute__((address_space(3))) void *;
+    if constexpr (OWN)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                     :: "s"(__builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(Place)to)), "v"(offset), "s"(from) : "memory", "m0");
+    else
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (Place)to, 16, offset, 0, 0, 0);
 }
 constexpr uint32_t kNowhere = 0x80000000u, kBufferBytes = 0x7ffffff0u;
 

@@ -59,10 +59,11 @@ __device__ __forceinline__ void clear_outside(const Product &g, uint32_t block, 
 template <class T, bool TURNED, bool ALIGNED, int R, int C, int M, int N>
 __global__ __launch_bounds__(64 * R * C, 2) void product_kernel(Product g) {
     constexpr uint32_t kRows = 32 * R * M, kCols = 32 * C * N, kThreads = 64 * R * C;
-    constexpr uint32_t kX = kRows * kDeep, kW = kCols * kDeep, kStage = kX + kW;    // values of a stage
+    constexpr uint32_t kX = kRows * kDeep, kW = kCols * kDeep, kStageW = 2 * kX;    // values of a stage; where the weights begin
     constexpr uint32_t kLoadsX = kX / 8 / kThreads, kLoadsW = kW / 8 / kThreads;
+    constexpr uint32_t kPlaces = 3;    // of the weights, which come from further away: other rows of them for every stage of W^T
     constexpr uint32_t kPieces = kDeep / 8;                                         // of a row
-    __shared__ __attribute__((aligned(16))) uint16_t lds[2 * kStage];
+    __shared__ __attribute__((aligned(16))) uint16_t lds[2 * kX + kPlaces * kW];    // two stages of x, then those of the weights
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const uint32_t tiles = g.tiles_r * g.tiles_c;
     if (blockIdx.x >= tiles) {
@@ -90,19 +91,36 @@ __global__ __launch_bounds__(64 * R * C, 2) void product_kernel(Product g) {
     const uint32_t w_at = TURNED ? (col0 + w_col < g.wide ? (w_row * g.wide + w_col) * 2 : kNowhere) : (w_row * g.deep + w_col) * 2;
     const uint32_t w_here = min(g.wide - col0, kCols);
     Words4 held_x[ALIGNED ? 1 : kLoadsX], held_w[ALIGNED ? 1 : kLoadsW];
-    // Asks for a stage's values; ALIGNED: right into LDS.  Past the rows, the columns and the sum come zeros.
-    const auto fetch = [&](uint32_t stage) __attribute__((always_inline)) {
+    // Ask for a stage's values; ALIGNED: right into LDS.  Past the rows, the columns and the sum come zeros.
+    const auto fetch_x = [&](uint32_t stage, auto place) __attribute__((always_inline)) {
         const uint32_t k0 = stage * kDeep;
         if constexpr (ALIGNED) {
-            uint16_t *to = lds + (stage & 1) * kStage + wave * 512;
+            uint16_t *to = lds + decltype(place)::value * kX + wave * 512;
             const uint32_t xo = k0 + x_col < g.deep ? x_at : kNowhere;
-            const uint32_t wo = TURNED || k0 + w_col < g.deep ? w_at : kNowhere;
 #pragma unroll
             for (uint32_t i = 0; i < kLoadsX; ++i) {
                 const uint32_t left = here > i * kStepX ? min(here - i * kStepX, kStepX) : 0;
-                copy_to_lds(buffer(x + i * kStepX * g.pitch + k0, __builtin_amdgcn_readfirstlane(left * (uint32_t)g.pitch * 2)), xo,
+                copy_to_lds<TURNED>(buffer(x + i * kStepX * g.pitch + k0, __builtin_amdgcn_readfirstlane(left * (uint32_t)g.pitch * 2)), xo,
                             to + i * kThreads * 8);
             }
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < kLoadsX; ++i) {
+                const raw *row = x + min(x_row + i * kStepX, here - 1) * g.pitch;
+                Slice<T> s;
+                if (k0 + kDeep <= g.deep)
+                    get<false>(s.w, row + k0 + x_col);
+                else
+                    s = load_words<T>(row, k0 + x_col, g.deep);
+                held_x[i] = Words4{s.w[0], s.w[1], s.w[2], s.w[3]};
+            }
+        }
+    };
+    const auto fetch_w = [&](uint32_t stage, auto place) __attribute__((always_inline)) {
+        const uint32_t k0 = stage * kDeep;
+        if constexpr (ALIGNED) {
+            uint16_t *to = lds + kStageW + decltype(place)::value * kW + wave * 512;
+            const uint32_t wo = TURNED || k0 + w_col < g.deep ? w_at : kNowhere;
 #pragma unroll
             for (uint32_t i = 0; i < kLoadsW; ++i) {
                 uint32_t bytes;
@@ -116,37 +134,40 @@ __global__ __launch_bounds__(64 * R * C, 2) void product_kernel(Product g) {
                     from = w + (uint64_t)(i * kStepW) * g.deep + k0;
                     bytes = left * g.deep * 2;
                 }
-                copy_to_lds(buffer(from, __builtin_amdgcn_readfirstlane(bytes)), wo, to + kX + i * kThreads * 8);
+                copy_to_lds<TURNED>(buffer(from, __builtin_amdgcn_readfirstlane(bytes)), wo, to + i * kThreads * 8);
             }
         } else {
-#pragma unroll
-            for (uint32_t i = 0; i < kLoadsX; ++i) {
-                const Slice<T> s = load_words<T>(x + min(x_row + i * kStepX, here - 1) * g.pitch, k0 + x_col, g.deep);
-                held_x[i] = Words4{s.w[0], s.w[1], s.w[2], s.w[3]};
-            }
 #pragma unroll
             for (uint32_t i = 0; i < kLoadsW; ++i) {
                 Slice<T> s;
                 if constexpr (TURNED) {
                     const uint32_t k = k0 + w_row + i * kStepW;
-                    s = load_words<T>(w - col0 + (uint64_t)min(k, g.deep - 1) * g.wide, col0 + w_col, g.wide);
+                    const raw *row = w + (uint64_t)min(k, g.deep - 1) * g.wide;
+                    if (k0 + kDeep <= g.deep && col0 + kCols <= g.wide) {
+                        get<false>(s.w, row + w_col);
+                    } else {
+                        s = load_words<T>(row - col0, col0 + w_col, g.wide);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) s.w[j] = k < g.deep ? s.w[j] : 0u;
+                        for (int j = 0; j < 4; ++j) s.w[j] = k < g.deep ? s.w[j] : 0u;
+                    }
                 } else {
-                    s = load_words<T>(w + (uint64_t)min(w_row + i * kStepW, w_here - 1) * g.deep, k0 + w_col, g.deep);
+                    const raw *row = w + (uint64_t)min(w_row + i * kStepW, w_here - 1) * g.deep;
+                    if (k0 + kDeep <= g.deep)
+                        get<false>(s.w, row + k0 + w_col);
+                    else
+                        s = load_words<T>(row, k0 + w_col, g.deep);
                 }
                 held_w[i] = Words4{s.w[0], s.w[1], s.w[2], s.w[3]};
             }
         }
     };
-    const auto deposit = [&](uint32_t stage) __attribute__((always_inline)) {
-        if constexpr (!ALIGNED) {
-            Words4 *to = (Words4 *)(lds + (stage & 1) * kStage) + tid;
+    const auto deposit = [&](auto place_x, auto place_w) __attribute__((always_inline)) {
+        Words4 *to_x = (Words4 *)(lds + decltype(place_x)::value * kX) + tid;
+        Words4 *to_w = (Words4 *)(lds + kStageW + decltype(place_w)::value * kW) + tid;
 #pragma unroll
-            for (uint32_t i = 0; i < kLoadsX; ++i) to[i * kThreads] = held_x[i];
+        for (uint32_t i = 0; i < kLoadsX; ++i) to_x[i * kThreads] = held_x[i];
 #pragma unroll
-            for (uint32_t i = 0; i < kLoadsW; ++i) to[kX / 8 + i * kThreads] = held_w[i];
-        }
+        for (uint32_t i = 0; i < kLoadsW; ++i) to_w[i * kThreads] = held_w[i];
     };
 
     // A wave's operands: values [16 s + 8 (lane / 32), ...) of its rows and columns.
@@ -158,18 +179,18 @@ __global__ __launch_bounds__(64 * R * C, 2) void product_kernel(Product g) {
     for (int s = 0; s < 4; ++s) {
         const uint32_t piece = ((2 * s + half) ^ l32 / 2) & 7;
         x_from[s] = base + ((r0 + l32) * kDeep + piece * 8) * 2;
-        if constexpr (!TURNED) w_from[s] = base + (kX + (c0 + l32) * kDeep + piece * 8) * 2;
+        if constexpr (!TURNED) w_from[s] = base + (kStageW + (c0 + l32) * kDeep + piece * 8) * 2;
     }
     if constexpr (TURNED) {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const uint32_t k = 8 * half + lane % 16 / 4, piece = ((c0 / 8 + 4 * n) ^ 4 * (k & 3)) + 2 * (lane / 16 % 2) + lane % 4 / 2;
-            w_from[n] = base + (kX + k * kCols + piece * 8 + lane % 2 * 4) * 2;
+            w_from[n] = base + (kStageW + k * kCols + piece * 8 + lane % 2 * 4) * 2;
         }
     }
     Words4 a[2][M], b[2][N];
-    const auto read = [&](auto stage, int s) {    // stage: its place in LDS
-        constexpr uint32_t kAt = decltype(stage)::value * kStage * 2;
+    const auto read = [&](auto place_x, auto place_w, int s) {    // of the stage that lies there
+        constexpr uint32_t kAtX = decltype(place_x)::value * kX * 2, kAt = decltype(place_w)::value * kW * 2;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             if constexpr (TURNED) {
@@ -182,7 +203,7 @@ __global__ __launch_bounds__(64 * R * C, 2) void product_kernel(Product g) {
         }
 #pragma unroll
         for (int m = 0; m < M; ++m)
-            a[s & 1][m] = *(__attribute__((address_space(3))) const Words4 *)((Bytes)(uintptr_t)x_from[s] + kAt + 64 * m * kDeep);
+            a[s & 1][m] = *(__attribute__((address_space(3))) const Words4 *)((Bytes)(uintptr_t)x_from[s] + kAtX + 64 * m * kDeep);
     };
     constexpr int kReads = M + (TURNED ? 2 * N : N), kProducts = M * N;
     Acc acc[M][N] = {};
@@ -205,46 +226,76 @@ __global__ __launch_bounds__(64 * R * C, 2) void product_kernel(Product g) {
         }
         if constexpr (kProducts > kTwo + kOne) then<kMatrix, kProducts - kTwo - kOne>();
     };
-    // Until every wave of the block has what it read, and what it asked for is in LDS.
-    const auto meet = [&] {
-        __builtin_amdgcn_s_waitcnt(ALIGNED ? 0x0070 : 0xc07f);    // vmcnt(0) lgkmcnt(0); not ALIGNED: lgkmcnt(0)
+    // Until every wave of the block has what it read, and what it asked for is in LDS but for the latest `left` loads.
+    const auto meet = [&](auto left) {
+        constexpr int n = decltype(left)::value;
+        static_assert(n < 16);
+        __builtin_amdgcn_s_waitcnt(ALIGNED ? 0x0070 | n : 0xc07f);    // vmcnt(n) lgkmcnt(0); not ALIGNED: lgkmcnt(0)
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    using First = std::integral_constant<int, 0>;
-    using Second = std::integral_constant<int, 1>;
-    fetch(0);
-    deposit(0);
-    meet();
-    if (stages > 1) {
-        fetch(1);
-        deposit(1);
+    using N0 = std::integral_constant<int, 0>;
+    using N1 = std::integral_constant<int, 1>;
+    using N2 = std::integral_constant<int, 2>;
+    using Ahead = std::integral_constant<int, (int)kLoadsW>;    // loads of weights that may be on their way
+    fetch_x(0, N0{});
+    fetch_w(0, N0{});
+    if constexpr (!ALIGNED) deposit(N0{}, N0{});
+    if (ALIGNED && stages > 1) {
+        fetch_w(1, N1{});
+        meet(Ahead{});
+    } else {
+        meet(N0{});
     }
-    read(First{}, 0);
-    const auto step = [&](auto place, auto other, uint32_t i) __attribute__((always_inline)) {
+    if (stages > 1) {
+        fetch_x(1, N1{});
         if constexpr (!ALIGNED) {
-            if (i + 2 < stages) fetch(i + 2);
+            fetch_w(1, N1{});
+            deposit(N1{}, N1{});
         }
-        read(place, 1);
+    }
+    if (ALIGNED && stages > 2) fetch_w(2, N2{});
+    read(N0{}, N0{}, 0);
+    const auto step = [&](auto turn, uint32_t i) __attribute__((always_inline)) {
+        constexpr int n = decltype(turn)::value;
+        using X = std::integral_constant<int, n % 2>;
+        using W = std::integral_constant<int, n % 3>;
+        using NextX = std::integral_constant<int, (n + 1) % 2>;
+        using NextW = std::integral_constant<int, (n + 1) % 3>;
+        using AfterW = std::integral_constant<int, (n + 2) % 3>;
+        if constexpr (!ALIGNED) {
+            if (i + 2 < stages) {
+                fetch_x(i + 2, X{});
+                fetch_w(i + 2, AfterW{});
+            }
+        }
+        read(X{}, W{}, 1);
         multiply(0);
-        read(place, 2);
+        read(X{}, W{}, 2);
         multiply(1);
-        read(place, 3);
+        read(X{}, W{}, 3);
         multiply(2);
-        meet();
-        if (i + 2 < stages) {
-            if constexpr (ALIGNED)
-                fetch(i + 2);
-            else
-                deposit(i + 2);
+        if (i + 2 < stages)    // the weights of the stage after the next may be on their way
+            meet(Ahead{});
+        else
+            meet(N0{});
+        if constexpr (ALIGNED) {
+            if (i + 2 < stages) fetch_x(i + 2, X{});
+            if (i + 3 < stages) fetch_w(i + 3, W{});
+        } else {
+            if (i + 2 < stages) deposit(X{}, AfterW{});
         }
-        read(other, 0);    // after the last stage: of what lies there, to no use
+        read(NextX{}, NextW{}, 0);    // after the last stage: of what lies there, to no use
         multiply(3);
     };
-    for (uint32_t i = 0; i < stages; i += 2) {
-        step(First{}, Second{}, i);
-        if (i + 1 < stages) step(Second{}, First{}, i + 1);
+    for (uint32_t i = 0; i < stages; i += 6) {    // the places are the same again after six
+        step(N0{}, i);
+        if (i + 1 < stages) step(N1{}, i + 1);
+        if (i + 2 < stages) step(N2{}, i + 2);
+        if (i + 3 < stages) step(std::integral_constant<int, 3>{}, i + 3);
+        if (i + 4 < stages) step(std::integral_constant<int, 4>{}, i + 4);
+        if (i + 5 < stages) step(std::integral_constant<int, 5>{}, i + 5);
     }
 
     // A lane has a row, and of each 32 columns 4 of every 8: the two halves of the wave trade theirs, so that a lane
