@@ -4,6 +4,8 @@
 // operand) or column (second) l % 32, and of the result column l % 32, rows (r & 3) + 8 (r >> 2) + 4 (l / 32), r in [0, 16).
 #include "layers_device.h"
 
+#include <type_traits>
+
 namespace pl {
 
 using Acc = float __attribute__((ext_vector_type(16)));
@@ -22,6 +24,17 @@ template <>
 __device__ __forceinline__ Acc mfma<F16>(Words4 a, Words4 b, Acc c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(HalfVec, a), __builtin_bit_cast(HalfVec, b), c, 0,
                                                   0, 0);
+}
+
+// 16 x 32 by 32 x 16: lane l holds eight neighbouring values from 8 (l / 16) on of row or column l % 16, and of the result
+// column l % 16, rows 4 (l / 16) + r.
+using Acc4 = float __attribute__((ext_vector_type(4)));
+template <class T>
+__device__ __forceinline__ Acc4 mfma16(Words4 a, Words4 b, Acc4 c) {
+    if constexpr (std::is_same_v<T, BF16>)
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(BrainVec, a), __builtin_bit_cast(BrainVec, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(HalfVec, a), __builtin_bit_cast(HalfVec, b), c, 0, 0, 0);
 }
 
 using Rsrc = __amdgpu_buffer_rsrc_t;

@@ -2,8 +2,6 @@
 // matrix: y[t] = W[r] x[t] forward, dx[t] = W[r]^T dy[t] backward, r the range of row t.
 #include "layers_mfma.h"
 
-#include <type_traits>
-
 namespace pl {
 
 constexpr uint32_t kDeep = 64;           // values along the sum in a stage
@@ -326,6 +324,129 @@ __global__ __launch_bounds__(64 * R * C, 2) void product_kernel(Product g) {
     }
 }
 
+// ---- few rows ----
+
+constexpr uint32_t kFew = 32;        // rows of a block
+constexpr uint32_t kFewCols = 16;    // columns of a block
+
+// The tile-th piece of at most kFew rows of a range, empty ranges left out.  A lane looks at eight neighbouring ranges.
+__device__ __forceinline__ Place few_of(const Product &g, uint32_t tile) {
+    constexpr uint32_t kEach = (POSEIDON_EXPERTS_MAX + 64) / 64;
+    const uint32_t lane = threadIdx.x & 63, first = lane * kEach;
+    uint32_t bounds[kEach + 1], tiles = 0;
+#pragma unroll
+    for (uint32_t i = 0; i <= kEach; ++i) bounds[i] = bound_of(g.offsets, min(first + i, g.ranges), g.rows);
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i) tiles += (max(bounds[i], bounds[i + 1]) - bounds[i] + kFew - 1) / kFew;
+    uint32_t sum = tiles;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t up = __shfl_up(sum, d, 64);
+        if ((int)lane >= d) sum += up;
+    }
+    const uint64_t after = __ballot(sum > tile);
+    Place p = {0, 0, 0, after != 0};
+    if (!p.there) return p;
+    uint32_t at = tile - (sum - tiles), range = 0, begin = 0, end = 0;
+    bool found = false;
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i) {
+        const uint32_t n = (max(bounds[i], bounds[i + 1]) - bounds[i] + kFew - 1) / kFew;
+        const bool here = !found && at < n;
+        range = here ? first + i : range;
+        begin = here ? bounds[i] + at * kFew : begin;
+        end = here ? bounds[i + 1] : end;
+        found |= here;
+        at -= found ? 0 : n;
+    }
+    const int owner = __ffsll((unsigned long long)after) - 1;
+    p.range = __builtin_amdgcn_readfirstlane(__shfl(range, owner, 64));
+    p.begin = __builtin_amdgcn_readfirstlane(__shfl(begin, owner, 64));
+    p.end = __builtin_amdgcn_readfirstlane(__shfl(end, owner, 64));
+    return p;
+}
+
+// out[t] = W x[t].  The weights' bytes bound it: they go from memory into operands, once, and a block has 16 columns alone,
+// whose sum its four waves share, 32 values at a time each, so that even one token's products are blocks for every CU.
+template <class T>
+__global__ __launch_bounds__(kBlock) void few_rows_kernel(Product g) {
+    constexpr uint32_t kTurn = 4 * 32;    // values that the waves take in a turn
+    constexpr uint32_t kAhead = 4;        // turns that are asked for at a time
+    __shared__ float sums[4][2][kFewCols][17];
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const uint32_t blocks = g.tiles_r * g.tiles_c;
+    if (blockIdx.x >= blocks) {
+        clear_outside<T>(g, blockIdx.x - blocks, gridDim.x - blocks, kBlock);
+        return;
+    }
+    const uint32_t tile = blockIdx.x / g.tiles_c, col0 = blockIdx.x % g.tiles_c * kFewCols;
+    Place at = {0, tile * kFew, g.rows, tile * kFew < g.rows};
+    if (g.offsets) at = few_of(g, tile);
+    if (!at.there) return;
+    const uint32_t here = min(at.end - at.begin, kFew), l16 = lane % 16, mine = 8 * (lane / 16);
+    using raw = typename T::raw;
+    // lanes of rows past the last read that one again
+    const raw *x0 = (const raw *)g.x + (at.begin + min(l16, here - 1)) * g.pitch;
+    const raw *x1 = (const raw *)g.x + (at.begin + min(16 + l16, here - 1)) * g.pitch;
+    const raw *w = (const raw *)g.weights + ((uint64_t)at.range * g.wide + min(col0 + l16, g.wide - 1)) * g.deep;
+    const auto words = [](const raw *p) {
+        uint32_t u[4];
+        get<false>(u, p);
+        return Words4{u[0], u[1], u[2], u[3]};
+    };
+    const auto masked = [&](const raw *row, uint32_t k) {
+        const Slice<T> u = load_words<T>(row, k, g.deep);
+        return Words4{u.w[0], u.w[1], u.w[2], u.w[3]};
+    };
+    Acc4 sum[2] = {};
+    uint32_t k = wave * 32;
+    const auto go = [&](auto two) __attribute__((always_inline)) {
+        constexpr bool kTwo = decltype(two)::value;
+        for (; k + (kAhead - 1) * kTurn + 32 <= g.deep; k += kAhead * kTurn) {
+            Words4 a[kAhead], b[kAhead], c[kAhead];
+#pragma unroll
+            for (uint32_t i = 0; i < kAhead; ++i) a[i] = words(w + k + i * kTurn + mine);
+#pragma unroll
+            for (uint32_t i = 0; i < kAhead; ++i) {
+                b[i] = words(x0 + k + i * kTurn + mine);
+                if constexpr (kTwo) c[i] = words(x1 + k + i * kTurn + mine);
+            }
+            __builtin_amdgcn_sched_barrier(0);    // all of them asked for before the first is used
+#pragma unroll
+            for (uint32_t i = 0; i < kAhead; ++i) {
+                sum[0] = mfma16<T>(a[i], b[i], sum[0]);
+                if constexpr (kTwo) sum[1] = mfma16<T>(a[i], c[i], sum[1]);
+            }
+        }
+        for (; k < g.deep; k += kTurn) {
+            const Words4 a = masked(w, k + mine);
+            sum[0] = mfma16<T>(a, masked(x0, k + mine), sum[0]);
+            if constexpr (kTwo) sum[1] = mfma16<T>(a, masked(x1, k + mine), sum[1]);
+        }
+    };
+    if (here > 16)
+        go(std::true_type{});
+    else
+        go(std::false_type{});
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sums[wave][h][mine / 2 + r][l16] = sum[h][r];    // [column][row]
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < here * kFewCols; i += kBlock) {
+        const uint32_t t = i / kFewCols, c = i % kFewCols;
+        if (col0 + c >= g.wide) continue;
+        float v = sums[0][t / 16][c][t % 16];
+#pragma unroll
+        for (int s = 1; s < 4; ++s) v += sums[s][t / 16][c][t % 16];
+        const uint64_t to = (at.begin + t) * g.out_pitch + col0 + c;
+        if (g.out_type == POSEIDON_F32)
+            ((float *)g.out)[to] = v;
+        else
+            ((raw *)g.out)[to] = T::down(v);
+    }
+}
+
 }  // namespace pl
 
 using namespace pl;
@@ -359,6 +480,20 @@ int poseidon_expert_product(const void *x, uint64_t pitch, uint32_t type, uint64
         kernel<<<(uint32_t)(r * c) + (offsets ? kClearing : 0), threads, 0, (hipStream_t)hip_stream>>>(g);
         return launched();
     };
+    // A few rows a range on average, or in all, whose weights a large tile would read no faster and whose columns would be too
+    // few large tiles (one range of 4096 x 4096: 64 rows 26 us and 33 in tiles, 128 rows 46 and 35; 64 ranges of 4096 x 2048: 64
+    // rows 140 us and 179, 256 rows 237 and 238, 512 rows 264 and 242).
+    if (!transposed && (rows <= 64 || rows <= 4ull * n_ranges)) {
+        const uint64_t r = rows < rows / kFew + n_ranges ? rows : rows / kFew + n_ranges, c = (wide + kFewCols - 1) / kFewCols;
+        g.tiles_r = (uint32_t)r;
+        g.tiles_c = (uint32_t)c;
+        const uint32_t blocks = (uint32_t)(r * c) + (offsets ? kClearing : 0);
+        if (type == POSEIDON_F16)
+            few_rows_kernel<F16><<<blocks, kBlock, 0, (hipStream_t)hip_stream>>>(g);
+        else
+            few_rows_kernel<BF16><<<blocks, kBlock, 0, (hipStream_t)hip_stream>>>(g);
+        return launched();
+    }
     const uint64_t large = tiles_for(rows, n_ranges, 256) * ((wide + 255) / 256);
     const auto pick = [&](auto t, auto turned, auto whole_) -> int {
         using T = decltype(t);
