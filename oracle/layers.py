@@ -114,3 +114,58 @@ def embed_backward(ids, dout, vocab, scale):
         if 0 <= i < vocab:
             d[i] += scale * dout[t]
     return d
+
+
+def norm_forward(x, residual, weight, eps):
+    """(out, sum, 1 / root of the mean square of each row)"""
+    h = x if residual is None else x + residual
+    rstd = 1 / np.sqrt((h * h).sum(axis=1) / h.shape[1] + eps)
+    return h * rstd[:, None] * weight, h, rstd
+
+
+def norm_backward(dout, h, rstd, weight, dsum):
+    """(dx, dweight) for the rstd that is given"""
+    n, g = h * rstd[:, None], dout * weight
+    dx = rstd[:, None] * (g - n * (n * g).sum(axis=1, keepdims=True) / h.shape[1])
+    return dx if dsum is None else dx + dsum, (dout * n).sum(axis=0)
+
+
+def expert_product(x, weights, offsets, transposed):
+    out = np.zeros((x.shape[0], weights.shape[2] if transposed else weights.shape[1]))
+    for w, a, b in zip(weights, offsets, offsets[1:]):
+        out[a:b] = x[a:b] @ (w if transposed else w.T)
+    return out
+
+
+def attention_forward(q, k, v, offsets, scale):
+    """(out [tokens, heads, dim], lse [heads, tokens]), a query at a time."""
+    n, heads, _ = q.shape
+    group = heads // k.shape[1]
+    out, lse = np.zeros(q.shape[:2] + v.shape[2:]), np.full((heads, n), -np.inf)
+    for a, b in zip(offsets, offsets[1:]):
+        for h in range(heads):
+            for i in range(a, b):
+                s = scale * (k[a:i + 1, h // group] @ q[i, h])
+                p = np.exp(s - s.max())
+                out[i, h] = p @ v[a:i + 1, h // group] / p.sum()
+                lse[h, i] = s.max() + np.log(p.sum())
+    return out, lse
+
+
+def attention_backward(dout, q, k, v, out, offsets, scale):
+    """(dq, dk, dv), a sequence and a head at a time."""
+    heads = q.shape[1]
+    group = heads // k.shape[1]
+    dq, dk, dv = np.zeros_like(q), np.zeros_like(k), np.zeros_like(v)
+    for a, b in zip(offsets, offsets[1:]):
+        later = np.triu(np.ones((b - a, b - a), bool), 1)
+        for h in range(heads):
+            j = h // group
+            s = np.where(later, -np.inf, scale * q[a:b, h] @ k[a:b, j].T)
+            p = np.exp(s - s.max(axis=1, keepdims=True)) if b > a else s
+            p /= p.sum(axis=1, keepdims=True)
+            ds = p * (dout[a:b, h] @ v[a:b, j].T - (dout[a:b, h] * out[a:b, h]).sum(axis=1, keepdims=True))
+            dq[a:b, h] = scale * ds @ k[a:b, j]
+            dk[a:b, j] += scale * ds.T @ q[a:b, h]
+            dv[a:b, j] += p.T @ dout[a:b, h]
+    return dq, dk, dv

@@ -15,7 +15,7 @@ namespace pl {
 constexpr uint32_t kTile = 64;               // keys (backward for dk and dv: queries) in LDS at a time
 constexpr int kWaves = 4;                    // of a block
 constexpr uint32_t kClearBlocks = 64;        // blocks that look for rows outside of all sequences
-constexpr float kLog2e = 1.44269504f;
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 
 // Rows [tokens][heads][dim] of a 16-bit type: where a token's and a head's values begin.
 struct Heads {
@@ -135,6 +135,16 @@ __device__ __forceinline__ Words4 piece_of(const typename T::raw *row, int s, ui
     return c < dim ? *(const Words4 *)(row + c) : Words4{};
 }
 
+// Of the scores' operand in registers: scores are kept as their products, which `scale` only stretches, so a scale below zero
+// turns this operand's signs round, and one of zero makes it zero.
+__device__ __forceinline__ Words4 directed(Words4 w, float scale) {
+    const uint32_t flip = scale < 0.0f ? 0x80008000u : 0u, keep = scale == 0.0f ? 0u : ~0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = (w[i] ^ flip) & keep;
+    return w;
+}
+__device__ __forceinline__ float stretch(float scale) { return scale == 0.0f ? kLog2e : fabsf(scale) * kLog2e; }
+
 template <class T>
 __device__ __forceinline__ Words4 packed(const float (&v)[16], int s) {
     return Words4{pair<T>(v[8 * s], v[8 * s + 1]), pair<T>(v[8 * s + 2], v[8 * s + 3]), pair<T>(v[8 * s + 4], v[8 * s + 5]),
@@ -232,7 +242,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_forward_kernel(Attent
     {
         const raw *row = row_of<T>(a.q, min(q, at.end - 1), w.head);
 #pragma unroll
-        for (int s = 0; s < D / 16; ++s) query[s] = piece_of<T>(row, s, lane, a.dim);
+        for (int s = 0; s < D / 16; ++s) query[s] = directed(piece_of<T>(row, s, lane, a.dim), a.scale);
     }
     const Loader<D, 64 * WAVES> loader(a.dim);
     const Reader<D> reader(lds, lane);
@@ -244,7 +254,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_forward_kernel(Attent
         loader.template load<T>(row_of<T>(a.v, t, w.kv), a.v.token, v_place, rows, to + kTile * D);
     };
 
-    const float c = a.scale * kLog2e;
+    const float c = stretch(a.scale);
     float m = -__builtin_inff(), total = 0.0f;
     Acc sum[D / 32] = {};
     fetch(0);
@@ -315,7 +325,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_forward_kernel(Attent
     total = sum_half(total);
     const bool there = q < at.end;
     store_turned<T, D>(sum, 1.0f / total, there ? (raw *)row_of<T>(a.out, q, w.head) : nullptr, a.dim, lane);
-    if (there && lane < 32) a.lse[(uint64_t)w.head * a.tokens + q] = m * a.scale + __logf(total);
+    if (there && lane < 32) a.lse[(uint64_t)w.head * a.tokens + q] = (m * c + __builtin_amdgcn_logf(total)) * kLn2;
 }
 
 // dq, as the forward pass goes, with delta = <dout, out> for the other kernel.  p and ds are rounded to the operands' type.
@@ -346,7 +356,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_queries_kernel(Attent
         const raw *qr = row_of<T>(a.q, mine, w.head), *dr = row_of<T>(a.dout, mine, w.head), *outr = row_of<T>(a.out, mine, w.head);
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) {
-            query[s] = piece_of<T>(qr, s, lane, a.dim);
+            query[s] = directed(piece_of<T>(qr, s, lane, a.dim), a.scale);
             dout[s] = piece_of<T>(dr, s, lane, a.dim);
             const Words4 o = piece_of<T>(outr, s, lane, a.dim);
             raw x[8], y[8];
@@ -367,7 +377,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_queries_kernel(Attent
         loader.template load<T>(row_of<T>(a.v, t, w.kv), a.v.token, v_place, rows, to + kTile * D);
     };
 
-    const float c = a.scale * kLog2e, lse = a.lse[(uint64_t)w.head * a.tokens + mine] * kLog2e;
+    const float c = stretch(a.scale), lse = a.lse[(uint64_t)w.head * a.tokens + mine] * kLog2e;
     if (there && lane < 32) {
         a.delta[(uint64_t)w.head * a.tokens + q] = delta;
         a.base[(uint64_t)w.head * a.tokens + q] = -lse;
@@ -457,7 +467,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_keys_kernel(Attention
         const raw *kr = row_of<T>(a.k, mine, kv), *vr = row_of<T>(a.v, mine, kv);
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) {
-            keys[s] = piece_of<T>(kr, s, lane, a.dim);
+            keys[s] = directed(piece_of<T>(kr, s, lane, a.dim), a.scale);
             const Words4 v = piece_of<T>(vr, s, lane, a.dim);
             if (s < kHeld)
                 vals[s] = v;
@@ -488,7 +498,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_keys_kernel(Attention
         }
     };
 
-    const float c = a.scale * kLog2e;
+    const float c = stretch(a.scale);
     Acc dk[D / 32] = {}, dv[D / 32] = {};
     const auto use = [&](auto stage, int t, uint32_t t0) {    // 32 queries
         constexpr uint32_t kSet = decltype(stage)::value, kQueries = kSet * kStage, kDout = kQueries + kTile * D;
