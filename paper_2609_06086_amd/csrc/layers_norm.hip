@@ -11,11 +11,9 @@
 namespace pl {
 
 constexpr uint32_t kNormWidth = POSEIDON_NORM_WIDTH_MAX;
-constexpr uint32_t kParts = 512;    // blocks of a backward pass, each a row of sums for dw
-
 template <uint32_t TEAM>
 struct Team {
-    static constexpr uint32_t kThreads = TEAM < kBlock ? kBlock : TEAM;
+    static constexpr uint32_t kThreads = TEAM <= 64 ? kBlock : TEAM;    // teams that meet at barriers have a block each
     static constexpr uint32_t kPerBlock = kThreads / TEAM;
     static constexpr uint32_t kWaves = TEAM < 64 ? 1 : TEAM / 64;
 };
@@ -294,30 +292,57 @@ __global__ __launch_bounds__(kBlock) void norm_join_kernel(const float *parts, u
     dweight[col] = accumulate ? dweight[col] + v : v;
 }
 
-// Runs f(team size, slices a lane) for the smallest team that holds a row.
+// Runs f(team size, slices a lane) for the smallest team that holds a row.  Forward a lane has two slices (65536 x 4096 of 16
+// bits, sum kept: 440 us, 5.5 TB/s, with one 452; 32768 x 8192 467 us and 532), but for the widths of whole blocks of one
+// (131072 x 2048: 468 us, with two in blocks of 128 lanes 511).  Backward it holds sums besides, and one slice
+// leaves room for the waves that keep memory busy (65536 x 4096: 356 us, 5.3 TB/s, with two 523).
 template <class F>
-inline void for_width(uint32_t padded, F f) {
+inline void for_width(uint32_t padded, bool two, F f) {
     using std::integral_constant;
-    const auto with = [&](auto team) {
-        if (padded <= team)
-            f(team, integral_constant<uint32_t, 1>{});
+    using One = integral_constant<uint32_t, 1>;
+    using Two = integral_constant<uint32_t, 2>;
+    if (two || padded > 1024) {
+        if (padded <= 32)
+            f(integral_constant<uint32_t, 16>{}, Two{});
+        else if (padded <= 128)
+            f(integral_constant<uint32_t, 64>{}, Two{});
+        else if (padded <= 256)
+            f(integral_constant<uint32_t, 256>{}, One{});
+        else if (padded <= 512)
+            f(integral_constant<uint32_t, 256>{}, Two{});
+        else if (padded <= 1024)
+            f(integral_constant<uint32_t, 512>{}, Two{});
         else
-            f(team, integral_constant<uint32_t, 2>{});
-    };
-    if (padded <= 32)
-        with(integral_constant<uint32_t, 16>{});
-    else if (padded <= 128)
-        with(integral_constant<uint32_t, 64>{});
-    else if (padded <= 512)
-        with(integral_constant<uint32_t, 256>{});
-    else
-        with(integral_constant<uint32_t, 1024>{});
+            f(integral_constant<uint32_t, 1024>{}, Two{});
+    } else {
+        if (padded <= 16)
+            f(integral_constant<uint32_t, 16>{}, One{});
+        else if (padded <= 32)
+            f(integral_constant<uint32_t, 32>{}, One{});
+        else if (padded <= 64)
+            f(integral_constant<uint32_t, 64>{}, One{});
+        else if (padded <= 128)
+            f(integral_constant<uint32_t, 128>{}, One{});
+        else if (padded <= 256)
+            f(integral_constant<uint32_t, 256>{}, One{});
+        else if (padded <= 512)
+            f(integral_constant<uint32_t, 512>{}, One{});
+        else
+            f(integral_constant<uint32_t, 1024>{}, One{});
+    }
 }
 
-inline uint32_t teams_per_block(uint32_t padded) { return padded <= 32 ? kBlock / 16 : padded <= 128 ? kBlock / 64 : 1; }
-inline uint32_t norm_blocks(uint64_t rows, uint32_t padded, uint32_t most) {
-    const uint64_t n = (rows + teams_per_block(padded) - 1) / teams_per_block(padded);
+// Blocks that leave each CU `threads` threads, or fewer where the rows are.
+template <uint32_t TEAM>
+inline uint32_t norm_blocks(uint64_t rows, uint32_t threads) {
+    const uint64_t n = (rows + Team<TEAM>::kPerBlock - 1) / Team<TEAM>::kPerBlock, most = 256 * threads / Team<TEAM>::kThreads;
     return (uint32_t)(n < most ? n : most);
+}
+// Backward each is a row of sums for dw besides: half as many (4096 x 4096: 32 us, with twice as many 40).
+inline uint32_t norm_parts(uint64_t rows, uint32_t padded) {
+    uint32_t n = 0;
+    for_width(padded, false, [&](auto team, auto) { n = norm_blocks<team.value>(rows, 1024); });
+    return n;
 }
 inline uint32_t norm_padded(uint64_t width) { return groups_of(width) * (kGroup / kSlice); }
 
@@ -351,16 +376,17 @@ int poseidon_norm_forward(const void *x, uint64_t x_pitch, const void *residual,
                            out_codes, sum_codes, out_scales, sum_scales};
     const uint32_t size = size_of(type);
     const uint64_t bytes = rows * width * (size * (1 + !!residual + !!out + !!sum) + keep_out + keep_sum);
-    PL_STREAM(bytes, PL_TYPE(type, for_width(padded, [&](auto team, auto n) {
-        norm_forward_kernel<T, team.value, n.value, STREAM>
-            <<<norm_blocks(rows, padded, team.value > 256 ? 512 : 2048), Team<team.value>::kThreads, 0, (hipStream_t)hip_stream>>>(a);
+    PL_STREAM(bytes, PL_TYPE(type, for_width(padded, true, [&](auto team, auto n) {
+        if constexpr (n.value == 2 || team.value == 256)
+            norm_forward_kernel<T, team.value, n.value, STREAM>
+                <<<norm_blocks<team.value>(rows, 2048), Team<team.value>::kThreads, 0, (hipStream_t)hip_stream>>>(a);
     })));
     return launched();
 }
 
 uint64_t poseidon_norm_backward_workspace(uint64_t rows, uint64_t width) {
     if (check_sizes(rows, width) != POSEIDON_OK || width > kNormWidth) return UINT64_MAX;
-    return (uint64_t)norm_blocks(rows, norm_padded(width), kParts) * width * 4;
+    return (uint64_t)norm_parts(rows, norm_padded(width)) * width * 4;
 }
 
 int poseidon_norm_backward(const void *dout, uint64_t dout_pitch, uint32_t type, uint64_t rows, uint64_t width,
@@ -381,19 +407,21 @@ int poseidon_norm_backward(const void *dout, uint64_t dout_pitch, uint32_t type,
     if (rows && (!rstd || !aligned(rstd, 4))) return POSEIDON_E_INVAL;
     if (accumulate > 1 || !aligned(dweight, 4) || (accumulate && !dweight)) return POSEIDON_E_INVAL;
     if (dweight) PL_TRY(check_workspace(workspace, workspace_bytes, poseidon_norm_backward_workspace(rows, width)));
-    const uint32_t padded = norm_padded(width), blocks = norm_blocks(rows, padded, kParts);
+    const uint32_t padded = norm_padded(width), blocks = norm_parts(rows, padded);
     if (rows) {
         const NormBackward a = {dout, sum, dsum, weight, dout_pitch, sum_pitch, dsum_pitch, dx_pitch, codes, scales, rstd,
                                 (uint32_t)rows, (uint32_t)width, padded, weight_type, dx, dweight ? (float *)workspace : nullptr};
         const uint32_t size = size_of(type);
         const uint64_t bytes = rows * width * (size * (2 + !kept + !!dsum) + kept);
-        PL_STREAM(bytes, PL_TYPE(type, for_width(padded, [&](auto team, auto n) {
-            if (kept)
-                norm_backward_kernel<T, true, team.value, n.value, STREAM>
-                    <<<blocks, Team<team.value>::kThreads, 0, (hipStream_t)hip_stream>>>(a);
-            else
-                norm_backward_kernel<T, false, team.value, n.value, STREAM>
-                    <<<blocks, Team<team.value>::kThreads, 0, (hipStream_t)hip_stream>>>(a);
+        PL_STREAM(bytes, PL_TYPE(type, for_width(padded, false, [&](auto team, auto n) {
+            if constexpr (n.value == 1 || team.value == 1024) {
+                if (kept)
+                    norm_backward_kernel<T, true, team.value, n.value, STREAM>
+                        <<<blocks, Team<team.value>::kThreads, 0, (hipStream_t)hip_stream>>>(a);
+                else
+                    norm_backward_kernel<T, false, team.value, n.value, STREAM>
+                        <<<blocks, Team<team.value>::kThreads, 0, (hipStream_t)hip_stream>>>(a);
+            }
         })));
         PL_TRY(launched());
     }

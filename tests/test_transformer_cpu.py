@@ -102,7 +102,7 @@ def test_workspaces():
     lib = L.lib()
     norm, attention = lib.poseidon_norm_backward_workspace, lib.poseidon_attention_backward_workspace
     assert norm(0, 64) == 0 and norm(1, 64) == 64 * 4 and norm(1 << 31, 64) == NONE and norm(64, 16385) == NONE
-    assert norm((1 << 31) - 1, 16384) == 512 * 16384 * 4
+    assert norm((1 << 31) - 1, 16384) == 256 * 16384 * 4
     assert attention(1 << 31, 8, 8, 64, 1) == NONE and attention(64, 8, 3, 64, 1) == NONE and attention(64, 8, 8, 136, 1) == NONE
     assert attention(0, 8, 8, 64, 1) == 0
     assert attention(1000, 8, 8, 64, 1) == 1000 * 8 * 8        # every head has keys of its own: no parts
