@@ -1,8 +1,9 @@
 """Layers of a pipeline stage on one GPU, and the planner's tables measured from them.
 
-``Embedding`` and ``ExpertBlock`` (a mixture of experts with gated activations and a residual) run a micro-batch
-forward and backward through the layer operators of ``layers.py``: between the two they keep activations in 8 bits only, and
-their weight gradients add up over the micro-batches of a step.  ``measure`` times one layer of each kind, as the
+``Embedding``, ``AttentionBlock`` (norm, causal attention over packed sequences and a residual) and ``ExpertBlock`` (a mixture of
+experts with gated activations and a residual) run a micro-batch forward and backward through the layer operators of
+``layers.py``: between the two they keep activations in 8 bits, but for what attention reads again in its own 16, and
+their weight gradients add up over the micro-batches of a step.  ``Layer`` is an attention block before an expert block.  ``measure`` times one layer of each kind, as the
 paper's profiling module does (Sec. 4.1.3; one layer per distinct type), and ``plan_problem`` makes the
 planner's tables of the times and of the bytes that S micro-batches in flight keep:
 
@@ -13,7 +14,7 @@ from __future__ import annotations
 import argparse
 import statistics
 from dataclasses import dataclass, replace
-from typing import List, Optional
+from typing import Optional
 
 import numpy as np
 import torch
@@ -25,14 +26,18 @@ from .workloads import Problem
 
 @dataclass
 class Shape:
-    """Sizes of a model: its vocabulary, width, experts (of `inner` gated values, `chosen` per token), and the tokens of a
-    micro-batch."""
+    """Sizes of a model: its vocabulary, width, experts (of `inner` gated values, `chosen` per token), the tokens of a
+    micro-batch, and with `heads` attention before the experts: its heads, the heads of its keys (0: as many) and the
+    tokens of a sequence (0: all of a micro-batch)."""
     vocab: int = 32000
     width: int = 2048
     experts: int = 16
     chosen: int = 2
     inner: int = 2048
     tokens: int = 4096
+    heads: int = 0
+    kv_heads: int = 0
+    sequence: int = 0
 
 
 class Embedding:
@@ -57,13 +62,81 @@ class Embedding:
 
 
 @dataclass
+class KeptAttention:
+    """What an AttentionBlock keeps of a micro-batch for its backward pass."""
+    offsets: Optional[torch.Tensor]
+    h: L.Stash                 # the norm's input
+    y: L.Stash                 # its output, the projections' input
+    rstd: torch.Tensor
+    both: torch.Tensor         # queries, keys and values
+    a: torch.Tensor            # attention's output
+    lse: torch.Tensor
+
+    @property
+    def kept_bytes(self) -> int:
+        plain = (self.rstd, self.both, self.a, self.lse) + (() if self.offsets is None else (self.offsets,))
+        return sum(t.numel() * t.element_size() for t in plain) + self.h.nbytes + self.y.nbytes
+
+    @property
+    def plain_bytes(self) -> int:
+        """The same with the activations in their own 16 bits."""
+        return self.kept_bytes + sum(2 * s.rows * s.width - s.nbytes for s in (self.h, self.y))
+
+
+class AttentionBlock:
+    """out = x + Wo attention(Wqkv norm(x)), causal within each of the packed sequences."""
+
+    def __init__(self, shape: Shape, device, seed: int = 0, dtype=torch.bfloat16):
+        g = torch.Generator(device=device)
+        g.manual_seed(seed)
+        d, self.heads, self.kv_heads = shape.width, shape.heads, shape.kv_heads or shape.heads
+        if not self.heads or d % self.heads:
+            raise ValueError(f"{self.heads} heads do not share a width of {d}")
+        self.dim = d // self.heads
+        self.parts = [n * self.dim for n in (self.heads, self.kv_heads, self.kv_heads)]
+
+        def weight(*size):
+            return (torch.randn(*size, generator=g, device=device) * size[-1] ** -0.5).to(dtype)
+
+        self.norm, self.wqkv, self.wo = torch.ones(d, dtype=dtype, device=device), weight(sum(self.parts), d), weight(d, d)
+        self.dnorm, self.dwqkv, self.dwo = (torch.zeros(w.shape, dtype=torch.float32, device=device)
+                                            for w in (self.norm, self.wqkv, self.wo))
+
+    @property
+    def weight_bytes(self) -> int:
+        return sum(w.numel() * (w.element_size() + 4) for w in (self.norm, self.wqkv, self.wo))
+
+    def _heads(self, both):
+        """Queries, keys and values as views of one product's rows."""
+        return [part.view(both.shape[0], -1, self.dim) for part in both.split(self.parts, dim=1)]
+
+    def forward(self, x, offsets=None):
+        y = L.poseidon_norm_forward(x, self.norm, keep_out=True, keep_sum=True)
+        both = L.poseidon_expert_product(y.out, self.wqkv)
+        a, lse = L.poseidon_attention_forward(*self._heads(both), offsets)
+        out = x + L.poseidon_expert_product(a.view(x.shape), self.wo)
+        return out, KeptAttention(offsets, y.kept_sum, y.kept_out, y.rstd, both, a, lse)
+
+    def backward(self, dout, kept: KeptAttention):
+        a = kept.a.view(dout.shape)
+        L.poseidon_weight_gradient(dout, L.poseidon_stash(a), out=self.dwo, accumulate=True)
+        da = L.poseidon_expert_product(dout, self.wo, transposed=True)
+        dboth = torch.empty_like(kept.both)
+        dq, dk, dv = self._heads(dboth)
+        L.poseidon_attention_backward(da.view(kept.a.shape), *self._heads(kept.both), kept.a, kept.lse, kept.offsets,
+                                      dq=dq, dk=dk, dv=dv)
+        L.poseidon_weight_gradient(dboth, kept.y, out=self.dwqkv, accumulate=True)
+        dy = L.poseidon_expert_product(dboth, self.wqkv, transposed=True)
+        return L.poseidon_norm_backward(dy, kept.h, kept.rstd, self.norm, dout, dweight=self.dnorm, accumulate=True)[0]
+
+
+@dataclass
 class Kept:
     """What an ExpertBlock keeps of a micro-batch for its backward pass."""
     x: torch.Tensor            # the router's input
     probs: torch.Tensor        # the chosen experts' weights
     choice: torch.Tensor
     plan: L.ExpertPlan
-    cuts: List[int]            # the experts' row ranges, on the host for the library's products
     xs: L.Stash
     gate: L.Stash
     up: L.Stash
@@ -101,42 +174,80 @@ class ExpertBlock:
     def weight_bytes(self) -> int:
         return sum(w.numel() * (w.element_size() + 4) for w in (self.router, self.w1, self.w2))
 
-    def _products(self, rows, weights, cuts, out):
-        """rows of each expert's range times its weights, [out rows] = rows @ weights[e]."""
+    @staticmethod
+    def _product(rows, weights, plan, transposed=False):
+        """rows of each expert's range times its weights; in 32 bits, which the operator does not take, by the library."""
+        if rows.dtype != torch.float32:
+            return L.poseidon_expert_product(rows, weights, plan.offsets, transposed=transposed)
+        weights = weights if transposed else weights.transpose(1, 2)
+        out, cuts = rows.new_zeros(rows.shape[0], weights.shape[2]), plan.offsets.tolist()
         for e, (a, b) in enumerate(zip(cuts, cuts[1:])):
-            if b > a:
-                torch.matmul(rows[a:b], weights[e], out=out[a:b])
+            torch.matmul(rows[a:b], weights[e], out=out[a:b])
         return out
 
     def forward(self, x):
-        d, f = x.shape[1], self.inner
+        f = self.inner
         logits, choice = torch.topk((x @ self.router.t()).float(), self.chosen, dim=1)
         probs, choice = torch.softmax(logits, 1), choice.to(torch.int32)
         plan = L.poseidon_expert_sort(choice, self.w1.shape[0])
         xs, kept_xs = L.poseidon_expert_gather(x, plan, keep=True)
-        cuts = plan.offsets.tolist()
-        both = self._products(xs, self.w1.transpose(1, 2), cuts, xs.new_empty(xs.shape[0], 2 * f))
+        both = self._product(xs, self.w1, plan)
         act, kept_gate, kept_up = L.poseidon_gated_forward(both[:, :f], both[:, f:])
-        ys = self._products(act, self.w2.transpose(1, 2), cuts, xs.new_empty(xs.shape[0], d))
+        ys = self._product(act, self.w2, plan)
         out = x + L.poseidon_expert_combine(ys, plan, probs)
-        return out, Kept(x, probs, choice, plan, cuts, kept_xs, kept_gate, kept_up, L.poseidon_stash(ys))
+        return out, Kept(x, probs, choice, plan, kept_xs, kept_gate, kept_up, L.poseidon_stash(ys))
 
     def backward(self, dout, kept: Kept):
-        f, plan, cuts = self.inner, kept.plan, kept.cuts
+        f, plan = self.inner, kept.plan
         dys, dprobs = L.poseidon_expert_combine_backward(dout, L.poseidon_restore(kept.ys), plan, kept.probs)
         act = L.poseidon_gated_forward(L.poseidon_restore(kept.gate), L.poseidon_restore(kept.up), keep=False)[0]
         L.poseidon_weight_gradient(dys, L.poseidon_stash(act), offsets=plan.offsets, out=self.dw2, accumulate=True)
-        dact = self._products(dys, self.w2, cuts, torch.empty_like(act))
+        dact = self._product(dys, self.w2, plan, transposed=True)
         dboth = act.new_empty(act.shape[0], 2 * f)
         L.poseidon_gated_backward(dact, kept.gate, kept.up, dgate=dboth[:, :f], dup=dboth[:, f:])
         L.poseidon_weight_gradient(dboth, kept.xs, offsets=plan.offsets, out=self.dw1, accumulate=True)
-        dxs = self._products(dboth, self.w1, cuts, dys.new_empty(dys.shape))
+        dxs = self._product(dboth, self.w1, plan, transposed=True)
         # the router: softmax over the chosen logits, then its product
         dlogits = kept.probs * (dprobs - (kept.probs * dprobs).sum(1, keepdim=True))
         dall = torch.zeros(kept.x.shape[0], self.router.shape[0], dtype=torch.float32, device=dout.device)
         dall.scatter_(1, kept.choice.long(), dlogits)
         self.drouter += dall.t() @ kept.x.float()
         return dout + L.poseidon_expert_combine(dxs, plan) + dall.to(dout.dtype) @ self.router
+
+
+@dataclass
+class KeptLayer:
+    """What a Layer keeps of a micro-batch: its two blocks' parts."""
+    attention: KeptAttention
+    experts: Kept
+
+    @property
+    def kept_bytes(self) -> int:
+        return self.attention.kept_bytes + self.experts.kept_bytes
+
+    @property
+    def plain_bytes(self) -> int:
+        return self.attention.plain_bytes + self.experts.plain_bytes
+
+
+class Layer:
+    """An attention block, then an expert block."""
+
+    def __init__(self, shape: Shape, device, seed: int = 0, dtype=torch.bfloat16):
+        self.attention = AttentionBlock(shape, device, seed, dtype)
+        self.experts = ExpertBlock(shape, device, seed + 1, dtype)
+
+    @property
+    def weight_bytes(self) -> int:
+        return self.attention.weight_bytes + self.experts.weight_bytes
+
+    def forward(self, x, offsets=None):
+        h, attention = self.attention.forward(x, offsets)
+        out, experts = self.experts.forward(h)
+        return out, KeptLayer(attention, experts)
+
+    def backward(self, dout, kept: KeptLayer):
+        return self.attention.backward(self.experts.backward(dout, kept.experts), kept.attention)
 
 
 @dataclass
@@ -177,15 +288,19 @@ def _work_bytes(f, device) -> int:
 
 
 def measure(shape: Shape, device=None, keep_8_bits: bool = True, repeats: int = 5):
-    """(profile of the embedding, profile of an expert block) on this GPU.  The layers run with their activations kept in 8
+    """(profile of the embedding, profile of an expert block, or with heads of a Layer) on this GPU.  The layers run with their activations kept in 8
     bits; keep_8_bits False gives those times with the bytes that 16 bits would keep."""
     device = torch.device("cuda", torch.cuda.current_device()) if device is None else device
     g = torch.Generator(device=device)
     g.manual_seed(1)
     ids = torch.randint(0, shape.vocab, (shape.tokens,), generator=g, device=device, dtype=torch.int32)
-    first, block = Embedding(shape, device), ExpertBlock(shape, device)
+    first, block = Embedding(shape, device), (Layer if shape.heads else ExpertBlock)(shape, device)
     x, _ = first.forward(ids)
-    out, kept = block.forward(x)
+    args = (x,)
+    if shape.heads and shape.sequence:
+        cuts = list(range(0, shape.tokens, shape.sequence)) + [shape.tokens]
+        args = (x, torch.tensor(cuts, dtype=torch.int32, device=device))
+    out, kept = block.forward(*args)
     dout = (torch.randn(out.shape, generator=g, device=device) * 0.01).to(out.dtype)
     dx = block.backward(dout, kept)
     first.backward(dx, ids)
@@ -196,7 +311,7 @@ def measure(shape: Shape, device=None, keep_8_bits: bool = True, repeats: int = 
                             plain_bytes, work)
 
     profiles = (profile(first, lambda: first.forward(ids), lambda: first.backward(dx, ids), ids.numel() * 4, ids.numel() * 4),
-                profile(block, lambda: block.forward(x), lambda: block.backward(dout, kept), kept.kept_bytes, kept.plain_bytes))
+                profile(block, lambda: block.forward(*args), lambda: block.backward(dout, kept), kept.kept_bytes, kept.plain_bytes))
     return profiles if keep_8_bits else tuple(p.in_16_bits() for p in profiles)
 
 
@@ -224,13 +339,17 @@ def main() -> None:
     ap.add_argument("--experts", type=int, default=16)
     ap.add_argument("--chosen", type=int, default=2)
     ap.add_argument("--inner", type=int, default=2048)
+    ap.add_argument("--heads", type=int, default=0, help="heads of attention before the experts (default: none)")
+    ap.add_argument("--kv-heads", type=int, default=0, help="heads of its keys (default: as many)")
+    ap.add_argument("--sequence", type=int, default=0, help="tokens of a sequence (default: all of a micro-batch)")
     ap.add_argument("--blocks", type=int, default=23)
     ap.add_argument("--stages", type=int, default=4)
     ap.add_argument("--micro-batches", type=int, default=32)
     ap.add_argument("--cap-mb", type=int, default=0,
                     help="memory of a device (default: 5%% above an even share, and what a pass works with)")
     a = ap.parse_args()
-    shape = Shape(width=a.width, experts=a.experts, chosen=a.chosen, inner=a.inner, tokens=a.tokens)
+    shape = Shape(width=a.width, experts=a.experts, chosen=a.chosen, inner=a.inner, tokens=a.tokens,
+                  heads=a.heads, kv_heads=a.kv_heads, sequence=a.sequence)
     first, eight = measure(shape)
     cap = a.cap_mb or int(1.05 * -(-a.blocks // a.stages) *
                           (eight.weight_bytes + min(a.stages, a.micro_batches) * eight.kept_bytes) / 1e6 +
