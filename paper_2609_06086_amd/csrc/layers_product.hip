@@ -87,7 +87,7 @@ __global__ __launch_bounds__(64 * R * C, 2) void product_kernel(Product g) {
     static_assert(kStepX % 16 == 0 && kStepW % 4 == 0);
     const uint32_t x_at = (x_row * (uint32_t)g.pitch + x_col) * 2;
     const uint32_t w_at = TURNED ? (col0 + w_col < g.wide ? (w_row * g.wide + w_col) * 2 : kNowhere) : (w_row * g.deep + w_col) * 2;
-    const uint32_t w_here = min(g.wide - col0, kCols);
+    const uint32_t w_here = min(g.wide - col0, kCols), w_safe = col0 + w_col < g.wide ? w_col : 0;
     Words4 held_x[ALIGNED ? 1 : kLoadsX], held_w[ALIGNED ? 1 : kLoadsW];
     // Ask for a stage's values; ALIGNED: right into LDS.  Past the rows, the columns and the sum come zeros.
     const auto fetch_x = [&](uint32_t stage, auto place) __attribute__((always_inline)) {
@@ -141,8 +141,8 @@ __global__ __launch_bounds__(64 * R * C, 2) void product_kernel(Product g) {
                 if constexpr (TURNED) {
                     const uint32_t k = k0 + w_row + i * kStepW;
                     const raw *row = w + (uint64_t)min(k, g.deep - 1) * g.wide;
-                    if (k0 + kDeep <= g.deep && col0 + kCols <= g.wide) {
-                        get<false>(s.w, row + w_col);
+                    if (k0 + kDeep < g.deep && g.wide >= kSlice) {    // past a row's end lies the next row: columns that nobody keeps
+                        get<false>(s.w, row + w_safe);
                     } else {
                         s = load_words<T>(row - col0, col0 + w_col, g.wide);
 #pragma unroll

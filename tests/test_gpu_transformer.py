@@ -187,7 +187,8 @@ def _product_case(rng, dev, kind, offsets, rows, o, i, transposed, out_kind=None
 
 @pytest.mark.parametrize("kind", SHORT)
 @pytest.mark.parametrize("transposed", [False, True])
-@pytest.mark.parametrize("o, i", [(1, 1), (8, 8), (7, 9), (64, 32), (65, 40), (130, 136), (200, 333), (96, 264)])
+@pytest.mark.parametrize("o, i", [(1, 1), (8, 8), (7, 9), (64, 32), (65, 40), (130, 136), (200, 333), (96, 264), (300, 5),
+                                  (5, 300), (333, 9)])
 @pytest.mark.parametrize("rows, offsets", [(1, [0, 1]), (5, [0, 0, 2, 2, 5]), (40, [3, 20, 20, 33]), (300, [0, 130, 131, 300]), (333, [7, 7, 320, 320])])
 def test_product(dev, kind, transposed, o, i, rows, offsets):
     rng = np.random.default_rng(rows + o * 7 + i)
