@@ -170,6 +170,7 @@ __global__ __launch_bounds__(64 * R * C, 2) void product_kernel(Product g) {
 
     // A wave's operands: values [16 s + 8 (lane / 32), ...) of its rows and columns.
     const uint32_t r0 = wave / C * 32 * M, c0 = wave % C * 32 * N, l32 = lane % 32, half = lane / 32;
+    const bool busy = r0 < here;    // a range's last tile may end before a wave's rows
     using Bytes = __attribute__((address_space(3))) const char *;
     const uint32_t base = (uint32_t)(uintptr_t)(Bytes)(const char *)lds;
     uint32_t x_from[4], w_from[TURNED ? N : 4];
@@ -268,12 +269,14 @@ __global__ __launch_bounds__(64 * R * C, 2) void product_kernel(Product g) {
                 fetch_w(i + 2, AfterW{});
             }
         }
-        read(X{}, W{}, 1);
-        multiply(0);
-        read(X{}, W{}, 2);
-        multiply(1);
-        read(X{}, W{}, 3);
-        multiply(2);
+        if (busy) {
+            read(X{}, W{}, 1);
+            multiply(0);
+            read(X{}, W{}, 2);
+            multiply(1);
+            read(X{}, W{}, 3);
+            multiply(2);
+        }
         if (i + 2 < stages)    // the weights of the stage after the next may be on their way
             meet(Ahead{});
         else
@@ -284,8 +287,10 @@ __global__ __launch_bounds__(64 * R * C, 2) void product_kernel(Product g) {
         } else {
             if (i + 2 < stages) deposit(X{}, AfterW{});
         }
-        read(NextX{}, NextW{}, 0);    // after the last stage: of what lies there, to no use
-        multiply(3);
+        if (busy) {
+            read(NextX{}, NextW{}, 0);    // after the last stage: of what lies there, to no use
+            multiply(3);
+        }
     };
     for (uint32_t i = 0; i < stages; i += 6) {    // the places are the same again after six
         step(N0{}, i);
