@@ -89,18 +89,29 @@ __global__ __launch_bounds__(64 * R * C, 2) void product_kernel(Product g) {
     const uint32_t w_at = TURNED ? (col0 + w_col < g.wide ? (w_row * g.wide + w_col) * 2 : kNowhere) : (w_row * g.deep + w_col) * 2;
     const uint32_t w_here = min(g.wide - col0, kCols), w_safe = col0 + w_col < g.wide ? w_col : 0;
     Words4 held_x[ALIGNED ? 1 : kLoadsX], held_w[ALIGNED ? 1 : kLoadsW];
+    // A lane's pieces as buffers of their own, which end with the tile's rows and, TURNED, with the sum: only an offset
+    // changes from stage to stage.
+    Rsrc from_x[kLoadsX], from_w[kLoadsW];
+    if constexpr (ALIGNED) {
+#pragma unroll
+        for (uint32_t i = 0; i < kLoadsX; ++i) {
+            const uint32_t left = here > i * kStepX ? min(here - i * kStepX, kStepX) : 0;
+            from_x[i] = buffer(x + i * kStepX * g.pitch, __builtin_amdgcn_readfirstlane(left * (uint32_t)g.pitch * 2));
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < kLoadsW; ++i) {
+            const uint32_t row = i * kStepW, left = TURNED ? (g.deep > row ? g.deep - row : 0) : w_here > row ? min(w_here - row, kStepW) : 0;
+            from_w[i] = buffer(w + (uint64_t)row * (TURNED ? g.wide : g.deep), __builtin_amdgcn_readfirstlane(left * (TURNED ? g.wide : g.deep) * 2));
+        }
+    }
     // Ask for a stage's values; ALIGNED: right into LDS.  Past the rows, the columns and the sum come zeros.
     const auto fetch_x = [&](uint32_t stage, auto place) __attribute__((always_inline)) {
         const uint32_t k0 = stage * kDeep;
         if constexpr (ALIGNED) {
             uint16_t *to = lds + decltype(place)::value * kX + wave * 512;
-            const uint32_t xo = k0 + x_col < g.deep ? x_at : kNowhere;
+            const uint32_t offset = k0 + x_col < g.deep ? x_at + 2 * k0 : kNowhere;
 #pragma unroll
-            for (uint32_t i = 0; i < kLoadsX; ++i) {
-                const uint32_t left = here > i * kStepX ? min(here - i * kStepX, kStepX) : 0;
-                copy_to_lds<TURNED>(buffer(x + i * kStepX * g.pitch + k0, __builtin_amdgcn_readfirstlane(left * (uint32_t)g.pitch * 2)), xo,
-                            to + i * kThreads * 8);
-            }
+            for (uint32_t i = 0; i < kLoadsX; ++i) copy_to_lds<TURNED>(from_x[i], offset, to + i * kThreads * 8);
         } else {
 #pragma unroll
             for (uint32_t i = 0; i < kLoadsX; ++i) {
@@ -118,22 +129,9 @@ __global__ __launch_bounds__(64 * R * C, 2) void product_kernel(Product g) {
         const uint32_t k0 = stage * kDeep;
         if constexpr (ALIGNED) {
             uint16_t *to = lds + kStageW + decltype(place)::value * kW + wave * 512;
-            const uint32_t wo = TURNED || k0 + w_col < g.deep ? w_at : kNowhere;
+            const uint32_t offset = TURNED ? w_at + 2 * k0 * g.wide : k0 + w_col < g.deep ? w_at + 2 * k0 : kNowhere;
 #pragma unroll
-            for (uint32_t i = 0; i < kLoadsW; ++i) {
-                uint32_t bytes;
-                const raw *from;
-                if constexpr (TURNED) {
-                    const uint32_t k = k0 + i * kStepW, left = g.deep > k ? min(g.deep - k, kStepW) : 0;
-                    from = w + (uint64_t)k * g.wide;
-                    bytes = left * g.wide * 2;
-                } else {
-                    const uint32_t left = w_here > i * kStepW ? min(w_here - i * kStepW, kStepW) : 0;
-                    from = w + (uint64_t)(i * kStepW) * g.deep + k0;
-                    bytes = left * g.deep * 2;
-                }
-                copy_to_lds<TURNED>(buffer(from, __builtin_amdgcn_readfirstlane(bytes)), wo, to + i * kThreads * 8);
-            }
+            for (uint32_t i = 0; i < kLoadsW; ++i) copy_to_lds<TURNED>(from_w[i], offset, to + i * kThreads * 8);
         } else {
 #pragma unroll
             for (uint32_t i = 0; i < kLoadsW; ++i) {
@@ -474,9 +472,10 @@ int poseidon_expert_product(const void *x, uint64_t pitch, uint32_t type, uint64
     if (rows && !aligned(offsets, 4)) return POSEIDON_E_INVAL;
     if (!rows) return POSEIDON_OK;
     Product g = {x, weights, pitch, out_pitch, (uint32_t)rows, n_ranges, (uint32_t)deep, (uint32_t)wide, offsets, 0, 0, out, out_type};
-    // 16-byte pieces that lie on 16 bytes and end with the row, at offsets of less than 2^31 bytes within a tile
+    // 16-byte pieces that lie on 16 bytes and end with the row, at offsets of less than 2^31 bytes within a tile's rows and, for
+    // W^T, within W
     const bool whole = deep % 8 == 0 && in_width % 8 == 0 && pitch % 8 == 0 && aligned(x, 16) && aligned(weights, 16) &&
-                       pitch < (1u << 21) ;
+                       pitch < (1u << 21) && (!transposed || out_width * in_width < (1u << 30));
     const auto run = [&](auto kernel, uint32_t tile_r, uint32_t tile_c, uint32_t threads) -> int {
         const uint64_t r = offsets ? tiles_for(rows, n_ranges, tile_r) : (rows + tile_r - 1) / tile_r, c = (wide + tile_c - 1) / tile_c;
         if (r * c > 0x7fffff00ull) return POSEIDON_E_RANGE;
