@@ -29,6 +29,7 @@ WIDTH_MAX, PITCH_MAX, ROWS_MAX = 1 << 20, 1 << 24, 2 ** 31 - 1
 EXPERTS_MAX, RANGES_MAX, VOCAB_MAX, TILES_MAX = 511, 65535, 2 ** 26 - 1, 1 << 22
 NORM_WIDTH_MAX, HEAD_MAX, HEADS_MAX = 16384, 128, 1024
 TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+_SHORT = (torch.float16, torch.bfloat16)
 
 _p, _u64, _u32 = C.c_void_p, C.c_uint64, C.c_uint32
 _ARGS = {
@@ -514,10 +515,10 @@ def poseidon_norm_forward(x, weight, residual=None, *, eps: float = 1e-6, keep_o
     h, residual_pitch = None, 0
     if residual is not None:
         residual, _, _, residual_pitch = _rows(residual, "poseidon_norm_forward: residual", dev, dt, (n, d))
-        h = torch.empty((n, d), dtype=dt, device=dev)
+        h = x.new_empty((n, d))
     weight = _weight(weight, "poseidon_norm_forward: weight", dev, d)
-    out, out_pitch = _out(out, "poseidon_norm_forward: out", dev, dt, n, d)
-    rstd = torch.empty(n, dtype=torch.float32, device=dev)
+    out, out_pitch = (x.new_empty((n, d)), d) if out is None else _out(out, "poseidon_norm_forward: out", dev, dt, n, d)
+    rstd = x.new_empty(n, dtype=torch.float32)
     so = Stash.empty(n, d, dt, dev) if keep_out else None
     sh = Stash.empty(n, d, dt, dev) if keep_sum else None
     _call("poseidon_norm_forward", dev, x.data_ptr(), pitch, None if residual is None else residual.data_ptr(), residual_pitch,
@@ -567,14 +568,13 @@ def poseidon_norm_backward(dout, h, rstd, weight, dsum=None, *, dx=None, dweight
 
 # ---- attention ----
 
-def _heads(x, where: str, device=None, dtype=None, shape=None):
+def _heads(x, name: str, which: str, device=None, dtype=None, shape=None):
     """Rows [tokens, heads, dim] with neighbouring values in a head (copied if the library can't take them as they are):
     (x, token pitch, head pitch)."""
-    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dim() != 3 or x.dtype not in (torch.float16, torch.bfloat16):
-        _refuse(f"{where}: not a 3-D float16 or bfloat16 tensor on the GPU")
-    if (device is not None and x.device != device) or (dtype is not None and x.dtype != dtype) or \
-            (shape is not None and x.shape != shape):
-        _refuse(f"{where}: device, type or shape differs from what the others ask for")
+    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dim() != 3 or x.dtype not in _SHORT:
+        _refuse(f"{name}: {which}: not a 3-D float16 or bfloat16 tensor on the GPU")
+    if shape is not None and (x.shape != shape or x.dtype != dtype or x.device != device):
+        _refuse(f"{name}: {which}: device, type or shape differs from what the others ask for")
     pitches = _pitches(x)
     if pitches is None:
         x = x.contiguous()
@@ -583,54 +583,53 @@ def _heads(x, where: str, device=None, dtype=None, shape=None):
             x = x.clone()
             pitches = _pitches(x)
             if pitches is None:
-                _refuse(f"{where}: heads that are no multiple of 8 wide")
-    return (x, *pitches)
+                _refuse(f"{name}: {which}: heads that are no multiple of 8 wide")
+    return x, pitches[0], pitches[1]
 
 
 def _pitches(x):
     """(token pitch, head pitch) of rows that the library takes as they are, or None."""
-    (n, h, d), (token, head, step) = x.shape, x.stride()
-    token, head = (h * d if n <= 1 else token), (d if h <= 1 else head)
-    if (step == 1 or d <= 1) and token >= d and head >= d and not (token % 8 or head % 8 or x.data_ptr() % 16) and \
-            token <= PITCH_MAX:
+    n, h, d = x.shape
+    token, head, step = x.stride()
+    if n <= 1:
+        token = h * d
+    if h <= 1:
+        head = d
+    if (step == 1 or d <= 1) and token >= d and head >= d and not ((token | head) % 8 or x.data_ptr() % 16) and token <= PITCH_MAX:
         return token, head
     return None
 
 
-def _heads_out(x, where: str, device, dtype, shape):
-    """Rows that the caller brought for a result, or new ones: (x, token pitch, head pitch)."""
+def _heads_out(x, name: str, which: str, like, shape):
+    """Rows that the caller brought for a result, or new ones, of the type of `like`: (x, token pitch, head pitch)."""
     if x is None:
-        x = torch.empty(shape, dtype=dtype, device=device)
-    elif not isinstance(x, torch.Tensor) or x.device != device or x.dtype != dtype or x.shape != shape:
-        _refuse(f"{where}: device, type or shape differs from the result's")
+        return like.new_empty(shape), shape[1] * shape[2], shape[2]
+    if not isinstance(x, torch.Tensor) or x.device != like.device or x.dtype != like.dtype or x.shape != shape:
+        _refuse(f"{name}: {which}: device, type or shape differs from the result's")
     pitches = _pitches(x)
     if pitches is None:
-        _refuse(f"{where}: layout: heads of neighbouring values on pitches that are multiples of 8, on a 16-byte boundary")
-    return (x, *pitches)
+        _refuse(f"{name}: {which}: layout: heads of neighbouring values on pitches that are multiples of 8, on a 16-byte boundary")
+    return x, pitches[0], pitches[1]
 
 
-def _attended(name: str, q, k, v, offsets, scale):
-    """The operands of an attention, looked over: ((q, pitches), (k, ...), (v, ...), offsets, sequences, scale)."""
-    q = _heads(q, f"{name}: q")
-    dev, dt, (n, h, d) = q[0].device, q[0].dtype, q[0].shape
+def _attended(name: str, q, k, v, offsets):
+    """The operands of an attention, looked over: q, k and v as _heads gives them, offsets, their address, sequences."""
+    q = _heads(q, name, "q")
+    x = q[0]
+    n, h, d = x.shape
     kv_heads = k.shape[1] if isinstance(k, torch.Tensor) and k.dim() == 3 else 0
     if not kv_heads or not d or h % kv_heads:
         _refuse(f"{name}: k: heads that do not divide the queries'")
     if d > HEAD_MAX or h > HEADS_MAX:
         raise PoseidonError(P.POSEIDON_E_RANGE, name)
-    k, v = (_heads(x, f"{name}: {w}", dev, dt, (n, kv_heads, d)) for x, w in ((k, "k"), (v, "v")))
-    sequences = 1
-    if offsets is not None:
-        offsets = _whole(offsets, f"{name}: offsets", dev, torch.int32, None)
-        if offsets.dim() != 1 or offsets.numel() < 2:
-            _refuse(f"{name}: offsets: not int32 [sequences + 1]")
-        sequences = offsets.numel() - 1
-    return q, k, v, offsets, sequences, d ** -0.5 if scale is None else scale
-
-
-def _places(*heads):
-    """(address, token pitch, head pitch) of each, in a row."""
-    return [y for x, token, head in heads for y in (x.data_ptr(), token, head)]
+    dev, dt, shape = x.device, x.dtype, (n, kv_heads, d)
+    k, v = _heads(k, name, "k", dev, dt, shape), _heads(v, name, "v", dev, dt, shape)
+    if offsets is None:
+        return q, k, v, None, None, 1
+    offsets = _whole(offsets, name, dev, torch.int32, None)
+    if offsets.dim() != 1 or offsets.numel() < 2:
+        _refuse(f"{name}: offsets: not int32 [sequences + 1]")
+    return q, k, v, offsets, offsets.data_ptr(), offsets.numel() - 1
 
 
 @_streamed
@@ -639,13 +638,14 @@ def poseidon_attention_forward(q, k, v, offsets=None, *, scale=None, out=None) -
     heads, dim], k and v [tokens, key heads, dim], each key head shared by heads / key heads neighbouring query heads;
     int32 offsets [sequences + 1] of packed sequences, without them one sequence.  scale: dim ** -0.5 if not given.
     Views of one product's rows are taken as they are."""
-    q, k, v, offsets, sequences, scale = _attended("poseidon_attention_forward", q, k, v, offsets, scale)
-    dev, dt, (n, h, d) = q[0].device, q[0].dtype, q[0].shape
-    out = _heads_out(out, "poseidon_attention_forward: out", dev, dt, (n, h, d))
-    lse = torch.empty((h, n), dtype=torch.float32, device=dev)
-    _call("poseidon_attention_forward", dev, *_places(q, k, v), TYPES[dt], n, h, k[0].shape[1], d, scale,
-          None if offsets is None else offsets.data_ptr(), sequences, *_places(out), lse.data_ptr())
-    return out[0], lse
+    name = "poseidon_attention_forward"
+    (q, qt, qh), (k, kt, kh), (v, vt, vh), offsets, at, sequences = _attended(name, q, k, v, offsets)
+    n, h, d = shape = q.shape
+    out, ot, oh = _heads_out(out, name, "out", q, shape)
+    lse = q.new_empty((h, n), dtype=torch.float32)
+    _call(name, q.device, q.data_ptr(), qt, qh, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, TYPES[q.dtype], n, h, k.shape[1], d,
+          d ** -0.5 if scale is None else scale, at, sequences, out.data_ptr(), ot, oh, lse.data_ptr())
+    return out, lse
 
 
 @_streamed
@@ -653,14 +653,17 @@ def poseidon_attention_backward(dout, q, k, v, out, lse, offsets=None, *, scale=
                                 dv=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """(dq, dk, dv) of poseidon_attention_forward, from its arguments and its results."""
     name = "poseidon_attention_backward"
-    q, k, v, offsets, sequences, scale = _attended(name, q, k, v, offsets, scale)
-    dev, dt, shape, kv_shape = q[0].device, q[0].dtype, q[0].shape, k[0].shape
+    (q, qt, qh), (k, kt, kh), (v, vt, vh), offsets, cuts, sequences = _attended(name, q, k, v, offsets)
+    dev, dt, shape, kv_shape = q.device, q.dtype, q.shape, k.shape
     n, h, d = shape
-    dout, out = (_heads(x, f"{name}: {w}", dev, dt, shape) for x, w in ((dout, "dout"), (out, "out")))
+    dout, gt, gh = _heads(dout, name, "dout", dev, dt, shape)
+    out, ot, oh = _heads(out, name, "out", dev, dt, shape)
     lse = _whole(lse, f"{name}: lse", dev, torch.float32, (h, n))
-    dq = _heads_out(dq, f"{name}: dq", dev, dt, shape)
-    dk, dv = (_heads_out(x, f"{name}: {w}", dev, dt, kv_shape) for x, w in ((dk, "dk"), (dv, "dv")))
+    dq, dqt, dqh = _heads_out(dq, name, "dq", q, shape)
+    dk, dkt, dkh = _heads_out(dk, name, "dk", q, kv_shape)
+    dv, dvt, dvh = _heads_out(dv, name, "dv", q, kv_shape)
     w, at, size = _workspace(name, dev, n, h, kv_shape[1], d, sequences)
-    _call(name, dev, *_places(dout, q, k, v, out), lse.data_ptr(), TYPES[dt], n, h, kv_shape[1], d, scale,
-          None if offsets is None else offsets.data_ptr(), sequences, *_places(dq, dk, dv), at, size)
-    return dq[0], dk[0], dv[0]
+    _call(name, dev, dout.data_ptr(), gt, gh, q.data_ptr(), qt, qh, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, out.data_ptr(), ot, oh,
+          lse.data_ptr(), TYPES[dt], n, h, kv_shape[1], d, d ** -0.5 if scale is None else scale, cuts, sequences,
+          dq.data_ptr(), dqt, dqh, dk.data_ptr(), dkt, dkh, dv.data_ptr(), dvt, dvh, at, size)
+    return dq, dk, dv
