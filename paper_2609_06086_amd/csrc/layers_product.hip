@@ -502,7 +502,9 @@ int poseidon_expert_product(const void *x, uint64_t pitch, uint32_t type, uint64
     const auto pick = [&](auto t, auto turned, auto whole_) -> int {
         using T = decltype(t);
         constexpr bool kTurned = decltype(turned)::value, kWhole = decltype(whole_)::value;
-        return large >= 256 ? run(product_kernel<T, kTurned, kWhole, 2, 4, 4, 2>, 256, 256, 512)
+        // 256 x 256 tiles, one a CU, where most CUs get one (one range of 3000 x 3000, 4096 rows, 204 tiles: 89 us, in 128 x 128 120;
+        // 6000 rows of 2048 x 2048, 192: 57 and 60; 5120 rows, 168: 59 and 56).
+        return large >= 180 ? run(product_kernel<T, kTurned, kWhole, 2, 4, 4, 2>, 256, 256, 512)
                             : run(product_kernel<T, kTurned, kWhole, 2, 2, 2, 2>, 128, 128, 256);
     };
     const auto of = [&](auto t) -> int {

@@ -230,6 +230,28 @@ def test_product_of_many_ranges_and_of_one_matrix(dev):
     assert (wide[:, :3] == 7).all() and (wide[:, 75:] == 7).all()
 
 
+def test_offsets_outside_of_the_rows(dev):
+    """Bounds are cut to the rows that there are, and offsets that descend touch nothing else."""
+    rng = np.random.default_rng(18)
+    x, w = _make(rng, (40, 64), "bf16", dev), _make(rng, (2 * 300, 64), "bf16", dev).contiguous().view(2, 300, 64)
+    big = _make(rng, (400, 64), "bf16", dev)
+    q, k, v, dout = _attention_case(rng, dev, "bf16", 40, 2, 1, 64)
+    for given, cut in (([-5, 20, 1000], [0, 20, 40]), ([-2 ** 31, -1, 2 ** 31 - 1], [0, 0, 40]), ([2 ** 31 - 1] * 3, [40, 40, 40])):
+        at, inside = (torch.tensor(o, dtype=torch.int32, device=dev) for o in (given, cut))
+        _same(L.poseidon_expert_product(x, w, at), L.poseidon_expert_product(x, w, inside))
+        _same(L.poseidon_expert_product(big, w, at), L.poseidon_expert_product(big, w, torch.tensor([min(max(o, 0), 400) for o in given], dtype=torch.int32, device=dev)))
+        out, lse = L.poseidon_attention_forward(q, k, v, at)
+        want = L.poseidon_attention_forward(q, k, v, inside)
+        _same(out, want[0])
+        _same(lse, want[1])
+        for a, b in zip(L.poseidon_attention_backward(dout, q, k, v, out, lse, at), L.poseidon_attention_backward(dout, q, k, v, out, lse, inside)):
+            _same(a, b)
+    down = torch.tensor([30, 10, 35], dtype=torch.int32, device=dev)
+    assert L.poseidon_expert_product(x, w, down).shape == (40, 300)
+    assert L.poseidon_attention_forward(q, k, v, down)[0].shape == q.shape
+    torch.cuda.synchronize()
+
+
 def test_product_keeps_infinities_in_their_rows(dev):
     """Rows past a range and values past a row never reach a result, whatever they hold."""
     rng = np.random.default_rng(6)
