@@ -50,9 +50,6 @@ __device__ __forceinline__ uint2 read_turned(__attribute__((address_space(3))) c
     using Four = short __attribute__((ext_vector_type(4)));
     return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) Four *)lds));
 }
-__device__ __forceinline__ uint2 read_turned(const uint16_t *lds) {
-    return read_turned((__attribute__((address_space(3))) const void *)lds);
-}
 
 // 16 bytes a lane from a buffer to LDS, at `to` + 16 lane; an offset past the buffer's end brings zeros.  Before a turned read
 // the compiler waits for every such load that it knows of, though it may be meant for another stage.  OWN loads are instructions that it
@@ -78,7 +75,7 @@ __device__ __forceinline__ uint32_t pair(float lo, float hi) {
 }
 
 // How the compiler is to mix what a block of code does: first N of a kind, and so on, in the order of the calls.
-constexpr int kMatrix = 0x8, kAlu = 0x402, kReadLds = 0x100;
+constexpr int kMatrix = 0x8, kReadLds = 0x100;
 template <int KIND, int N>
 __device__ __forceinline__ void then() {
     __builtin_amdgcn_sched_group_barrier(KIND, N, 0);

@@ -54,6 +54,11 @@ __device__ __forceinline__ void clear_outside(const Product &g, uint32_t block, 
 // LDS holds two stages of 64 values along the sum, 128 bytes of a row.  The last of a stage's operands are in registers when
 // a quarter of its products is still to come: there the waves meet, the stage's place is given to the one after the
 // next, and the next one's first operands are read beside the last products, so that no wave waits for LDS at a stage's start.
+//
+// The matrix units bound it, at the clock that their power leaves: 16384 rows of 8192 values by 4096 x 8192 take 862 us
+// (1275 TFLOP/s), W^T of 8192 x 4096 1030 us (1068; units busy for 49 % of the time at 1.72 GHz), 64 ragged ranges of 65536 rows by
+// 4096 x 2048 1150 us (956; 50 %, 1.66 GHz); no bank conflicts.  Stages of 32 values with four places: the ragged ranges
+// 1530 us where those of 64 took 1347.
 template <class T, bool TURNED, bool ALIGNED, int R, int C, int M, int N>
 __global__ __launch_bounds__(64 * R * C, 2) void product_kernel(Product g) {
     constexpr uint32_t kRows = 32 * R * M, kCols = 32 * C * N, kThreads = 64 * R * C;
@@ -370,11 +375,15 @@ __device__ __forceinline__ Place few_of(const Product &g, uint32_t tile) {
 }
 
 // out[t] = W x[t].  The weights' bytes bound it: they go from memory into operands, once, and a block has 16 columns alone,
-// whose sum its four waves share, 32 values at a time each, so that even one token's products are blocks for every CU.
+// whose sum its four waves share, so that even one token's products are blocks for every CU.  A lane takes 16
+// neighbouring values, so that one wave asks for whole lines (16 rows by 8192 x 8192: 33 us, with 8 neighbouring ones 39).
+// One token's 8 ranges of 4096 x 2048, 134 MB of weights: 29 us, 4.6 TB/s; 512
+// rows of 64 such ranges 218 us, 4.9 TB/s.  Eight turns ahead in place of four, or loads
+// marked as read once: no faster, and 3.5 TB/s.
 template <class T>
 __global__ __launch_bounds__(kBlock) void few_rows_kernel(Product g) {
-    constexpr uint32_t kTurn = 4 * 32;    // values that the waves take in a turn
-    constexpr uint32_t kAhead = 4;        // turns that are asked for at a time
+    constexpr uint32_t kEach = 64, kTurn = 4 * kEach;    // values that a wave and the block take in a turn
+    constexpr uint32_t kAhead = 2;                           // turns that are asked for at a time
     __shared__ float sums[4][2][kFewCols][17];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint32_t blocks = g.tiles_r * g.tiles_c;
@@ -386,7 +395,7 @@ __global__ __launch_bounds__(kBlock) void few_rows_kernel(Product g) {
     Place at = {0, tile * kFew, g.rows, tile * kFew < g.rows};
     if (g.offsets) at = few_of(g, tile);
     if (!at.there) return;
-    const uint32_t here = min(at.end - at.begin, kFew), l16 = lane % 16, mine = 8 * (lane / 16);
+    const uint32_t here = min(at.end - at.begin, kFew), l16 = lane % 16, mine = 16 * (lane / 16);
     using raw = typename T::raw;
     // lanes of rows past the last read that one again
     const raw *x0 = (const raw *)g.x + (at.begin + min(l16, here - 1)) * g.pitch;
@@ -402,30 +411,38 @@ __global__ __launch_bounds__(kBlock) void few_rows_kernel(Product g) {
         return Words4{u.w[0], u.w[1], u.w[2], u.w[3]};
     };
     Acc4 sum[2] = {};
-    uint32_t k = wave * 32;
+    uint32_t k = wave * kEach;
     const auto go = [&](auto two) __attribute__((always_inline)) {
         constexpr bool kTwo = decltype(two)::value;
-        for (; k + (kAhead - 1) * kTurn + 32 <= g.deep; k += kAhead * kTurn) {
-            Words4 a[kAhead], b[kAhead], c[kAhead];
+        for (; k + (kAhead - 1) * kTurn + kEach <= g.deep; k += kAhead * kTurn) {
+            Words4 a[kAhead][2], b[kAhead][2], c[kAhead][2];
 #pragma unroll
-            for (uint32_t i = 0; i < kAhead; ++i) a[i] = words(w + k + i * kTurn + mine);
+            for (uint32_t i = 0; i < kAhead; ++i)
 #pragma unroll
-            for (uint32_t i = 0; i < kAhead; ++i) {
-                b[i] = words(x0 + k + i * kTurn + mine);
-                if constexpr (kTwo) c[i] = words(x1 + k + i * kTurn + mine);
-            }
+                for (uint32_t j = 0; j < 2; ++j) a[i][j] = words(w + k + i * kTurn + mine + 8 * j);
+#pragma unroll
+            for (uint32_t i = 0; i < kAhead; ++i)
+#pragma unroll
+                for (uint32_t j = 0; j < 2; ++j) {
+                    b[i][j] = words(x0 + k + i * kTurn + mine + 8 * j);
+                    if constexpr (kTwo) c[i][j] = words(x1 + k + i * kTurn + mine + 8 * j);
+                }
             __builtin_amdgcn_sched_barrier(0);    // all of them asked for before the first is used
 #pragma unroll
-            for (uint32_t i = 0; i < kAhead; ++i) {
-                sum[0] = mfma16<T>(a[i], b[i], sum[0]);
-                if constexpr (kTwo) sum[1] = mfma16<T>(a[i], c[i], sum[1]);
+            for (uint32_t i = 0; i < kAhead; ++i)
+#pragma unroll
+                for (uint32_t j = 0; j < 2; ++j) {
+                    sum[0] = mfma16<T>(a[i][j], b[i][j], sum[0]);
+                    if constexpr (kTwo) sum[1] = mfma16<T>(a[i][j], c[i][j], sum[1]);
+                }
+        }
+        for (; k < g.deep; k += kTurn)
+#pragma unroll
+            for (uint32_t j = 0; j < 2; ++j) {
+                const Words4 a = masked(w, k + mine + 8 * j);
+                sum[0] = mfma16<T>(a, masked(x0, k + mine + 8 * j), sum[0]);
+                if constexpr (kTwo) sum[1] = mfma16<T>(a, masked(x1, k + mine + 8 * j), sum[1]);
             }
-        }
-        for (; k < g.deep; k += kTurn) {
-            const Words4 a = masked(w, k + mine);
-            sum[0] = mfma16<T>(a, masked(x0, k + mine), sum[0]);
-            if constexpr (kTwo) sum[1] = mfma16<T>(a, masked(x1, k + mine), sum[1]);
-        }
     };
     if (here > 16)
         go(std::true_type{});
@@ -434,7 +451,7 @@ __global__ __launch_bounds__(kBlock) void few_rows_kernel(Product g) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) sums[wave][h][mine / 2 + r][l16] = sum[h][r];    // [column][row]
+        for (int r = 0; r < 4; ++r) sums[wave][h][mine / 4 + r][l16] = sum[h][r];    // [column][row]
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < here * kFewCols; i += kBlock) {
         const uint32_t t = i / kFewCols, c = i % kFewCols;
@@ -485,9 +502,9 @@ int poseidon_expert_product(const void *x, uint64_t pitch, uint32_t type, uint64
         return launched();
     };
     // A few rows a range on average, or in all, whose weights a large tile would read no faster and whose columns would be too
-    // few large tiles (one range of 4096 x 4096: 64 rows 26 us and 33 in tiles, 128 rows 46 and 35; 64 ranges of 4096 x 2048: 64
-    // rows 140 us and 179, 256 rows 237 and 238, 512 rows 264 and 242).
-    if (!transposed && (rows <= 64 || rows <= 4ull * n_ranges)) {
+    // few large tiles (one range of 4096 x 4096: 64 rows 24 us and 33 in tiles, 96 rows 35 and 33; 64 ranges of 4096 x 2048: 384
+    // rows 211 us and 227, 512 rows 218 and 228, 768 rows 245 and 235; 16 of 1001 x 1365: 128 rows 24 us and 28, 256 34 and 28).
+    if (!transposed && (rows <= 64 || rows <= 8ull * n_ranges)) {
         const uint64_t r = rows < rows / kFew + n_ranges ? rows : rows / kFew + n_ranges, c = (wide + kFewCols - 1) / kFewCols;
         g.tiles_r = (uint32_t)r;
         g.tiles_c = (uint32_t)c;
