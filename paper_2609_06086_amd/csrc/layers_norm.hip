@@ -4,6 +4,8 @@
 //
 // A team of lanes holds a row in registers, so every operand is read once; memory bounds both directions.  Teams stay for
 // many rows: they read the weights once, and the backward pass holds its sums for dw in registers until its last row.
+// Widths of whole pieces of 16 bytes run at 4.5 to 5.8 TB/s forward and backward up to 8192 values, where a copy of 1 GiB reaches 6.2,
+// wider ones at 3.3 to 5.2 (two slices a lane backward do not fit the registers), odd ones at 3.3 to 4.1.
 #include "layers_device.h"
 
 #include <type_traits>
@@ -11,28 +13,37 @@
 namespace pl {
 
 constexpr uint32_t kNormWidth = POSEIDON_NORM_WIDTH_MAX;
+constexpr uint32_t kWhole = 0;    // a team of as many waves as its block has, which meet at barriers
 template <uint32_t TEAM>
 struct Team {
-    static constexpr uint32_t kThreads = TEAM <= 64 ? kBlock : TEAM;    // teams that meet at barriers have a block each
-    static constexpr uint32_t kPerBlock = kThreads / TEAM;
-    static constexpr uint32_t kWaves = TEAM < 64 ? 1 : TEAM / 64;
+    static constexpr uint32_t kPerBlock = TEAM == kWhole ? 1 : kBlock / TEAM;
+    static constexpr uint32_t kMost = TEAM == kWhole ? 1024 : kBlock;    // threads of a block
+    static constexpr uint32_t kSlots = TEAM == kWhole ? 16 : 1;          // one for each wave that may meet
+    static __device__ __forceinline__ uint32_t size() { return TEAM == kWhole ? blockDim.x : TEAM; }
 };
+
+// Waves that a SIMD has at a time: what their registers allow.  Backward from 8 bits six of them would leave registers in
+// memory (32768 x 8192: 528 us, with five 380).
+template <uint32_t N>
+constexpr uint32_t kForwardWaves = N == 1 ? 8 : 4;
+template <uint32_t TEAM, uint32_t N, bool KEPT>
+constexpr uint32_t kBackwardWaves = N == 2 ? 4 : TEAM == kWhole && !KEPT ? 6 : 5;
 
 __device__ __forceinline__ float add(float a, float b) { return a + b; }
 __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return max(a, b); }
 
-// `op` over the lanes of a team, in one order; `slots`: one word a wave, not in use by an earlier call that a wave may
-// still read.
+// `op` over the lanes of a team, in one order; `slots`: a word for each wave, 0 past the team's (which `op` leaves alone), not in use
+// by an earlier call that a wave may still read.
 template <uint32_t TEAM, class V, class F>
 __device__ __forceinline__ V over_team(V v, F op, V *slots) {
 #pragma unroll
-    for (uint32_t d = (TEAM < 64 ? TEAM : 64) / 2; d; d >>= 1) v = op(v, __shfl_xor(v, (int)d, 64));
-    if constexpr (TEAM > 64) {
+    for (uint32_t d = (TEAM == kWhole ? 64 : TEAM) / 2; d; d >>= 1) v = op(v, __shfl_xor(v, (int)d, 64));
+    if constexpr (TEAM == kWhole) {
         if ((threadIdx.x & 63) == 0) slots[threadIdx.x / 64] = v;
         __syncthreads();
         v = slots[0];
 #pragma unroll
-        for (uint32_t w = 1; w < Team<TEAM>::kWaves; ++w) v = op(v, slots[w]);
+        for (uint32_t w = 1; w < Team<TEAM>::kSlots; ++w) v = op(v, slots[w]);
     }
     return v;
 }
@@ -103,26 +114,30 @@ __device__ __forceinline__ float far_rstd(const float (&h)[N][8], float size, fl
 }
 
 template <class T, uint32_t TEAM, uint32_t N, bool STREAM>
-__global__ __launch_bounds__(Team<TEAM>::kThreads) void norm_forward_kernel(NormForward a) {
-    __shared__ float sums[3][Team<TEAM>::kWaves];
-    __shared__ uint32_t most[Team<TEAM>::kWaves];
-    const uint32_t lane = threadIdx.x % TEAM;
-    const uint32_t first = blockIdx.x * Team<TEAM>::kPerBlock + threadIdx.x / TEAM, step = gridDim.x * Team<TEAM>::kPerBlock;
+__global__ __launch_bounds__(Team<TEAM>::kMost, kForwardWaves<N>) void norm_forward_kernel(NormForward a) {
+    __shared__ __attribute__((aligned(16))) float sums[3][Team<TEAM>::kSlots];
+    __shared__ __attribute__((aligned(16))) uint32_t most[Team<TEAM>::kSlots];
+    const uint32_t lanes = Team<TEAM>::size(), lane = TEAM == kWhole ? threadIdx.x : threadIdx.x % TEAM;
+    const uint32_t first = blockIdx.x * Team<TEAM>::kPerBlock + (TEAM == kWhole ? 0 : threadIdx.x / lanes), step = gridDim.x * Team<TEAM>::kPerBlock;
+    if constexpr (TEAM == kWhole) {
+        if (threadIdx.x < 16) sums[0][threadIdx.x] = sums[1][threadIdx.x] = sums[2][threadIdx.x] = 0.0f, most[threadIdx.x] = 0;
+        __syncthreads();
+    }
     const float size = (float)a.width;
     float w[N][8];
 #pragma unroll
-    for (uint32_t j = 0; j < N; ++j) load_weight(a.weight, a.weight_type, (lane + j * TEAM) * kSlice, a.width, w[j]);
+    for (uint32_t j = 0; j < N; ++j) load_weight(a.weight, a.weight_type, (lane + j * lanes) * kSlice, a.width, w[j]);
     uint32_t turn = 0;
     for (uint64_t row = first; row < a.rows; row += step, turn ^= 1) {
         const typename T::raw *x = (const typename T::raw *)a.x + row * a.x_pitch;
         float h[N][8];
         Slice<T> in[N], more[N];
 #pragma unroll
-        for (uint32_t j = 0; j < N; ++j) in[j] = load_words<T, STREAM>(x, (lane + j * TEAM) * kSlice, a.width);
+        for (uint32_t j = 0; j < N; ++j) in[j] = load_words<T, STREAM>(x, (lane + j * lanes) * kSlice, a.width);
         if (a.residual) {
             const typename T::raw *r = (const typename T::raw *)a.residual + row * a.residual_pitch;
 #pragma unroll
-            for (uint32_t j = 0; j < N; ++j) more[j] = load_words<T, STREAM>(r, (lane + j * TEAM) * kSlice, a.width);
+            for (uint32_t j = 0; j < N; ++j) more[j] = load_words<T, STREAM>(r, (lane + j * lanes) * kSlice, a.width);
         }
 #pragma unroll
         for (uint32_t j = 0; j < N; ++j) values<T>(in[j], h[j]);
@@ -147,14 +162,14 @@ __global__ __launch_bounds__(Team<TEAM>::kThreads) void norm_forward_kernel(Norm
         if (a.sum) {
 #pragma unroll
             for (uint32_t j = 0; j < N; ++j)
-                store_slice<T, STREAM>((typename T::raw *)a.sum + row * a.sum_pitch, (lane + j * TEAM) * kSlice, a.width, h[j]);
+                store_slice<T, STREAM>((typename T::raw *)a.sum + row * a.sum_pitch, (lane + j * lanes) * kSlice, a.width, h[j]);
         }
         if (a.sum_codes) {
 #pragma unroll
             for (uint32_t j = 0; j < N; ++j) {
                 float v[8];
                 as_written<T>(h[j], v);
-                keep_slice<T, STREAM>(v, row, lane + j * TEAM, a.padded, a.sum_codes, a.sum_scales);
+                keep_slice<T, STREAM>(v, row, lane + j * lanes, a.padded, a.sum_codes, a.sum_scales);
             }
         }
 #pragma unroll
@@ -164,14 +179,14 @@ __global__ __launch_bounds__(Team<TEAM>::kThreads) void norm_forward_kernel(Norm
         if (a.out) {
 #pragma unroll
             for (uint32_t j = 0; j < N; ++j)
-                store_slice<T, STREAM>((typename T::raw *)a.out + row * a.out_pitch, (lane + j * TEAM) * kSlice, a.width, h[j]);
+                store_slice<T, STREAM>((typename T::raw *)a.out + row * a.out_pitch, (lane + j * lanes) * kSlice, a.width, h[j]);
         }
         if (a.out_codes) {
 #pragma unroll
             for (uint32_t j = 0; j < N; ++j) {
                 float v[8];
                 as_written<T>(h[j], v);
-                keep_slice<T, STREAM>(v, row, lane + j * TEAM, a.padded, a.out_codes, a.out_scales);
+                keep_slice<T, STREAM>(v, row, lane + j * lanes, a.padded, a.out_codes, a.out_scales);
             }
         }
     }
@@ -189,14 +204,18 @@ struct NormBackward {
 };
 
 template <class T, bool KEPT, uint32_t TEAM, uint32_t N, bool STREAM>
-__global__ __launch_bounds__(Team<TEAM>::kThreads) void norm_backward_kernel(NormBackward a) {
-    __shared__ float sums[2][Team<TEAM>::kWaves];
-    const uint32_t lane = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
-    const uint32_t first = blockIdx.x * Team<TEAM>::kPerBlock + team, step = gridDim.x * Team<TEAM>::kPerBlock;
+__global__ __launch_bounds__(Team<TEAM>::kMost, (kBackwardWaves<TEAM, N, KEPT>)) void norm_backward_kernel(NormBackward a) {
+    __shared__ __attribute__((aligned(16))) float sums[2][Team<TEAM>::kSlots];
+    const uint32_t lanes = Team<TEAM>::size(), lane = TEAM == kWhole ? threadIdx.x : threadIdx.x % TEAM;
+    if constexpr (TEAM == kWhole) {
+        if (threadIdx.x < 16) sums[0][threadIdx.x] = sums[1][threadIdx.x] = 0.0f;
+        __syncthreads();
+    }
+    const uint32_t team = TEAM == kWhole ? 0 : threadIdx.x / lanes, first = blockIdx.x * Team<TEAM>::kPerBlock + team, step = gridDim.x * Team<TEAM>::kPerBlock;
     const float size = (float)a.width;
     float w[N][8], dw[N][8] = {};
 #pragma unroll
-    for (uint32_t j = 0; j < N; ++j) load_weight(a.weight, a.weight_type, (lane + j * TEAM) * kSlice, a.width, w[j]);
+    for (uint32_t j = 0; j < N; ++j) load_weight(a.weight, a.weight_type, (lane + j * lanes) * kSlice, a.width, w[j]);
     uint32_t turn = 0;
     for (uint64_t row = first; row < a.rows; row += step, turn ^= 1) {
         const typename T::raw *dout = (const typename T::raw *)a.dout + row * a.dout_pitch;
@@ -204,10 +223,10 @@ __global__ __launch_bounds__(Team<TEAM>::kThreads) void norm_backward_kernel(Nor
         uint32_t code[N][2];
         float scale[N];
 #pragma unroll
-        for (uint32_t j = 0; j < N; ++j) in[j] = load_words<T, STREAM>(dout, (lane + j * TEAM) * kSlice, a.width);
+        for (uint32_t j = 0; j < N; ++j) in[j] = load_words<T, STREAM>(dout, (lane + j * lanes) * kSlice, a.width);
 #pragma unroll
         for (uint32_t j = 0; j < N; ++j) {
-            const uint32_t s = lane + j * TEAM;
+            const uint32_t s = lane + j * lanes;
             if constexpr (KEPT) {
                 const uint64_t i = row * a.padded + (s < a.padded ? s : 0);
                 load_codes<STREAM>(a.codes, i, code[j]);
@@ -219,7 +238,7 @@ __global__ __launch_bounds__(Team<TEAM>::kThreads) void norm_backward_kernel(Nor
         if (a.dsum) {
             const typename T::raw *d = (const typename T::raw *)a.dsum + row * a.dsum_pitch;
 #pragma unroll
-            for (uint32_t j = 0; j < N; ++j) more[j] = load_words<T, STREAM>(d, (lane + j * TEAM) * kSlice, a.width);
+            for (uint32_t j = 0; j < N; ++j) more[j] = load_words<T, STREAM>(d, (lane + j * lanes) * kSlice, a.width);
         }
         const float rstd = a.rstd[row];
         float g[N][8], n[N][8], dot = 0.0f;
@@ -227,13 +246,12 @@ __global__ __launch_bounds__(Team<TEAM>::kThreads) void norm_backward_kernel(Nor
         for (uint32_t j = 0; j < N; ++j) {
             values<T>(in[j], g[j]);
             if constexpr (KEPT)
-                values_of(code[j], lane + j * TEAM < a.padded ? scale[j] : 0.0f, n[j]);
+                values_of(code[j], lane + j * lanes < a.padded ? scale[j] : 0.0f, n[j]);
             else
                 values<T>(at[j], n[j]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                // past the row nothing counts, whatever its last group holds
-                n[j][i] = (lane + j * TEAM) * kSlice + i < a.width ? n[j][i] * rstd : 0.0f;
+            for (int i = 0; i < 8; ++i) {    // past the row dout counts as 0
+                n[j][i] *= rstd;
                 dw[j][i] = fmaf(g[j][i], n[j][i], dw[j][i]);
                 g[j][i] *= w[j][i];
                 dot = fmaf(g[j][i], n[j][i], dot);
@@ -246,7 +264,7 @@ __global__ __launch_bounds__(Team<TEAM>::kThreads) void norm_backward_kernel(Nor
             if (a.dsum) values<T>(more[j], d);
 #pragma unroll
             for (int i = 0; i < 8; ++i) d[i] = fmaf(rstd, fmaf(-dot, n[j][i], g[j][i]), d[i]);
-            store_slice<T, STREAM>((typename T::raw *)a.dx + row * a.dx_pitch, (lane + j * TEAM) * kSlice, a.width, d);
+            store_slice<T, STREAM>((typename T::raw *)a.dx + row * a.dx_pitch, (lane + j * lanes) * kSlice, a.width, d);
         }
     }
     if (!a.parts) return;
@@ -256,9 +274,9 @@ __global__ __launch_bounds__(Team<TEAM>::kThreads) void norm_backward_kernel(Nor
 #pragma unroll
         for (uint32_t j = 0; j < N; ++j)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) all[team][(lane + j * TEAM) * kSlice + i] = dw[j][i];
+            for (int i = 0; i < 8; ++i) all[team][(lane + j * lanes) * kSlice + i] = dw[j][i];
         __syncthreads();
-        for (uint32_t c = threadIdx.x; c < a.width; c += Team<TEAM>::kThreads) {
+        for (uint32_t c = threadIdx.x; c < a.width; c += kBlock) {
             float v = 0.0f;
 #pragma unroll
             for (uint32_t t = 0; t < Team<TEAM>::kPerBlock; ++t) v += all[t][c];
@@ -269,7 +287,7 @@ __global__ __launch_bounds__(Team<TEAM>::kThreads) void norm_backward_kernel(Nor
         for (uint32_t j = 0; j < N; ++j)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const uint32_t c = (lane + j * TEAM) * kSlice + i;
+                const uint32_t c = (lane + j * lanes) * kSlice + i;
                 if (c < a.width) part[c] = dw[j][i];
             }
     }
@@ -292,57 +310,54 @@ __global__ __launch_bounds__(kBlock) void norm_join_kernel(const float *parts, u
     dweight[col] = accumulate ? dweight[col] + v : v;
 }
 
-// Runs f(team size, slices a lane) for the smallest team that holds a row.  Forward a lane has two slices (65536 x 4096 of 16
-// bits, sum kept: 440 us, 5.5 TB/s, with one 452; 32768 x 8192 467 us and 532), but for the widths of whole blocks of one
-// (131072 x 2048: 468 us, with two in blocks of 128 lanes 511).  Backward it holds sums besides, and one slice
-// leaves room for the waves that keep memory busy (65536 x 4096: 356 us, 5.3 TB/s, with two 523).
+// Runs f(team size, slices a lane, threads of a block) for the smallest team that holds a row; a block that is a team has as
+// many waves as that takes (26214 x 5120 with residual: 205 us, in eight waves of two slices 245).
 template <class F>
 inline void for_width(uint32_t padded, bool two, F f) {
     using std::integral_constant;
-    using One = integral_constant<uint32_t, 1>;
-    using Two = integral_constant<uint32_t, 2>;
-    if (two || padded > 1024) {
-        if (padded <= 32)
-            f(integral_constant<uint32_t, 16>{}, Two{});
-        else if (padded <= 128)
-            f(integral_constant<uint32_t, 64>{}, Two{});
-        else if (padded <= 256)
-            f(integral_constant<uint32_t, 256>{}, One{});
-        else if (padded <= 512)
-            f(integral_constant<uint32_t, 256>{}, Two{});
-        else if (padded <= 1024)
-            f(integral_constant<uint32_t, 512>{}, Two{});
+    const auto of = [&](auto n) {
+        const uint32_t lanes = (padded + n.value - 1) / n.value;
+        if (lanes <= 16)
+            f(integral_constant<uint32_t, 16>{}, n, kBlock);
+        else if (lanes <= 32)
+            f(integral_constant<uint32_t, 32>{}, n, kBlock);
+        else if (lanes <= 64)
+            f(integral_constant<uint32_t, 64>{}, n, kBlock);
         else
-            f(integral_constant<uint32_t, 1024>{}, Two{});
-    } else {
-        if (padded <= 16)
-            f(integral_constant<uint32_t, 16>{}, One{});
-        else if (padded <= 32)
-            f(integral_constant<uint32_t, 32>{}, One{});
-        else if (padded <= 64)
-            f(integral_constant<uint32_t, 64>{}, One{});
-        else if (padded <= 128)
-            f(integral_constant<uint32_t, 128>{}, One{});
-        else if (padded <= 256)
-            f(integral_constant<uint32_t, 256>{}, One{});
-        else if (padded <= 512)
-            f(integral_constant<uint32_t, 512>{}, One{});
-        else
-            f(integral_constant<uint32_t, 1024>{}, One{});
-    }
+            f(integral_constant<uint32_t, kWhole>{}, n, (lanes + 63) / 64 * 64);
+    };
+    if (two || padded > 1024)
+        of(integral_constant<uint32_t, 2>{});
+    else
+        of(integral_constant<uint32_t, 1>{});
+}
+// Forward a lane has two slices where a team is a wave or less (262144 x 512: 98 us, in whole waves of one 169), one where it is
+// a block: 64 registers a lane then and twice the waves (32768 x 4096 with residual: 194 us either way, 21845 x 6144 192 and
+// 288, 65536 x 2048 195 and 221).  Backward it holds sums besides (65536 x 4096: 390 us with one, 523 with two).
+template <class F>
+inline void for_forward(uint32_t padded, F f) {
+    for_width(padded, padded > 16 && padded <= 128, f);
+}
+template <class F>
+inline void for_backward(uint32_t padded, F f) {
+    for_width(padded, false, f);
 }
 
-// Blocks that leave each CU `threads` threads, or fewer where the rows are.
+// Blocks that the chip holds at a time, `waves` of their waves a SIMD, or fewer where the rows are: a block more a CU would begin
+// when the others end (26214 x 5120 with two blocks of ten waves a CU 205 us, with three 245).  A block's waves go to the four SIMDs
+// in turn, and blocks that fill 17 of 20 places have found theirs.
 template <uint32_t TEAM>
-inline uint32_t norm_blocks(uint64_t rows, uint32_t threads) {
-    const uint64_t n = (rows + Team<TEAM>::kPerBlock - 1) / Team<TEAM>::kPerBlock, most = 256 * threads / Team<TEAM>::kThreads;
+inline uint32_t norm_blocks(uint64_t rows, uint32_t block, uint32_t waves) {
+    const uint32_t w = block / 64, whole = w <= 4 ? 4 / w * waves : waves / ((w + 3) / 4), part = 17 * waves / (5 * w);
+    const uint64_t n = (rows + Team<TEAM>::kPerBlock - 1) / Team<TEAM>::kPerBlock, most = 256 * (whole > part ? whole : part);
     return (uint32_t)(n < most ? n : most);
 }
-// Backward each is a row of sums for dw besides: half as many (4096 x 4096: 32 us, with twice as many 40).
-inline uint32_t norm_parts(uint64_t rows, uint32_t padded) {
-    uint32_t n = 0;
-    for_width(padded, false, [&](auto team, auto) { n = norm_blocks<team.value>(rows, 1024); });
-    return n;
+// Backward each is a row of sums for dw besides, so a team has four rows, where that leaves 512 blocks (4096 x 1024: 17 us, with as
+// many as the chip holds 28, with 16 rows a team 25; 65536 x 128: 17 us, with eight rows 21).
+template <uint32_t TEAM>
+inline uint32_t norm_parts(uint64_t rows, uint32_t block, uint32_t waves) {
+    const uint64_t most = rows / (4 * Team<TEAM>::kPerBlock), least = 512, n = norm_blocks<TEAM>(rows, block, waves);
+    return (uint32_t)(n < least || n < most ? n : most < least ? least : most);
 }
 inline uint32_t norm_padded(uint64_t width) { return groups_of(width) * (kGroup / kSlice); }
 
@@ -376,17 +391,21 @@ int poseidon_norm_forward(const void *x, uint64_t x_pitch, const void *residual,
                            out_codes, sum_codes, out_scales, sum_scales};
     const uint32_t size = size_of(type);
     const uint64_t bytes = rows * width * (size * (1 + !!residual + !!out + !!sum) + keep_out + keep_sum);
-    PL_STREAM(bytes, PL_TYPE(type, for_width(padded, true, [&](auto team, auto n) {
-        if constexpr (n.value == 2 || team.value == 256)
+    PL_STREAM(bytes, PL_TYPE(type, for_forward(padded, [&](auto team, auto n, uint32_t block) {
+        if constexpr (n.value == 2 || team.value == 16 || team.value == kWhole)
             norm_forward_kernel<T, team.value, n.value, STREAM>
-                <<<norm_blocks<team.value>(rows, 2048), Team<team.value>::kThreads, 0, (hipStream_t)hip_stream>>>(a);
+                <<<norm_blocks<team.value>(rows, block, kForwardWaves<n.value>), block, 0, (hipStream_t)hip_stream>>>(a);
     })));
     return launched();
 }
 
 uint64_t poseidon_norm_backward_workspace(uint64_t rows, uint64_t width) {
     if (check_sizes(rows, width) != POSEIDON_OK || width > kNormWidth) return UINT64_MAX;
-    return (uint64_t)norm_parts(rows, norm_padded(width)) * width * 4;
+    uint64_t parts = 0;    // of a sum that is not in 8 bits, which has more of them
+    for_backward(norm_padded(width), [&](auto team, auto n, uint32_t block) {
+        parts = norm_parts<team.value>(rows, block, kBackwardWaves<team.value, n.value, false>);
+    });
+    return parts * width * 4;
 }
 
 int poseidon_norm_backward(const void *dout, uint64_t dout_pitch, uint32_t type, uint64_t rows, uint64_t width,
@@ -407,20 +426,23 @@ int poseidon_norm_backward(const void *dout, uint64_t dout_pitch, uint32_t type,
     if (rows && (!rstd || !aligned(rstd, 4))) return POSEIDON_E_INVAL;
     if (accumulate > 1 || !aligned(dweight, 4) || (accumulate && !dweight)) return POSEIDON_E_INVAL;
     if (dweight) PL_TRY(check_workspace(workspace, workspace_bytes, poseidon_norm_backward_workspace(rows, width)));
-    const uint32_t padded = norm_padded(width), blocks = norm_parts(rows, padded);
+    const uint32_t padded = norm_padded(width);
+    uint32_t blocks = 0;
     if (rows) {
         const NormBackward a = {dout, sum, dsum, weight, dout_pitch, sum_pitch, dsum_pitch, dx_pitch, codes, scales, rstd,
                                 (uint32_t)rows, (uint32_t)width, padded, weight_type, dx, dweight ? (float *)workspace : nullptr};
         const uint32_t size = size_of(type);
         const uint64_t bytes = rows * width * (size * (2 + !kept + !!dsum) + kept);
-        PL_STREAM(bytes, PL_TYPE(type, for_width(padded, false, [&](auto team, auto n) {
-            if constexpr (n.value == 1 || team.value == 1024) {
+        PL_STREAM(bytes, PL_TYPE(type, for_backward(padded, [&](auto team, auto n, uint32_t block) {
+            if constexpr (n.value == 1 || team.value == kWhole) {
+                const auto go = [&](auto kernel, uint32_t waves) {
+                    blocks = norm_parts<team.value>(rows, block, waves);
+                    kernel<<<blocks, block, 0, (hipStream_t)hip_stream>>>(a);
+                };
                 if (kept)
-                    norm_backward_kernel<T, true, team.value, n.value, STREAM>
-                        <<<blocks, Team<team.value>::kThreads, 0, (hipStream_t)hip_stream>>>(a);
+                    go(norm_backward_kernel<T, true, team.value, n.value, STREAM>, kBackwardWaves<team.value, n.value, true>);
                 else
-                    norm_backward_kernel<T, false, team.value, n.value, STREAM>
-                        <<<blocks, Team<team.value>::kThreads, 0, (hipStream_t)hip_stream>>>(a);
+                    go(norm_backward_kernel<T, false, team.value, n.value, STREAM>, kBackwardWaves<team.value, n.value, false>);
             }
         })));
         PL_TRY(launched());

@@ -115,6 +115,13 @@ def test_norm(dev, kind, shape, residual, pad, shift):
     _check_norm_backward(dx, dweight, dout, whole, y.rstd, weight, dsum, kind)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("d", [130, 300, 500, 700, 1030, 1500, 2500, 3500, 4600, 5120, 6100, 7168, 8200, 9216, 12200])
+def test_norm_of_widths(dev, kind, d):
+    """Teams of every number of waves."""
+    test_norm(dev, kind, (7, d), True, 0, 0)
+
+
 def test_norm_of_many_rows(dev):
     """Teams go through many rows, and the weight's gradient adds up over all of them; into rows with gaps, added to what is there."""
     rng = np.random.default_rng(3)
