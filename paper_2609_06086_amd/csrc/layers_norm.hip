@@ -22,10 +22,11 @@ struct Team {
     static __device__ __forceinline__ uint32_t size() { return TEAM == kWhole ? blockDim.x : TEAM; }
 };
 
-// Waves that a SIMD has at a time: what their registers allow.  Backward from 8 bits six of them would leave registers in
-// memory (32768 x 8192: 528 us, with five 380).
-template <uint32_t N>
-constexpr uint32_t kForwardWaves = N == 1 ? 8 : 4;
+// Waves that a SIMD has at a time: what their registers allow.  Forward in 32 bits eight of them would leave registers in
+// memory (32768 x 4096, the sum kept too: 569 us, with six 486).
+// So would six waves backward from 8 bits (32768 x 8192: 528 us, with five 367).
+template <class T, uint32_t N>
+constexpr uint32_t kForwardWaves = N == 1 ? (T::kShort ? 8 : 6) : 4;
 template <uint32_t TEAM, uint32_t N, bool KEPT>
 constexpr uint32_t kBackwardWaves = N == 2 ? 4 : TEAM == kWhole && !KEPT ? 6 : 5;
 
@@ -114,7 +115,7 @@ __device__ __forceinline__ float far_rstd(const float (&h)[N][8], float size, fl
 }
 
 template <class T, uint32_t TEAM, uint32_t N, bool STREAM>
-__global__ __launch_bounds__(Team<TEAM>::kMost, kForwardWaves<N>) void norm_forward_kernel(NormForward a) {
+__global__ __launch_bounds__(Team<TEAM>::kMost, (kForwardWaves<T, N>)) void norm_forward_kernel(NormForward a) {
     __shared__ __attribute__((aligned(16))) float sums[3][Team<TEAM>::kSlots];
     __shared__ __attribute__((aligned(16))) uint32_t most[Team<TEAM>::kSlots];
     const uint32_t lanes = Team<TEAM>::size(), lane = TEAM == kWhole ? threadIdx.x : threadIdx.x % TEAM;
@@ -394,7 +395,7 @@ int poseidon_norm_forward(const void *x, uint64_t x_pitch, const void *residual,
     PL_STREAM(bytes, PL_TYPE(type, for_forward(padded, [&](auto team, auto n, uint32_t block) {
         if constexpr (n.value == 2 || team.value == 16 || team.value == kWhole)
             norm_forward_kernel<T, team.value, n.value, STREAM>
-                <<<norm_blocks<team.value>(rows, block, kForwardWaves<n.value>), block, 0, (hipStream_t)hip_stream>>>(a);
+                <<<norm_blocks<team.value>(rows, block, kForwardWaves<T, n.value>), block, 0, (hipStream_t)hip_stream>>>(a);
     })));
     return launched();
 }
