@@ -8,7 +8,9 @@
  * activations kept in 8 bits until the backward pass (they decide how many
  * micro-batches a stage's memory holds), the gated activation and the weight
  * gradients that read what was kept, the sort of tokens by expert with its
- * gather and weighted combination, and the embedding of the first stage.
+ * gather and weighted combination, the experts' products over their rows, the
+ * norm with the residual's addition, causal attention over packed sequences,
+ * and the embedding of the first stage.
  * Forward and backward are both here.
  *
  * Matrices are row-major in DEVICE memory: `rows` rows of `width` values,
