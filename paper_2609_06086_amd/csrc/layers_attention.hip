@@ -218,7 +218,7 @@ __device__ __forceinline__ void clear_token(const Heads &x, uint64_t token, uint
 // the sums then stay below 2^8 times the number of keys, and most tiles leave what was summed alone.
 //
 // Here and in the two kernels below the matrix units bound a long sequence, at the clock that their power leaves; two
-// waves a SIMD, one in its products while the other is in its scores.  16384 tokens, 16 heads of 128 values on 4: 1026 us, 1071
+// waves a SIMD, one in its products while the other is in its scores.  16384 tokens, 16 heads of 128 values on 4: 990 us, 1110
 // TFLOP/s of the 1386 to 1596 that large products reach; units busy for 56 % of the time at 1.65 GHz, no bank conflicts.
 // Eight waves a block: 1321 us where four took 1234.
 template <class T, int D, int WAVES>
