@@ -51,7 +51,8 @@ __device__ __forceinline__ void clear_outside(const Product &g, uint32_t block, 
 // TURNED: W^T, whose values along the sum are a row apart.  ALIGNED: rows begin on 16 bytes and are whole pieces of 16 bytes, which
 // go to LDS without a register between; else they are read with plain loads, which take any address, and masked.
 //
-// LDS holds two stages of 64 values along the sum, 128 bytes of a row.  The last of a stage's operands are in registers when
+// LDS holds X stages (two or three) of 64 values along the sum, 128 bytes of a row, of x and three of the weights, which come
+// from further away: other rows of them for every stage of W^T.  The last of a stage's operands are in registers when
 // a quarter of its products is still to come: there the waves meet, the stage's place is given to the one after the
 // next, and the next one's first operands are read beside the last products, so that no wave waits for LDS at a stage's start.
 //
@@ -59,14 +60,13 @@ __device__ __forceinline__ void clear_outside(const Product &g, uint32_t block, 
 // (1275 TFLOP/s), W^T of 8192 x 4096 1030 us (1068; units busy for 49 % of the time at 1.72 GHz), 64 ragged ranges of 65536 rows by
 // 4096 x 2048 1150 us (956; 50 %, 1.66 GHz); no bank conflicts.  Stages of 32 values with four places: the ragged ranges
 // 1530 us where those of 64 took 1347.
-template <class T, bool TURNED, bool ALIGNED, int R, int C, int M, int N>
+template <class T, bool TURNED, bool ALIGNED, int R, int C, int M, int N, int X>
 __global__ __launch_bounds__(64 * R * C, 2) void product_kernel(Product g) {
     constexpr uint32_t kRows = 32 * R * M, kCols = 32 * C * N, kThreads = 64 * R * C;
-    constexpr uint32_t kX = kRows * kDeep, kW = kCols * kDeep, kStageW = 2 * kX;    // values of a stage; where the weights begin
+    constexpr uint32_t kX = kRows * kDeep, kW = kCols * kDeep, kStageW = X * kX;    // values of a stage; where the weights begin
     constexpr uint32_t kLoadsX = kX / 8 / kThreads, kLoadsW = kW / 8 / kThreads;
-    constexpr uint32_t kPlaces = 3;    // of the weights, which come from further away: other rows of them for every stage of W^T
     constexpr uint32_t kPieces = kDeep / 8;                                         // of a row
-    __shared__ __attribute__((aligned(16))) uint16_t lds[2 * kX + kPlaces * kW];    // two stages of x, then those of the weights
+    __shared__ __attribute__((aligned(16))) uint16_t lds[X * kX + 3 * kW];    // stages of x, then those of the weights
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const uint32_t tiles = g.tiles_r * g.tiles_c;
     if (blockIdx.x >= tiles) {
@@ -240,68 +240,77 @@ __global__ __launch_bounds__(64 * R * C, 2) void product_kernel(Product g) {
     using N0 = std::integral_constant<int, 0>;
     using N1 = std::integral_constant<int, 1>;
     using N2 = std::integral_constant<int, 2>;
-    using Ahead = std::integral_constant<int, (int)kLoadsW>;    // loads of weights that may be on their way
+    // Loads that may be on their way when the stage before theirs has to be there.
+    using Ahead = std::integral_constant<int, (int)(X == 3 ? kLoadsX + kLoadsW : kLoadsW)>;
+    static_assert(X == 2 || (X == 3 && ALIGNED));
     fetch_x(0, N0{});
     fetch_w(0, N0{});
     if constexpr (!ALIGNED) deposit(N0{}, N0{});
     if (ALIGNED && stages > 1) {
+        if constexpr (X == 3) fetch_x(1, N1{});
         fetch_w(1, N1{});
         meet(Ahead{});
     } else {
         meet(N0{});
     }
     if (stages > 1) {
-        fetch_x(1, N1{});
+        if constexpr (X == 2) fetch_x(1, N1{});
         if constexpr (!ALIGNED) {
             fetch_w(1, N1{});
             deposit(N1{}, N1{});
         }
     }
-    if (ALIGNED && stages > 2) fetch_w(2, N2{});
+    if (ALIGNED && stages > 2) {
+        if constexpr (X == 3) fetch_x(2, N2{});
+        fetch_w(2, N2{});
+    }
     read(N0{}, N0{}, 0);
     const auto step = [&](auto turn, uint32_t i) __attribute__((always_inline)) {
         constexpr int n = decltype(turn)::value;
-        using X = std::integral_constant<int, n % 2>;
-        using W = std::integral_constant<int, n % 3>;
-        using NextX = std::integral_constant<int, (n + 1) % 2>;
+        using AtX = std::integral_constant<int, n % X>;
+        using AtW = std::integral_constant<int, n % 3>;
+        using NextX = std::integral_constant<int, (n + 1) % X>;
         using NextW = std::integral_constant<int, (n + 1) % 3>;
+        using AfterX = std::integral_constant<int, (n + 2) % X>;
         using AfterW = std::integral_constant<int, (n + 2) % 3>;
         if constexpr (!ALIGNED) {
             if (i + 2 < stages) {
-                fetch_x(i + 2, X{});
+                fetch_x(i + 2, AfterX{});
                 fetch_w(i + 2, AfterW{});
             }
         }
         if (busy) {
-            read(X{}, W{}, 1);
+            read(AtX{}, AtW{}, 1);
             multiply(0);
-            read(X{}, W{}, 2);
+            read(AtX{}, AtW{}, 2);
             multiply(1);
-            read(X{}, W{}, 3);
+            read(AtX{}, AtW{}, 3);
             multiply(2);
         }
-        if (i + 2 < stages)    // the weights of the stage after the next may be on their way
+        if (i + 2 < stages)    // what was asked for of the stage after the next may be on its way
             meet(Ahead{});
         else
             meet(N0{});
         if constexpr (ALIGNED) {
-            if (i + 2 < stages) fetch_x(i + 2, X{});
-            if (i + 3 < stages) fetch_w(i + 3, W{});
+            if (i + X < stages) fetch_x(i + X, AtX{});
+            if (i + 3 < stages) fetch_w(i + 3, AtW{});
         } else {
-            if (i + 2 < stages) deposit(X{}, AfterW{});
+            if (i + 2 < stages) deposit(AfterX{}, AfterW{});
         }
         if (busy) {
             read(NextX{}, NextW{}, 0);    // after the last stage: of what lies there, to no use
             multiply(3);
         }
     };
-    for (uint32_t i = 0; i < stages; i += 6) {    // the places are the same again after six
+    for (uint32_t i = 0; i < stages; i += X == 3 ? 3 : 6) {    // then the places are the same again
         step(N0{}, i);
         if (i + 1 < stages) step(N1{}, i + 1);
         if (i + 2 < stages) step(N2{}, i + 2);
-        if (i + 3 < stages) step(std::integral_constant<int, 3>{}, i + 3);
-        if (i + 4 < stages) step(std::integral_constant<int, 4>{}, i + 4);
-        if (i + 5 < stages) step(std::integral_constant<int, 5>{}, i + 5);
+        if constexpr (X == 2) {
+            if (i + 3 < stages) step(std::integral_constant<int, 3>{}, i + 3);
+            if (i + 4 < stages) step(std::integral_constant<int, 4>{}, i + 4);
+            if (i + 5 < stages) step(std::integral_constant<int, 5>{}, i + 5);
+        }
     }
 
     // A lane has a row, and of each 32 columns 4 of every 8: the two halves of the wave trade theirs, so that a lane
@@ -501,10 +510,11 @@ int poseidon_expert_product(const void *x, uint64_t pitch, uint32_t type, uint64
         kernel<<<(uint32_t)(r * c) + (offsets ? kClearing : 0), threads, 0, (hipStream_t)hip_stream>>>(g);
         return launched();
     };
-    // A few rows a range on average, or in all, whose weights a large tile would read no faster and whose columns would be too
-    // few large tiles (one range of 4096 x 4096: 64 rows 24 us and 33 in tiles, 96 rows 35 and 33; 64 ranges of 4096 x 2048: 384
-    // rows 211 us and 227, 512 rows 218 and 228, 768 rows 245 and 235; 16 of 1001 x 1365: 128 rows 24 us and 28, 256 34 and 28).
-    if (!transposed && (rows <= 64 || rows <= 8ull * n_ranges)) {
+    // A few rows a range on average, or in all, whose weights a tile would read no faster and whose columns would be too few
+    // tiles (64 ranges of 4096 x 2048: 8 rows 29 us and in tiles 74 to 138, 384 rows 211 and 227, 512 rows 218 and 229, 768 rows 245 and
+    // 235; one of 8192 x 8192: 1 row 33 and 57, 32 rows 47 and 59, 64 rows 88 and 62; of 2048 x 8192: 64 rows 24 and 43, of 4096 x 4096 24
+    // either way).
+    if (!transposed && (rows <= 32 || (rows <= 64 && wide <= 4096) || rows <= 8ull * n_ranges)) {
         const uint64_t r = rows < rows / kFew + n_ranges ? rows : rows / kFew + n_ranges, c = (wide + kFewCols - 1) / kFewCols;
         g.tiles_r = (uint32_t)r;
         g.tiles_c = (uint32_t)c;
@@ -521,8 +531,12 @@ int poseidon_expert_product(const void *x, uint64_t pitch, uint32_t type, uint64
         constexpr bool kTurned = decltype(turned)::value, kWhole = decltype(whole_)::value;
         // 256 x 256 tiles, one a CU, where most CUs get one (one range of 3000 x 3000, 4096 rows, 204 tiles: 89 us, in 128 x 128 120;
         // 6000 rows of 2048 x 2048, 192: 57 and 60; 5120 rows, 168: 59 and 56).
-        return large >= 180 ? run(product_kernel<T, kTurned, kWhole, 2, 4, 4, 2>, 256, 256, 512)
-                            : run(product_kernel<T, kTurned, kWhole, 2, 2, 2, 2>, 128, 128, 256);
+        if (large >= 180) return run(product_kernel<T, kTurned, kWhole, 2, 4, 4, 2, 2>, 256, 256, 512);
+        // 128 x 128 where every CU gets one (4096 rows in 16 ranges of 1024 x 1024, 384 tiles: 18 us, in 64 x 128 21; 512 rows of 4096 x
+        // 4096, 160: 35 and 26; 256 rows of them 33 and 24).
+        if (tiles_for(rows, n_ranges, 128) * ((wide + 127) / 128) >= 256) return run(product_kernel<T, kTurned, kWhole, 2, 2, 2, 2, 2>, 128, 128, 256);
+        // with a third stage of x, as nothing else on a CU hides its way from memory (256 rows of 4096 x 4096: 24 us, with two 28)
+        return run(product_kernel<T, kTurned, kWhole, 2, 2, 1, 2, kWhole ? 3 : 2>, 64, 128, 256);
     };
     const auto of = [&](auto t) -> int {
         using Yes = std::true_type;

@@ -212,6 +212,16 @@ def test_product_over_large_tiles(dev, transposed, rows, o, i, ranges):
     _product_case(rng, dev, "bf16", [0] + cuts + [rows], rows, o, i, transposed)
 
 
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("deep", [8, 64, 72, 128, 136, 200, 264, 333, 392, 456, 520])
+def test_product_over_small_and_middle_tiles(dev, transposed, deep):
+    """64 x 128 and 128 x 128 tiles with one stage of the sum to nine, the last ones of a range and a row part full."""
+    rng = np.random.default_rng(deep)
+    for rows, offsets, wide in ((150, [0, 150], 264), (600, [5, 230, 230, 231, 590], 136), (2100, [0, 2100], 2000), (4300, [0, 1000, 1001, 2900, 4290], 1000)):
+        o, i = (deep, wide) if transposed else (wide, deep)
+        _product_case(rng, dev, "bf16", offsets, rows, o, i, transposed)
+
+
 @pytest.mark.parametrize("kind", SHORT)
 def test_product_of_few_rows(dev, kind):
     """One token by experts, the most rows that go the short way, and one range that has them all."""
