@@ -204,7 +204,8 @@ int poseidon_attention_forward(const void *q, uint64_t q_token, uint64_t q_head,
 /* Its gradients from dout and what the forward pass gave: with p[i][j] = exp(s[i][j] - lse[i]) and
  * ds[i][j] = p[i][j] (<dout[i], v[j]> - <dout[i], out[i]>): dq[i] = scale * sum over j of ds[i][j] k[j],
  * dk[j] = scale * sum over i of ds[i][j] q[i], dv[j] = sum over i of p[i][j] dout[i], those two over the query heads that share
- * the key, all in a fixed order.  p and ds are rounded to `type` for these products. */
+ * the key, all in a fixed order.  p and ds are rounded to `type` for these products, in f16 after a power of two that keeps them
+ * within its range: gradients that f16 holds are as near for a small dout, or a large one, as for one about 1. */
 int poseidon_attention_backward(const void *dout, uint64_t dout_token, uint64_t dout_head, const void *q,
                                 uint64_t q_token, uint64_t q_head, const void *k, uint64_t k_token, uint64_t k_head,
                                 const void *v, uint64_t v_token, uint64_t v_head, const void *out, uint64_t out_token,
