@@ -193,7 +193,8 @@ uint64_t poseidon_norm_backward_workspace(uint64_t rows, uint64_t width);
  * dim: a multiple of 8 up to POSEIDON_HEAD_MAX; kv_heads divides heads.  lse: float[heads][tokens].
  * offsets: DEVICE int32[sequences + 1], non-decreasing, sequence r = tokens [offsets[r], offsets[r + 1]), each cut to
  * [0, tokens]; tokens before the first and after the last sequence get zeros, their lse -infinity.  Offsets that descend leave
- * it open which tokens are written.  NULL with sequences == 1: all tokens.
+ * it open which tokens are written.  NULL with sequences == 1: all tokens.  POSEIDON_E_RANGE where
+ * heads * (tokens / 128 + sequences) passes 2^31 - 256.
  * An infinity or a NaN may reach every result of its own sequence, and none of another. */
 int poseidon_attention_forward(const void *q, uint64_t q_token, uint64_t q_head, const void *k, uint64_t k_token,
                                uint64_t k_head, const void *v, uint64_t v_token, uint64_t v_head, uint32_t type,

@@ -28,7 +28,7 @@ struct Attention {
     float *lse, *delta, *base;               // [heads][tokens]; base: -lse / ln 2 + kRaised
     const int32_t *offsets;                  // null: one sequence of all tokens
     float *parts;                            // [split][dk, dv][tokens][kv heads][dim] sums, where split > 1
-    uint32_t tokens, sequences, heads, kv_heads, dim, tiles, split;
+    uint32_t tokens, sequences, heads, kv_heads, dim, tiles, split, first;    // first: block of this launch
     float scale;
 };
 
@@ -235,11 +235,11 @@ __device__ __forceinline__ Place sequence_of(const Attention &a, uint32_t tile, 
     return p;
 }
 
-// f(token) for the tokens outside of all sequences that fall to block `block` of `blocks`.
+// f(token) for the tokens outside of all sequences that fall to block `block` of kClearBlocks.
 template <class F>
-__device__ __forceinline__ void outside(const Attention &a, uint32_t block, uint32_t blocks, F f) {
+__device__ __forceinline__ void outside(const Attention &a, uint32_t block, F f) {
     const uint32_t begin = bound_of(a.offsets, 0, a.tokens), end = max(begin, bound_of(a.offsets, a.sequences, a.tokens));
-    for (uint32_t i = block; i < begin + a.tokens - end; i += blocks) f((uint64_t)(i < begin ? i : end + (i - begin)));
+    for (uint32_t i = block; i < begin + a.tokens - end; i += kClearBlocks) f((uint64_t)(i < begin ? i : end + (i - begin)));
 }
 template <class T>
 __device__ __forceinline__ void clear_token(const Heads &x, uint64_t token, uint32_t heads, uint32_t dim) {
@@ -260,15 +260,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_forward_kernel(Attent
     constexpr uint32_t kQueries = 32 * WAVES, kStage = 2 * kTile * D;
     __shared__ __attribute__((aligned(16))) uint16_t lds[2 * kStage];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const uint32_t blocks = a.tiles * a.heads;
-    if (blockIdx.x >= blocks) {
-        outside(a, blockIdx.x - blocks, gridDim.x - blocks, [&](uint64_t t) {
+    const uint32_t blocks = a.tiles * a.heads, id = a.first + blockIdx.x;
+    if (id >= blocks) {
+        outside(a, id - blocks, [&](uint64_t t) {
             clear_token<T>(a.out, t, a.heads, a.dim);
             for (uint32_t h = threadIdx.x; h < a.heads; h += blockDim.x) a.lse[(uint64_t)h * a.tokens + t] = -__builtin_inff();
         });
         return;
     }
-    const Work w = work_of(blockIdx.x, a.heads, a.kv_heads);
+    const Work w = work_of(id, a.heads, a.kv_heads);
     uint32_t begin;    // the longest rows of a sequence first
     const Place at = sequence_of(a, a.tiles - 1 - w.tile, kQueries, begin);
     if (!at.there) return;
@@ -374,12 +374,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_queries_kernel(Attent
     constexpr uint32_t kQueries = 32 * WAVES, kStage = 2 * kTile * D;
     __shared__ __attribute__((aligned(16))) uint16_t lds[2 * kStage];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const uint32_t blocks = a.tiles * a.heads;
-    if (blockIdx.x >= blocks) {
-        outside(a, blockIdx.x - blocks, gridDim.x - blocks, [&](uint64_t t) { clear_token<T>(a.dq, t, a.heads, a.dim); });
+    const uint32_t blocks = a.tiles * a.heads, id = a.first + blockIdx.x;
+    if (id >= blocks) {
+        outside(a, id - blocks, [&](uint64_t t) { clear_token<T>(a.dq, t, a.heads, a.dim); });
         return;
     }
-    const Work w = work_of(blockIdx.x, a.heads, a.kv_heads);
+    const Work w = work_of(id, a.heads, a.kv_heads);
     uint32_t begin;
     const Place at = sequence_of(a, a.tiles - 1 - w.tile, kQueries, begin);
     if (!at.there) return;
@@ -485,16 +485,16 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_keys_kernel(Attention
     constexpr int kHeld = D == 128 ? 5 : D / 16, kSpare = D / 16 - kHeld;
     __shared__ Words4 spare[kSpare ? WAVES * kSpare * 64 : 1];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const uint32_t blocks = a.tiles * a.split * a.kv_heads;
-    if (blockIdx.x >= blocks) {
-        outside(a, blockIdx.x - blocks, gridDim.x - blocks, [&](uint64_t t) {
+    const uint32_t blocks = a.tiles * a.split * a.kv_heads, id = a.first + blockIdx.x;
+    if (id >= blocks) {
+        outside(a, id - blocks, [&](uint64_t t) {
             clear_token<T>(a.dk, t, a.kv_heads, a.dim);
             clear_token<T>(a.dv, t, a.kv_heads, a.dim);
         });
         return;
     }
-    const uint32_t kv = blockIdx.x % a.kv_heads, group = a.heads / a.kv_heads / a.split;
-    const uint32_t tile = blockIdx.x / a.kv_heads / a.split, part = blockIdx.x / a.kv_heads % a.split;
+    const uint32_t kv = id % a.kv_heads, group = a.heads / a.kv_heads / a.split;
+    const uint32_t tile = id / a.kv_heads / a.split, part = id / a.kv_heads % a.split;
     const uint32_t head0 = (kv * a.split + part) * group;    // the first of the block's query heads
     uint32_t begin;    // keys early in a sequence have the most queries: these first
     const Place at = sequence_of(a, tile, kKeys, begin);
@@ -715,10 +715,9 @@ template <class K>
 inline int run_attention(K kernel, Attention &a, uint64_t heads, void *hip_stream) {
     constexpr uint32_t waves = kWaves;
     const uint64_t tiles = attention_tiles(a.tokens, a.offsets ? a.sequences : 0);
-    if (tiles * heads > 0x7fffff00ull) return POSEIDON_E_RANGE;
+    if (tiles * heads > kBlocksMost) return POSEIDON_E_RANGE;
     a.tiles = (uint32_t)tiles;
-    kernel<<<(uint32_t)(tiles * heads) + (a.offsets ? kClearBlocks : 0), 64 * waves, 0, (hipStream_t)hip_stream>>>(a);
-    return launched();
+    return launch_blocks(kernel, a, tiles * heads + (a.offsets ? kClearBlocks : 0), 64 * waves, hip_stream);
 }
 
 }  // namespace pl

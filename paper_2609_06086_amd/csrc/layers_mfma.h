@@ -116,4 +116,18 @@ __device__ __forceinline__ Place place_of(const int32_t *offsets, uint32_t range
 }
 inline uint64_t tiles_for(uint64_t rows, uint64_t ranges, uint32_t size) { return rows / size + ranges; }
 
+// Blocks from a.first on, in as many launches as it takes: a grid holds less than 2^32 threads.  Each begins at a multiple of 8, so
+// that blocks go round the XCDs as in one.
+template <class K, class A>
+inline int launch_blocks(K kernel, A a, uint64_t blocks, uint32_t threads, void *hip_stream) {
+    const uint64_t most = 0xffffffffull / threads / 8 * 8;
+    for (uint64_t at = 0; at < blocks; at += most) {
+        a.first = (uint32_t)at;
+        kernel<<<(uint32_t)(blocks - at < most ? blocks - at : most), threads, 0, (hipStream_t)hip_stream>>>(a);
+        PL_TRY(launched());
+    }
+    return POSEIDON_OK;
+}
+constexpr uint64_t kBlocksMost = 0x7fffff00u;    // of a call
+
 }  // namespace pl

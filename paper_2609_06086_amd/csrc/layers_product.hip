@@ -12,7 +12,7 @@ struct Product {
     uint64_t pitch, out_pitch;
     uint32_t rows, ranges, deep, wide;    // deep: values that are summed, wide: values of an output row
     const int32_t *offsets;               // null: one range of all rows
-    uint32_t tiles_r, tiles_c;            // tiles of rows (an upper bound), and of columns
+    uint32_t tiles_r, tiles_c, first;     // tiles of rows (an upper bound), and of columns; block of this launch
     void *out;
     uint32_t out_type;
 };
@@ -32,11 +32,11 @@ __device__ __forceinline__ Tile tile_of(uint32_t id, uint32_t all, uint32_t tile
 }
 
 template <class T>
-__device__ __forceinline__ void clear_outside(const Product &g, uint32_t block, uint32_t blocks, uint32_t threads) {
+__device__ __forceinline__ void clear_outside(const Product &g, uint32_t block, uint32_t threads) {
     const uint32_t begin = bound_of(g.offsets, 0, g.rows), end = max(begin, bound_of(g.offsets, g.ranges, g.rows));
     const uint32_t gone = begin + g.rows - end, per_row = (g.wide + kSlice - 1) / kSlice;
     const float zero[8] = {};
-    for (uint32_t i = block; i < gone; i += blocks) {
+    for (uint32_t i = block; i < gone; i += kClearing) {
         const uint64_t row = i < begin ? i : end + (i - begin);
         for (uint32_t s = threadIdx.x; s < per_row; s += threads) {
             if (g.out_type == POSEIDON_F32)
@@ -68,12 +68,12 @@ __global__ __launch_bounds__(64 * R * C, 2) void product_kernel(Product g) {
     constexpr uint32_t kPieces = kDeep / 8;                                         // of a row
     __shared__ __attribute__((aligned(16))) uint16_t lds[X * kX + 3 * kW];    // stages of x, then those of the weights
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64);
-    const uint32_t tiles = g.tiles_r * g.tiles_c;
-    if (blockIdx.x >= tiles) {
-        clear_outside<T>(g, blockIdx.x - tiles, gridDim.x - tiles, kThreads);
+    const uint32_t tiles = g.tiles_r * g.tiles_c, id = g.first + blockIdx.x;
+    if (id >= tiles) {
+        clear_outside<T>(g, id - tiles, kThreads);
         return;
     }
-    const Tile tile = tile_of(blockIdx.x, tiles, g.tiles_r, g.tiles_c);
+    const Tile tile = tile_of(id, tiles, g.tiles_r, g.tiles_c);
     Place at = {0, tile.r * kRows, g.rows, tile.r * kRows < g.rows};
     if (g.offsets) at = place_of(g.offsets, g.ranges, g.rows, tile.r, kRows);
     if (!at.there) return;
@@ -395,12 +395,12 @@ __global__ __launch_bounds__(kBlock) void few_rows_kernel(Product g) {
     constexpr uint32_t kAhead = 2;                           // turns that are asked for at a time
     __shared__ float sums[4][2][kFewCols][17];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const uint32_t blocks = g.tiles_r * g.tiles_c;
-    if (blockIdx.x >= blocks) {
-        clear_outside<T>(g, blockIdx.x - blocks, gridDim.x - blocks, kBlock);
+    const uint32_t blocks = g.tiles_r * g.tiles_c, id = g.first + blockIdx.x;
+    if (id >= blocks) {
+        clear_outside<T>(g, id - blocks, kBlock);
         return;
     }
-    const uint32_t tile = blockIdx.x / g.tiles_c, col0 = blockIdx.x % g.tiles_c * kFewCols;
+    const uint32_t tile = id / g.tiles_c, col0 = id % g.tiles_c * kFewCols;
     Place at = {0, tile * kFew, g.rows, tile * kFew < g.rows};
     if (g.offsets) at = few_of(g, tile);
     if (!at.there) return;
@@ -497,18 +497,17 @@ int poseidon_expert_product(const void *x, uint64_t pitch, uint32_t type, uint64
     PL_TRY(check_matrix(out, out_pitch, out_type, rows, wide));
     if (rows && !aligned(offsets, 4)) return POSEIDON_E_INVAL;
     if (!rows) return POSEIDON_OK;
-    Product g = {x, weights, pitch, out_pitch, (uint32_t)rows, n_ranges, (uint32_t)deep, (uint32_t)wide, offsets, 0, 0, out, out_type};
+    Product g = {x, weights, pitch, out_pitch, (uint32_t)rows, n_ranges, (uint32_t)deep, (uint32_t)wide, offsets, 0, 0, 0, out, out_type};
     // 16-byte pieces that lie on 16 bytes and end with the row, at offsets of less than 2^31 bytes within a tile's rows and, for
     // W^T, within W
     const bool whole = deep % 8 == 0 && in_width % 8 == 0 && pitch % 8 == 0 && aligned(x, 16) && aligned(weights, 16) &&
                        pitch < (1u << 21) && (!transposed || out_width * in_width < (1u << 30));
     const auto run = [&](auto kernel, uint32_t tile_r, uint32_t tile_c, uint32_t threads) -> int {
         const uint64_t r = offsets ? tiles_for(rows, n_ranges, tile_r) : (rows + tile_r - 1) / tile_r, c = (wide + tile_c - 1) / tile_c;
-        if (r * c > 0x7fffff00ull) return POSEIDON_E_RANGE;
+        if (r * c > kBlocksMost) return POSEIDON_E_RANGE;
         g.tiles_r = (uint32_t)r;
         g.tiles_c = (uint32_t)c;
-        kernel<<<(uint32_t)(r * c) + (offsets ? kClearing : 0), threads, 0, (hipStream_t)hip_stream>>>(g);
-        return launched();
+        return launch_blocks(kernel, g, r * c + (offsets ? kClearing : 0), threads, hip_stream);
     };
     // A few rows a range on average, or in all, whose weights a tile would read no faster and whose columns would be too few
     // tiles (64 ranges of 4096 x 2048: 8 rows 29 us and in tiles 74 to 138, 384 rows 211 and 227, 512 rows 218 and 229, 768 rows 245 and
@@ -518,12 +517,9 @@ int poseidon_expert_product(const void *x, uint64_t pitch, uint32_t type, uint64
         const uint64_t r = rows < rows / kFew + n_ranges ? rows : rows / kFew + n_ranges, c = (wide + kFewCols - 1) / kFewCols;
         g.tiles_r = (uint32_t)r;
         g.tiles_c = (uint32_t)c;
-        const uint32_t blocks = (uint32_t)(r * c) + (offsets ? kClearing : 0);
-        if (type == POSEIDON_F16)
-            few_rows_kernel<F16><<<blocks, kBlock, 0, (hipStream_t)hip_stream>>>(g);
-        else
-            few_rows_kernel<BF16><<<blocks, kBlock, 0, (hipStream_t)hip_stream>>>(g);
-        return launched();
+        const uint64_t blocks = r * c + (offsets ? kClearing : 0);
+        return type == POSEIDON_F16 ? launch_blocks(few_rows_kernel<F16>, g, blocks, kBlock, hip_stream)
+                                    : launch_blocks(few_rows_kernel<BF16>, g, blocks, kBlock, hip_stream);
     }
     const uint64_t large = tiles_for(rows, n_ranges, 256) * ((wide + 255) / 256);
     const auto pick = [&](auto t, auto turned, auto whole_) -> int {
