@@ -72,6 +72,12 @@ struct Loader {
     }
 };
 
+// Two stages of two tiles in LDS.  The boundary is SmallReader's.
+template <int D>
+struct alignas(2 * D) Stages {
+    uint16_t at[4 * kTile * D];
+};
+
 // Operands from a tile in LDS that begins OFFSET values into it: 16 values from 16 s on of rows 32 t + lane % 32, and the
 // turned rows (lane: value 32 d + lane % 32) that go with the scores of rows [16 s, 16 s + 16) in a lane's registers:
 // 4 half + {0..3}, then 8 + 4 half + {0..3}.  A lane's places are found once; tiles and rows are offsets in the instructions.
@@ -79,8 +85,8 @@ template <int D>
 struct Reader {
     using Bytes = __attribute__((address_space(3))) const char *;
     uint32_t rows[D / 16], lo[D / 32], hi[D / 32];
-    __device__ __forceinline__ Reader(const uint16_t *lds, uint32_t lane) {
-        const uint32_t base = (uint32_t)(uintptr_t)(Bytes)(const char *)lds;
+    __device__ __forceinline__ Reader(const Stages<D> &lds, uint32_t lane) {
+        const uint32_t base = (uint32_t)(uintptr_t)(Bytes)(const char *)lds.at;
         const uint32_t r = lane % 32, u = 4 * (lane / 32) + lane % 16 / 4, c = 2 * (lane / 16 % 2) + lane % 4 / 2;
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) rows[s] = base + r * (2 * D) + ((2 * s + lane / 32) ^ mixed<D>(r)) * 16;
@@ -102,12 +108,14 @@ struct Reader {
     }
 };
 
-// The same with three places, from which the others are an exclusive or away: for a kernel that needs its registers.
+// The same with three places, from which the others are an exclusive or away: for a kernel that needs its registers.  An exclusive
+// or takes the place of an addition within a row of 2 D bytes, so rows begin at a multiple of that.
 template <int D>
 struct SmallReader {
     using Bytes = __attribute__((address_space(3))) const char *;
     uint32_t rows, lo, hi;
-    __device__ __forceinline__ SmallReader(const uint16_t *lds, uint32_t lane) {
+    static_assert(alignof(Stages<D>) % (2 * D) == 0 && 32 * (D / 16 - 1) < 2 * D && 64 * (D / 32 - 1) < 2 * D);
+    __device__ __forceinline__ SmallReader(const Stages<D> &lds, uint32_t lane) {
         const Reader<D> all(lds, lane);
         rows = all.rows[0];
         lo = all.lo[0];
@@ -258,7 +266,8 @@ __device__ __forceinline__ void clear_token(const Heads &x, uint64_t token, uint
 template <class T, int D, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void attention_forward_kernel(Attention a) {
     constexpr uint32_t kQueries = 32 * WAVES, kStage = 2 * kTile * D;
-    __shared__ __attribute__((aligned(16))) uint16_t lds[2 * kStage];
+    __shared__ Stages<D> lds;
+    static_assert(sizeof lds == 2 * 2 * kStage);
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint32_t blocks = a.tiles * a.heads, id = a.first + blockIdx.x;
     if (id >= blocks) {
@@ -288,7 +297,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_forward_kernel(Attent
     const uint32_t k_place = loader.place(a.k.token), v_place = loader.place(a.v.token);
     const auto fetch = [&](uint32_t i) {
         const uint32_t t = begin + i * kTile, rows = at.end - t;
-        uint16_t *to = lds + (i & 1) * kStage;
+        uint16_t *to = lds.at + (i & 1) * kStage;
         loader.template load<T>(row_of<T>(a.k, t, w.kv), a.k.token, k_place, rows, to);
         loader.template load<T>(row_of<T>(a.v, t, w.kv), a.v.token, v_place, rows, to + kTile * D);
     };
@@ -372,7 +381,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_forward_kernel(Attent
 template <class T, int D, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void attention_queries_kernel(Attention a) {
     constexpr uint32_t kQueries = 32 * WAVES, kStage = 2 * kTile * D;
-    __shared__ __attribute__((aligned(16))) uint16_t lds[2 * kStage];
+    __shared__ Stages<D> lds;
+    static_assert(sizeof lds == 2 * 2 * kStage);
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint32_t blocks = a.tiles * a.heads, id = a.first + blockIdx.x;
     if (id >= blocks) {
@@ -412,7 +422,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_queries_kernel(Attent
     const uint32_t k_place = loader.place(a.k.token), v_place = loader.place(a.v.token);
     const auto fetch = [&](uint32_t i) {
         const uint32_t t = begin + i * kTile, rows = at.end - t;
-        uint16_t *to = lds + (i & 1) * kStage;
+        uint16_t *to = lds.at + (i & 1) * kStage;
         loader.template load<T>(row_of<T>(a.k, t, w.kv), a.k.token, k_place, rows, to);
         loader.template load<T>(row_of<T>(a.v, t, w.kv), a.v.token, v_place, rows, to + kTile * D);
     };
@@ -480,7 +490,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_queries_kernel(Attent
 template <class T, int D, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void attention_keys_kernel(Attention a) {
     constexpr uint32_t kKeys = 32 * WAVES, kStage = 2 * kTile * D;
-    __shared__ __attribute__((aligned(16))) uint16_t lds[2 * kStage];
+    __shared__ Stages<D> lds;
+    static_assert(sizeof lds == 2 * 2 * kStage);
     __shared__ __attribute__((aligned(16))) float rows[2][2][kTile];    // base and delta
     constexpr int kHeld = D == 128 ? 5 : D / 16, kSpare = D / 16 - kHeld;
     __shared__ Words4 spare[kSpare ? WAVES * kSpare * 64 : 1];
@@ -528,7 +539,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_keys_kernel(Attention
     const auto fetch = [&](uint32_t set) {    // the next tile
         if (!more) return;
         const uint32_t t = at.begin + asked * kTile, n = at.end - t, head = head0 + g;
-        uint16_t *to = lds + set * kStage;
+        uint16_t *to = lds.at + set * kStage;
         loader.template load<T>(row_of<T>(a.q, t, head), a.q.token, q_place, n, to);
         loader.template load<T>(row_of<T>(a.dout, t, head), a.dout.token, dout_place, n, to + kTile * D);
         if (wave < 2) {    // rows past the end: zeros, as q and dout have there
