@@ -83,15 +83,29 @@ class KeptAttention:
         return self.kept_bytes + sum(2 * s.rows * s.width - s.nbytes for s in (self.h, self.y))
 
 
+def key_heads(shape: Shape, dtype=torch.bfloat16) -> int:
+    """The heads of the keys of an attention of these sizes; ValueError for what its operators do not take."""
+    d, heads, kv_heads = shape.width, shape.heads, shape.kv_heads or shape.heads
+    if not 0 < heads <= L.HEADS_MAX or d > L.NORM_WIDTH_MAX:
+        raise ValueError(f"{heads} heads of a width of {d}: 1 to {L.HEADS_MAX}, widths up to {L.NORM_WIDTH_MAX}")
+    if d % heads or d // heads % 8 or d // heads > L.HEAD_MAX:
+        raise ValueError(f"{heads} heads do not share a width of {d} in multiples of 8 up to {L.HEAD_MAX}")
+    if kv_heads < 0 or heads % kv_heads:
+        raise ValueError(f"{kv_heads} heads of keys do not divide {heads} heads")
+    if shape.sequence < 0:
+        raise ValueError(f"sequences of {shape.sequence} tokens")
+    if dtype not in (torch.float16, torch.bfloat16):
+        raise ValueError(f"attention in {dtype}: float16 or bfloat16")
+    return kv_heads
+
+
 class AttentionBlock:
-    """out = x + Wo attention(Wqkv norm(x)), causal within each of the packed sequences."""
+    """out = x + Wo attention(Wqkv norm(x)), causal within each of the packed sequences.  float16 or bfloat16."""
 
     def __init__(self, shape: Shape, device, seed: int = 0, dtype=torch.bfloat16):
         g = torch.Generator(device=device)
         g.manual_seed(seed)
-        d, self.heads, self.kv_heads = shape.width, shape.heads, shape.kv_heads or shape.heads
-        if not self.heads or d % self.heads:
-            raise ValueError(f"{self.heads} heads do not share a width of {d}")
+        d, self.heads, self.kv_heads = shape.width, shape.heads, key_heads(shape, dtype)
         self.dim = d // self.heads
         self.parts = [n * self.dim for n in (self.heads, self.kv_heads, self.kv_heads)]
 
@@ -350,6 +364,11 @@ def main() -> None:
     a = ap.parse_args()
     shape = Shape(width=a.width, experts=a.experts, chosen=a.chosen, inner=a.inner, tokens=a.tokens,
                   heads=a.heads, kv_heads=a.kv_heads, sequence=a.sequence)
+    if shape.heads:
+        try:
+            key_heads(shape)
+        except ValueError as e:
+            ap.error(str(e))
     first, eight = measure(shape)
     cap = a.cap_mb or int(1.05 * -(-a.blocks // a.stages) *
                           (eight.weight_bytes + min(a.stages, a.micro_batches) * eight.kept_bytes) / 1e6 +
