@@ -14,7 +14,7 @@ from __future__ import annotations
 import argparse
 import statistics
 from dataclasses import dataclass, replace
-from typing import Optional
+from typing import List, Optional
 
 import numpy as np
 import torch
@@ -151,6 +151,7 @@ class Kept:
     probs: torch.Tensor        # the chosen experts' weights
     choice: torch.Tensor
     plan: L.ExpertPlan
+    cuts: Optional[List[int]]  # in 32 bits the experts' row ranges, on the host for the library's products
     xs: L.Stash
     gate: L.Stash
     up: L.Stash
@@ -189,14 +190,15 @@ class ExpertBlock:
         return sum(w.numel() * (w.element_size() + 4) for w in (self.router, self.w1, self.w2))
 
     @staticmethod
-    def _product(rows, weights, plan, transposed=False):
+    def _product(rows, weights, plan, cuts, transposed=False):
         """rows of each expert's range times its weights; in 32 bits, which the operator does not take, by the library."""
-        if rows.dtype != torch.float32:
+        if cuts is None:
             return L.poseidon_expert_product(rows, weights, plan.offsets, transposed=transposed)
         weights = weights if transposed else weights.transpose(1, 2)
-        out, cuts = rows.new_zeros(rows.shape[0], weights.shape[2]), plan.offsets.tolist()
+        out = rows.new_zeros(rows.shape[0], weights.shape[2])
         for e, (a, b) in enumerate(zip(cuts, cuts[1:])):
-            torch.matmul(rows[a:b], weights[e], out=out[a:b])
+            if b > a:
+                torch.matmul(rows[a:b], weights[e], out=out[a:b])
         return out
 
     def forward(self, x):
@@ -205,22 +207,23 @@ class ExpertBlock:
         probs, choice = torch.softmax(logits, 1), choice.to(torch.int32)
         plan = L.poseidon_expert_sort(choice, self.w1.shape[0])
         xs, kept_xs = L.poseidon_expert_gather(x, plan, keep=True)
-        both = self._product(xs, self.w1, plan)
+        cuts = plan.offsets.tolist() if xs.dtype == torch.float32 else None
+        both = self._product(xs, self.w1, plan, cuts)
         act, kept_gate, kept_up = L.poseidon_gated_forward(both[:, :f], both[:, f:])
-        ys = self._product(act, self.w2, plan)
+        ys = self._product(act, self.w2, plan, cuts)
         out = x + L.poseidon_expert_combine(ys, plan, probs)
-        return out, Kept(x, probs, choice, plan, kept_xs, kept_gate, kept_up, L.poseidon_stash(ys))
+        return out, Kept(x, probs, choice, plan, cuts, kept_xs, kept_gate, kept_up, L.poseidon_stash(ys))
 
     def backward(self, dout, kept: Kept):
-        f, plan = self.inner, kept.plan
+        f, plan, cuts = self.inner, kept.plan, kept.cuts
         dys, dprobs = L.poseidon_expert_combine_backward(dout, L.poseidon_restore(kept.ys), plan, kept.probs)
         act = L.poseidon_gated_forward(L.poseidon_restore(kept.gate), L.poseidon_restore(kept.up), keep=False)[0]
         L.poseidon_weight_gradient(dys, L.poseidon_stash(act), offsets=plan.offsets, out=self.dw2, accumulate=True)
-        dact = self._product(dys, self.w2, plan, transposed=True)
+        dact = self._product(dys, self.w2, plan, cuts, transposed=True)
         dboth = act.new_empty(act.shape[0], 2 * f)
         L.poseidon_gated_backward(dact, kept.gate, kept.up, dgate=dboth[:, :f], dup=dboth[:, f:])
         L.poseidon_weight_gradient(dboth, kept.xs, offsets=plan.offsets, out=self.dw1, accumulate=True)
-        dxs = self._product(dboth, self.w1, plan, transposed=True)
+        dxs = self._product(dboth, self.w1, plan, cuts, transposed=True)
         # the router: softmax over the chosen logits, then its product
         dlogits = kept.probs * (dprobs - (kept.probs * dprobs).sum(1, keepdim=True))
         dall = torch.zeros(kept.x.shape[0], self.router.shape[0], dtype=torch.float32, device=dout.device)
