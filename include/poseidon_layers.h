@@ -64,6 +64,7 @@ extern "C" {
 #define POSEIDON_NORM_WIDTH_MAX 16384u     /* values in a row of the norm */
 #define POSEIDON_HEAD_MAX 128u             /* values of an attention head, a multiple of 8 */
 #define POSEIDON_HEADS_MAX 1024u           /* heads of an attention */
+#define POSEIDON_SCALE_MAX 0x1p127f        /* of an attention's scores, either sign */
 
 enum { POSEIDON_F32 = 0, POSEIDON_F16 = 1, POSEIDON_BF16 = 2 };   /* value types */
 
@@ -195,6 +196,8 @@ uint64_t poseidon_norm_backward_workspace(uint64_t rows, uint64_t width);
  * [0, tokens]; tokens before the first and after the last sequence get zeros, their lse -infinity.  Offsets that descend leave
  * it open which tokens are written.  NULL with sequences == 1: all tokens.  POSEIDON_E_RANGE where
  * heads * (tokens / 128 + sequences) passes 2^31 - 256.
+ * |scale| <= POSEIDON_SCALE_MAX.  <q, k>, and the gradients' sums for q and k, are summed in 32 bits before scale
+ * stretches them: what is below 2^-126 there counts as 0.  Where a stretched score passes 2^127 the row's results are NaN.
  * An infinity or a NaN may reach every result of its own sequence, and none of another. */
 int poseidon_attention_forward(const void *q, uint64_t q_token, uint64_t q_head, const void *k, uint64_t k_token,
                                uint64_t k_head, const void *v, uint64_t v_token, uint64_t v_head, uint32_t type,

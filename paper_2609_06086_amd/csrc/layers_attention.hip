@@ -151,6 +151,7 @@ __device__ __forceinline__ Words4 directed(Words4 w, float scale) {
     for (int i = 0; i < 4; ++i) w[i] = (w[i] ^ flip) & keep;
     return w;
 }
+// Of base-2 exponents: finite up to POSEIDON_SCALE_MAX.
 __device__ __forceinline__ float stretch(float scale) { return scale == 0.0f ? kLog2e : fabsf(scale) * kLog2e; }
 
 template <class T>
@@ -690,7 +691,7 @@ inline int check_attention(uint64_t tokens, uint64_t heads, uint64_t kv_heads, u
     if (!heads || !kv_heads || heads % kv_heads || !dim || dim % 8 || !sequences || (!offsets && sequences != 1) ||
         !aligned(offsets, 4) || !(scale > -__builtin_inff() && scale < __builtin_inff()))
         return POSEIDON_E_INVAL;
-    if (tokens > POSEIDON_ROWS_MAX || heads > POSEIDON_HEADS_MAX || dim > POSEIDON_HEAD_MAX || sequences > POSEIDON_ROWS_MAX)
+    if (fabsf(scale) > POSEIDON_SCALE_MAX || tokens > POSEIDON_ROWS_MAX || heads > POSEIDON_HEADS_MAX || dim > POSEIDON_HEAD_MAX || sequences > POSEIDON_ROWS_MAX)
         return POSEIDON_E_RANGE;
     return POSEIDON_OK;
 }
