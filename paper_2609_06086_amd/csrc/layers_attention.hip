@@ -6,6 +6,11 @@
 // the others in LDS.  Products are laid out so that a lane holds one query (key) and its scores of 32 keys (queries)
 // lie in the lane's registers as the next product's operand wants them, up to the order of what is summed over, which the
 // other operand follows: nothing is exchanged between lanes but a row's largest score, and at the end its sum.
+//
+// p and ds go to their products in 16 bits, as the matrix instructions take operands; the sums of p, and all other
+// statistics, are made of what they were before.  In bf16 outputs are off by 0.0018 to 0.0022 of their norm and dq and dk by 0.0027 where
+// the rounding of results alone gives 0.0016.  What the rounding drops could go through products of its own: three in place of two
+// forward, ten in place of seven backward.
 #include "layers_mfma.h"
 
 #include <type_traits>
@@ -260,10 +265,10 @@ __device__ __forceinline__ void clear_token(const Heads &x, uint64_t token, uint
 // WAVES waves of 32 queries each.  The running largest score m follows a row's scores only when one outgrows it by 2^8:
 // the sums then stay below 2^8 times the number of keys, and most tiles leave what was summed alone.
 //
-// Here and in the two kernels below the matrix units bound a long sequence, at the clock that their power leaves; two
-// waves a SIMD, one in its products while the other is in its scores.  16384 tokens, 16 heads of 128 values on 4: 990 us, 1110
-// TFLOP/s of the 1386 to 1596 that large products reach; units busy for 56 % of the time at 1.65 GHz, no bank conflicts.
-// Eight waves a block: 1321 us where four took 1234.
+// Here and in the two kernels below two waves a SIMD, one in its products while the other is in its scores, share it: of 8192 tokens
+// and 32 heads of 128 values on 8 the matrix units take 57 % of the time and vector instructions' issue 48 % (dq: 60 and 38, dk and dv:
+// 61 and 36), so neither alone bounds a long sequence.  16384 tokens, 16 heads on 4: 990 us, 1110 TFLOP/s of the 1386 to 1596 that
+// large products reach, at 1.65 GHz, no bank conflicts.  Eight waves a block: 1321 us where four took 1234.
 template <class T, int D, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void attention_forward_kernel(Attention a) {
     constexpr uint32_t kQueries = 32 * WAVES, kStage = 2 * kTile * D;
@@ -378,7 +383,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_forward_kernel(Attent
 }
 
 // dq, as the forward pass goes, with delta = <dout, out> for the other kernel.  p and ds are rounded to the operands' type.
-// 8192 tokens, 32 heads of 128 values on 8: 745 us, 1107 TFLOP/s; units busy for 59 % of the time at 1.65 GHz.
+// 8192 tokens, 32 heads of 128 values on 8: 745 us, 1107 TFLOP/s, at 1.65 GHz.
 template <class T, int D, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void attention_queries_kernel(Attention a) {
     constexpr uint32_t kQueries = 32 * WAVES, kStage = 2 * kTile * D;
@@ -486,7 +491,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_queries_kernel(Attent
 
 // dk and dv: WAVES waves of 32 keys each go through the queries of every head that shares them, in one order.  With 128
 // values a head the keys, the values and both sums would leave no registers for what is read ahead, so some of the
-// values lie in LDS.  The same 8192 tokens: 965 us, 1139 TFLOP/s; units busy for 61 % at 1.61 GHz.  Eight waves a block: 1905 us
+// values lie in LDS.  The same 8192 tokens: 965 us, 1139 TFLOP/s, at 1.65 GHz.  Eight waves a block: 1905 us
 // where four took 1678; one wave a SIMD with the next scores beside its products: 1772.
 template <class T, int D, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void attention_keys_kernel(Attention a) {

@@ -64,7 +64,7 @@ __device__ __forceinline__ void copy_to_lds(Rsrc from, uint32_t offset, uint16_t
     else
         __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (Place)to, 16, offset, 0, 0, 0);
 }
-constexpr uint32_t kNowhere = 0x80000000u, kBufferBytes = 0x7ffffff0u;
+constexpr uint32_t kNowhere = 0x80000000u;
 
 // Two values rounded to nearest even, in one instruction.
 template <class T>

@@ -4,8 +4,8 @@
 //
 // A team of lanes holds a row in registers, so every operand is read once; memory bounds both directions.  Teams stay for
 // many rows: they read the weights once, and the backward pass holds its sums for dw in registers until its last row.
-// Widths of whole pieces of 16 bytes run at 4.5 to 5.8 TB/s forward and backward up to 8192 values, where a copy of 1 GiB reaches 6.2,
-// wider ones at 3.3 to 5.2 (two slices a lane backward do not fit the registers), odd ones at 3.3 to 4.1.
+// Widths of whole pieces of 16 bytes run at 4.5 to 5.8 TB/s forward and backward up to 8192 values, where a plain copy kernel
+// reaches 6.2 at 1 GiB and the library's copy 5.2, wider ones at 3.3 to 5.2 (two slices a lane backward do not fit the registers), odd ones at 3.3 to 4.1.
 #include "layers_device.h"
 
 #include <type_traits>
@@ -22,9 +22,12 @@ struct Team {
     static __device__ __forceinline__ uint32_t size() { return TEAM == kWhole ? blockDim.x : TEAM; }
 };
 
-// Waves that a SIMD has at a time: what their registers allow.  Forward in 32 bits eight of them would leave registers in
-// memory (32768 x 4096, the sum kept too: 569 us, with six 486).
-// So would six waves backward from 8 bits (32768 x 8192: 528 us, with five 367).
+// Waves that a SIMD has at a time: what their registers allow, but for a few that are kept in memory (forward in 16 bits with one
+// slice 3 to 5, backward from the sum as it is 2 to 3).  Forward in 16 bits: 32768 x 8192 with the residual and the sum kept 438 us,
+// with six or seven waves, which keep none in memory, 471; 21845 x 6144 without what is kept 191 and 186.  Forward in 32 bits
+// eight would keep many there (32768 x 4096, the sum kept too: 569 us, with six 486).
+// So would six waves backward from 8 bits (32768 x 8192: 528 us, with five 367); from the sum as it is 32768 x 4096 takes 193 us
+// with six and 222 with five, in 32 bits 416 and 408.
 template <class T, uint32_t N>
 constexpr uint32_t kForwardWaves = N == 1 ? (T::kShort ? 8 : 6) : 4;
 template <uint32_t TEAM, uint32_t N, bool KEPT>

@@ -56,9 +56,10 @@ __device__ __forceinline__ void clear_outside(const Product &g, uint32_t block, 
 // a quarter of its products is still to come: there the waves meet, the stage's place is given to the one after the
 // next, and the next one's first operands are read beside the last products, so that no wave waits for LDS at a stage's start.
 //
-// The matrix units bound it, at the clock that their power leaves: 16384 rows of 8192 values by 4096 x 8192 take 862 us
-// (1275 TFLOP/s), W^T of 8192 x 4096 1030 us (1068; units busy for 49 % of the time at 1.72 GHz), 64 ragged ranges of 65536 rows by
-// 4096 x 2048 1150 us (956; 50 %, 1.66 GHz); no bank conflicts.  Stages of 32 values with four places: the ragged ranges
+// 16384 rows of 8192 values by 4096 x 8192 take 862 us (1275 TFLOP/s; the library's product 844 to 881), W^T of 8192 x 4096 1030 us
+// (1068; the library's 966 to 1000), 64 ragged ranges of 65536 rows by 4096 x 2048 1150 us (956).  In the last two the matrix units
+// are busy for 51 % of the time at 1.67 GHz, and waves wait for memory, barriers and LDS for 32 % of theirs: a block has its CU
+// alone, so its first loads and its stores have nothing beside them.  No bank conflicts.  Stages of 32 values with four places: the ragged ranges
 // 1530 us where those of 64 took 1347.
 template <class T, bool TURNED, bool ALIGNED, int R, int C, int M, int N, int X>
 __global__ __launch_bounds__(64 * R * C, 2) void product_kernel(Product g) {
@@ -387,8 +388,8 @@ __device__ __forceinline__ Place few_of(const Product &g, uint32_t tile) {
 // whose sum its four waves share, so that even one token's products are blocks for every CU.  A lane takes 16
 // neighbouring values, so that one wave asks for whole lines (16 rows by 8192 x 8192: 33 us, with 8 neighbouring ones 39).
 // One token's 8 ranges of 4096 x 2048, 134 MB of weights: 29 us, 4.6 TB/s; 512
-// rows of 64 such ranges 218 us, 4.9 TB/s.  Eight turns ahead in place of four, or loads
-// marked as read once: no faster, and 3.5 TB/s.
+// rows of 64 such ranges 218 us, 4.9 TB/s.  With one, three and four turns asked for ahead in place of two these are 30, 32 and 26 us, and
+// 219, 252 and 222.
 template <class T>
 __global__ __launch_bounds__(kBlock) void few_rows_kernel(Product g) {
     constexpr uint32_t kEach = 64, kTurn = 4 * kEach;    // values that a wave and the block take in a turn

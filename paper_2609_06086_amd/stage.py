@@ -132,7 +132,7 @@ class AttentionBlock:
         return out, KeptAttention(offsets, y.kept_sum, y.kept_out, y.rstd, both, a, lse)
 
     def backward(self, dout, kept: KeptAttention):
-        a = kept.a.view(dout.shape)
+        a = kept.a.view(dout.shape)    # in 8 bits for its product's gradient, as all weight gradients take rows
         L.poseidon_weight_gradient(dout, L.poseidon_stash(a), out=self.dwo, accumulate=True)
         da = L.poseidon_expert_product(dout, self.wo, transposed=True)
         dboth = torch.empty_like(kept.both)
@@ -305,8 +305,8 @@ def _work_bytes(f, device) -> int:
 
 
 def measure(shape: Shape, device=None, keep_8_bits: bool = True, repeats: int = 5):
-    """(profile of the embedding, profile of an expert block, or with heads of a Layer) on this GPU.  The layers run with their activations kept in 8
-    bits; keep_8_bits False gives those times with the bytes that 16 bits would keep."""
+    """(profile of the embedding, profile of an expert block, or with heads of a Layer) on this GPU.  The layers run with
+    their activations kept in 8 bits; keep_8_bits False gives those times with the bytes that 16 bits would keep."""
     device = torch.device("cuda", torch.cuda.current_device()) if device is None else device
     g = torch.Generator(device=device)
     g.manual_seed(1)
